@@ -418,6 +418,119 @@ HBF_API int hbf_get_retention_blocks(hbf_ctx *ctx, double *damage, uint32_t *dis
 HBF_API int hbf_get_retention_plan(hbf_ctx *ctx, uint32_t *quanta, uint64_t cap, uint64_t *count);
 HBF_API int hbf_get_retention_totals(hbf_ctx *ctx, hbf_retention_totals_t *out);
 
+/* ---- Operators of a served layer whose memory lies in registered ranges -------------------------------------------------
+ * The paper times kernels that really run while their memory lies in HBF ranges (Implementation; its workloads are a
+ * mixture-of-experts model under a serving framework, Evaluation setup).  These calls run the parts of such a layer whose
+ * accesses depend on the data: which experts are read is the router's choice, which cache pages a table's.  Each has a call that
+ * writes the records of what it reads and programs, in the caller's own addresses, for hbf_submit_batch: register
+ * the weights or the cache as a range, run the operator, submit its records.
+ *
+ * They need no context; each runs asynchronously on cuda_stream (a cudaStream_t, NULL = default stream) of the current device, on which
+ * its memory must lie (HBF_E_INVAL otherwise; checked at the weights', the keys' or the pages' pointer).  Argument structs are host
+ * memory and read during the call; every other pointer is device memory, the caller's, and must stay valid until the work has
+ * run.  Strides are in elements.  Nothing is allocated.  d_workspace: device scratch, 256-byte aligned, of the bytes that the operator's
+ * ..._workspace_bytes function gives for the same arguments on the same device (0 = arguments refused); two calls that may overlap,
+ * on two streams or in two graphs that are replayed at once, need one each.  Every call can be captured into a CUDA graph; a replay reads
+ * the tables, lengths and scores anew.  Counts in the structs are fixed at capture.
+ * Values are bf16 or fp16, products exact, sums in 32 bits, outputs rounded once. */
+enum { HBF_BF16 = 0, HBF_FP16 = 1 };
+
+/* A paged key/value cache of one layer: the key of slot s of page g, key head h, begins at k + g * page_stride + s * slot_stride +
+ * h * head_stride; its head_dim elements lie side by side; values alike.  head_dim 64 or 128; any page_tokens up to 2^20; pointers
+ * 16-byte aligned, strides multiples of 8. */
+typedef struct {
+    uint32_t n_pages, page_tokens, kv_heads, head_dim, dtype, pad;
+    const void *k, *v;
+    int64_t page_stride, slot_stride, head_stride;
+} hbf_kv_t;
+
+/* Attention of one decode step for a batch that shares a prefix: for request b and query head h, with key head h / (q_heads /
+ * kv_heads), out = sum_i softmax(scale * q k_i) v_i over the prefix_len keys in prefix_pages and then the own_len[b] keys in
+ * own_pages[b * own_pages_stride ...].  The prefix is read once for the batch.  prefix_pages [ceil(prefix_len / page_tokens)]; own_len
+ * [batch], 0..max_own_len; own_pages_stride >= ceil(max_own_len / page_tokens); with max_own_len 0 both may be NULL.
+ * A row without any key is zeros.  What lies in a page behind a sequence's end is not read into the result, whatever it is.  A page
+ * number outside 0..n_pages-1, or a length outside 0..max_own_len, makes the rows that need it NaN (nothing is read there).
+ * lse (nullable, [batch][q_heads]): natural logarithm of the sum of exp(scale * q k_i), -inf for a row without keys.
+ * q and out: rows and heads at their strides (multiples of 8), 16-byte aligned; out may be q.  Lengths up to HBF_ATTENTION_MAX_LEN. */
+#define HBF_ATTENTION_MAX_LEN (1u << 30)
+typedef struct {
+    hbf_kv_t kv;
+    uint32_t batch, q_heads, prefix_len, max_own_len, own_pages_stride;
+    float scale;
+    const int32_t *prefix_pages, *own_pages, *own_len;
+    const void *q; int64_t q_row_stride, q_head_stride;
+    void *out; int64_t out_row_stride, out_head_stride;
+    float *lse;
+} hbf_attention_t;
+HBF_API size_t hbf_attention_workspace_bytes(const hbf_attention_t *a);
+HBF_API int hbf_prefix_attention(const hbf_attention_t *a, void *d_workspace, size_t workspace_bytes, void *cuda_stream);
+/* Records of the step's reads, n = hbf_attention_access_count(a): two per page (keys, values), whole pages, the prefix's once, then
+ * ceil(max_own_len / page_tokens) pages for every request in turn; record i is issued at issue_ns + i * gap_ns.  Pages that a request does not
+ * have (its length is read on the device), or that are none, give records of one byte at address 0, which is outside every range (so not to be
+ * used with a range registered at 0).  Needs pages that are one stretch of memory (HBF_E_INVAL otherwise).  q and out may be NULL here. */
+HBF_API uint64_t hbf_attention_access_count(const hbf_attention_t *a);
+HBF_API int hbf_attention_accesses(const hbf_attention_t *a, int64_t issue_ns, int64_t gap_ns, hbf_access_t *d_acc, uint64_t n, void *cuda_stream);
+
+/* A mixture-of-experts layer for a few tokens: of scores [tokens][n_experts] (the router's, float) every token's top_k largest, ties
+ * to the lowest expert; weights = softmax over the chosen scores (renormalise 1) or the chosen part of the softmax over all (0);
+ * out[t] = sum over the chosen of weight * down_e (silu(gate_e x_t) * (up_e x_t)).  Expert e's matrices lie one behind the other at experts +
+ * e * expert_stride: gate [inter][hidden], up [inter][hidden], down [hidden][inter].  hidden and inter multiples of 8 up to 2^20, x and experts
+ * 16-byte aligned, x_stride and expert_stride multiples of 8.  silu(..) * (..) * weight is held between the products as the sum of two
+ * numbers of the values' type (in fp16 its magnitude must stay below 65,504, as the output's).
+ * A score of -inf is never chosen; a token with fewer than top_k others has -1 (weight 0) in the places left, and zeros when none is.  A token
+ * with a NaN among its scores has no choice: chosen -1, out NaN.  chosen [tokens][top_k], weights [tokens][top_k]: nullable outputs. */
+#define HBF_MOE_MAX_TOKENS 128
+#define HBF_MOE_MAX_EXPERTS 512
+#define HBF_MOE_MAX_TOP_K 16
+typedef struct {
+    uint32_t tokens, hidden, inter, n_experts, top_k, dtype, renormalise, pad;
+    const void *x; int64_t x_stride;
+    const float *scores; int64_t scores_stride;
+    const void *experts; int64_t expert_stride;
+    void *out; int64_t out_stride;
+    int32_t *chosen;
+    float *weights;
+} hbf_moe_t;
+HBF_API size_t hbf_moe_workspace_bytes(const hbf_moe_t *m);
+HBF_API int hbf_moe_layer(const hbf_moe_t *m, void *d_workspace, size_t workspace_bytes, void *cuda_stream);
+/* Records of the layer's reads, n = hbf_moe_access_count(m, tile_bytes): every expert that some token chose once, ascending, its
+ * matrices in tiles of tile_bytes (the last one shorter); min(n_experts, tokens * top_k) experts have places, the unused ones as above. */
+HBF_API uint64_t hbf_moe_access_count(const hbf_moe_t *m, uint32_t tile_bytes);
+HBF_API int hbf_moe_accesses(const hbf_moe_t *m, uint32_t tile_bytes, int64_t issue_ns, int64_t gap_ns, hbf_access_t *d_acc, uint64_t n, void *cuda_stream);
+
+/* The pages of a cache: n_slabs buffers (the keys and the values of every layer) of n_pages pages each, page g of slab s at base +
+ * s * slab_stride + g * page_stride (bytes; multiples of 16, no two pages overlapping).  refs [n_pages]: how many rows hold a page, 0 = free.
+ * lens [rows]: a row's tokens; tables [rows][table_cols] at table_stride: its pages, of which the first ceil(len / page_tokens) count.
+ *   copy     the bytes of page src[i] to page dst[i] in every slab, for i < n.  refs, lens and tables stay.
+ *   fork     row children[i] (of length 0) becomes row parents[i] as it was before the call: full pages are shared, a begun page is copied
+ *            into a page of its own, the lowest free one, in the order of the list; the rest of the child's table is set to -1.
+ *   free     the rows' pages are held by one row less each, their tables set to -1, their lengths to 0.
+ *   compact  the k-th page in use whose number is not below the number of pages in use moves into the k-th free page below it;
+ *            tables and refs follow.  Afterwards the pages in use are the lowest.  Pages that no table knows move too.
+ * A call that would be wrong changes nothing: its outcome is written to d_result (nullable, int32 [3]: code; pages moved, per slab; pages in
+ * use, compact only): HBF_E_INVAL for a page, row, length or table entry that does not exist or is free, a row or destination
+ * named twice, a source that is a destination, a child that is not empty; HBF_E_CAPACITY when a fork finds too few free pages.  The return
+ * value covers arguments and launches only.  The bytes of freed pages, and of pages that were moved away, stay as they are.
+ * hbf_pages_accesses writes the records of the moves of the call that last used d_workspace: for each moved page and slab a read and a program,
+ * 2 * moved * n_slabs of them; n is the caller's, places behind them as above, records that do not fit are left out. */
+#define HBF_MAX_CACHE_PAGES (1u << 20)
+typedef struct {
+    void *base; uint64_t page_bytes, page_stride, slab_stride;
+    uint32_t n_slabs, n_pages, page_tokens, rows, table_cols, pad;
+    int64_t table_stride;
+    int32_t *refs, *lens, *tables;
+} hbf_pages_t;
+HBF_API size_t hbf_pages_workspace_bytes(const hbf_pages_t *p);
+HBF_API int hbf_pages_copy(const hbf_pages_t *p, const int32_t *d_src, const int32_t *d_dst, uint32_t n, int32_t *d_result, void *d_workspace,
+                           size_t workspace_bytes, void *cuda_stream);
+HBF_API int hbf_pages_fork(const hbf_pages_t *p, const int32_t *d_parents, const int32_t *d_children, uint32_t n, int32_t *d_result,
+                           void *d_workspace, size_t workspace_bytes, void *cuda_stream);
+HBF_API int hbf_pages_free(const hbf_pages_t *p, const int32_t *d_rows, uint32_t n, int32_t *d_result, void *d_workspace,
+                           size_t workspace_bytes, void *cuda_stream);
+HBF_API int hbf_pages_compact(const hbf_pages_t *p, int32_t *d_result, void *d_workspace, size_t workspace_bytes, void *cuda_stream);
+HBF_API int hbf_pages_accesses(const hbf_pages_t *p, const void *d_workspace, int64_t issue_ns, int64_t gap_ns, hbf_access_t *d_acc,
+                               uint64_t n, void *cuda_stream);
+
 HBF_API const char *hbf_strerror(int code);
 
 #ifdef __cplusplus

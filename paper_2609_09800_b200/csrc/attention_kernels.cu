@@ -1,0 +1,435 @@
+// Attention of one decode step for a batch that shares a long prefix: row (request b, query head h) against the prefix's keys, which
+// all rows have in common, and the keys that only request b has, both of key head h / G, in pages:
+//   o = sum_i softmax(scale * q k_i) v_i over the prefix and the request's own keys.
+//
+// The softmax over both is joined from pieces: a piece (some rows, a stretch of keys) leaves its largest score m, its sum of weights
+// l = sum exp(s - m) and sum exp(s - m) v, which add up after scaling by exp(m - M).  So the prefix is read once for
+// all requests (a tile of rows that belong to different requests against the same keys), and long sequences of few requests are cut
+// into enough pieces for the device.
+#include "attention.cuh"
+
+namespace hbf {
+
+constexpr int kAttWarps = 4, kAttThreads = kAttWarps * 32;
+constexpr int kStageKeys = 16;
+template <int D> constexpr int kAttRing = D == 128 ? 3 : 6;  // stages on their way, a warp: 24 KB, 192 KB an SM
+template <int D> constexpr size_t att_smem() { return (size_t)kAttWarps * kAttRing<D> * kStageKeys * D * 4; }
+
+// One piece by four warps: 16 rows (a group's heads of one request, or rows of several requests before the prefix), stages of 16 keys
+// that go to the warps in turn, each with sums of its own, joined at the end.  Keys and values stream through a ring of each
+// warp's own.  The sum over a head's dimensions may take its 16-wide steps in any order, so a lane takes 16 consecutive
+// bytes of a key, copied by itself; values need the transpose, and lie in rows whose 16-byte columns are permuted by the row's number.
+template <class Ty, int D>
+__global__ void __launch_bounds__(kAttThreads)
+k_attend(const __grid_constant__ AttnDev p) {
+    extern __shared__ __align__(128) unsigned char smem[];
+    constexpr int kRing = kAttRing<D>, kBlocks = D / 32, kHalf = kStageKeys * D * 2, kStage = 2 * kHalf;
+    const uint32_t lane = lane_id(), warp = threadIdx.x >> 5, row = lane >> 2, quad = lane & 3u;
+    pdl_trigger();
+    uint32_t item = blockIdx.x, head, tile, piece, b = 0u, begin, end, slot_out;
+    const int32_t *table;
+    uint32_t n_rows;                                         // rows of the tile in use
+    bool bad = false;
+    const bool shared = item < p.n_prefix_items;
+    if (shared) {
+        piece = item % p.prefix_pieces; item /= p.prefix_pieces;
+        tile = item % p.row_tiles; head = item / p.row_tiles;
+        begin = piece * p.prefix_chunk; end = min(p.prefix_len, begin + p.prefix_chunk);
+        table = p.prefix_pages;
+        n_rows = min(16u, p.B * p.G - tile * 16u);
+        slot_out = p.own_pieces + piece;
+    } else {
+        item -= p.n_prefix_items;
+        piece = item % p.own_pieces; item /= p.own_pieces;
+        tile = item % p.group_tiles; item /= p.group_tiles;
+        head = item % p.Hk; b = item / p.Hk;
+        const int32_t len = p.own_len ? p.own_len[b] : 0;
+        bad = len < 0 || (uint32_t)len > p.max_own;
+        begin = piece * p.own_chunk; end = bad ? 0u : min((uint32_t)len, begin + p.own_chunk);
+        table = p.own_pages + (size_t)b * p.own_stride;
+        n_rows = min(16u, p.G - tile * 16u);
+        slot_out = piece;
+    }
+    // row r of the tile: request and query head
+    auto place = [&](uint32_t r, uint32_t &rb, uint32_t &rh) {
+        if (shared) { const uint32_t n = tile * 16u + r; rb = n / p.G; rh = head * p.G + n % p.G; }
+        else { rb = b; rh = head * p.G + tile * 16u + r; }
+    };
+
+    const uint32_t base = smem_addr(smem) + warp * (kRing * kStage);
+    const uint32_t stages = begin < end ? (end - begin + kStageKeys - 1u) / kStageKeys : 0u;
+    uint32_t in = warp, in_slot = 0u;
+    int32_t page0 = 0, page1 = 0; uint32_t at0 = 0u, at1 = 0u;
+    auto look_up = [&]() {                                   // the pages of the next stage's two keys of this lane
+        if (in >= stages) return;
+        const uint32_t k0 = begin + in * kStageKeys + row, k1 = k0 + 8u;
+        const uint32_t n0 = div32(k0, p.div_page), n1 = div32(k1, p.div_page);
+        at0 = k0 - n0 * p.page_tokens; at1 = k1 - n1 * p.page_tokens;
+        if (k0 < end) page0 = table[n0];
+        if (k1 < end) page1 = table[n1];
+    };
+    auto issue = [&]() {
+        if (in < stages) {
+            const uint32_t k0 = begin + in * kStageKeys + row, k1 = k0 + 8u;
+            int64_t o0, o1;
+            bool ok0 = key_place(p, page0, at0, o0), ok1 = key_place(p, page1, at1, o1);
+            bad |= (k0 < end && !ok0) || (k1 < end && !ok1);
+            ok0 &= k0 < end; ok1 &= k1 < end;
+            if (!ok0) o0 = 0;
+            if (!ok1) o1 = 0;
+            const int64_t off = (int64_t)head * p.head_stride + quad * 8u;
+            const uint32_t dst = base + in_slot * kStage;
+#pragma unroll
+            for (int i = 0; i < kBlocks; ++i) {
+                copy_async16(dst + (i * 2) * 512u + lane * 16u, p.k + o0 + off + i * 32, ok0);
+                copy_async16(dst + (i * 2 + 1) * 512u + lane * 16u, p.k + o1 + off + i * 32, ok1);
+            }
+#pragma unroll
+            for (int i = 0; i < kBlocks; ++i) {
+                const uint32_t c = ((quad + 4u * i) ^ row) * 16u;
+                copy_async16(dst + kHalf + row * (D * 2) + c, p.v + o0 + off + i * 32, ok0);
+                copy_async16(dst + kHalf + (row + 8u) * (D * 2) + c, p.v + o1 + off + i * 32, ok1);
+            }
+            in_slot = in_slot + 1u == kRing ? 0u : in_slot + 1u;
+            in += kAttWarps;
+            look_up();
+        }
+        copy_commit();
+    };
+    look_up();
+#pragma unroll
+    for (int i = 0; i < kRing; ++i) issue();
+
+    uint4 q0[kBlocks], q1[kBlocks];                          // this lane's parts of rows `row` and `row + 8`
+    {
+        uint32_t rb, rh;
+        place(row, rb, rh);
+        const uint16_t *s0 = p.q + (int64_t)rb * p.q_row + (int64_t)rh * p.q_head + quad * 8u;
+        place(row + 8u, rb, rh);
+        const uint16_t *s1 = p.q + (int64_t)rb * p.q_row + (int64_t)rh * p.q_head + quad * 8u;
+#pragma unroll
+        for (int i = 0; i < kBlocks; ++i) {
+            q0[i] = row < n_rows ? __ldg(reinterpret_cast<const uint4 *>(s0 + i * 32)) : make_uint4(0u, 0u, 0u, 0u);
+            q1[i] = row + 8u < n_rows ? __ldg(reinterpret_cast<const uint4 *>(s1 + i * 32)) : make_uint4(0u, 0u, 0u, 0u);
+        }
+    }
+    const bool both = n_rows > 8u;
+    float o[D / 8][4], m0 = -INFINITY, m1 = -INFINITY, l0 = 0.0f, l1 = 0.0f;
+#pragma unroll
+    for (int j = 0; j < D / 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.0f;
+    uint32_t slot = 0u;
+    for (uint32_t st = warp; st < stages; st += kAttWarps) {
+        copy_wait<kRing - 1>();
+        __syncwarp();
+        const uint32_t src = base + slot * kStage;
+        slot = slot + 1u == kRing ? 0u : slot + 1u;
+        float s[2][4] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll
+        for (int i = 0; i < kBlocks; ++i) {
+            const uint4 ka = ld_shared16(src + (i * 2) * 512u + lane * 16u), kb = ld_shared16(src + (i * 2 + 1) * 512u + lane * 16u);
+            Ty::mma(s[0], q0[i].x, q1[i].x, q0[i].y, q1[i].y, ka.x, ka.y);
+            Ty::mma(s[1], q0[i].x, q1[i].x, q0[i].y, q1[i].y, kb.x, kb.y);
+            Ty::mma(s[0], q0[i].z, q1[i].z, q0[i].w, q1[i].w, ka.z, ka.w);
+            Ty::mma(s[1], q0[i].z, q1[i].z, q0[i].w, q1[i].w, kb.z, kb.w);
+        }
+        const uint32_t key = begin + st * kStageKeys + quad * 2u;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                s[t][c] *= p.scale_log2;
+                if (key + t * 8u + (c & 1) >= end) s[t][c] = -INFINITY;
+            }
+        // the running maximum of both rows; while it is -inf there is nothing to scale and every weight is 0
+        float a0 = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1])), a1 = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
+        a0 = fmaxf(a0, __shfl_xor_sync(0xffffffffu, a0, 1)); a1 = fmaxf(a1, __shfl_xor_sync(0xffffffffu, a1, 1));
+        a0 = fmaxf(a0, __shfl_xor_sync(0xffffffffu, a0, 2)); a1 = fmaxf(a1, __shfl_xor_sync(0xffffffffu, a1, 2));
+        if (__any_sync(0xffffffffu, a0 > m0 || (both && a1 > m1))) {
+            const float n0 = fmaxf(m0, a0), n1 = fmaxf(m1, a1);
+            const float f0 = n0 == -INFINITY ? 1.0f : exp2_fast(m0 - n0), f1 = n1 == -INFINITY ? 1.0f : exp2_fast(m1 - n1);
+            m0 = n0; m1 = n1; l0 *= f0; l1 *= f1;
+#pragma unroll
+            for (int j = 0; j < D / 8; ++j) { o[j][0] *= f0; o[j][1] *= f0; o[j][2] *= f1; o[j][3] *= f1; }
+        }
+        const float z0 = m0 == -INFINITY ? 0.0f : m0 - Ty::kLift, z1 = m1 == -INFINITY ? 0.0f : m1 - Ty::kLift;
+        // The weights as an A operand (rows, then keys 8 to 15), each as the sum of two numbers of the values' type: rounding them once would
+        // cost as much again as rounding the output does.  The first is rounded down and the second is positive where the weight
+        // is, so that both take an infinite value the same way.
+        uint32_t hi[4], lo[4];
+        auto split = [&](int k, float pa, float pb) {
+            hi[k] = Ty::pack_down(pa, pb);
+            const float2 r = Ty::unpack(hi[k]);
+            lo[k] = Ty::pack(fmaxf(pa - r.x, fminf(pa, Ty::kTiny)), fmaxf(pb - r.y, fminf(pb, Ty::kTiny)));
+        };
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const float p0 = exp2_fast(s[t][0] - z0), p1 = exp2_fast(s[t][1] - z0);
+            l0 += p0 + p1;
+            split(t * 2, p0, p1);
+            hi[t * 2 + 1] = lo[t * 2 + 1] = 0u;
+            if (both) {
+                const float p2 = exp2_fast(s[t][2] - z1), p3 = exp2_fast(s[t][3] - z1);
+                l1 += p2 + p3;
+                split(t * 2 + 1, p2, p3);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) {
+            uint32_t b0, b1, b2, b3;
+            const uint32_t r = (lane & 7u) + ((lane >> 3) & 1u) * 8u, c = j * 2u + (lane >> 4);
+            load_tiles_t(src + kHalf + r * (D * 2) + ((c ^ (r & 7u)) * 16u), b0, b1, b2, b3);
+            Ty::mma(o[j * 2], hi[0], hi[1], hi[2], hi[3], b0, b1);
+            Ty::mma(o[j * 2 + 1], hi[0], hi[1], hi[2], hi[3], b2, b3);
+            Ty::mma(o[j * 2], lo[0], lo[1], lo[2], lo[3], b0, b1);
+            Ty::mma(o[j * 2 + 1], lo[0], lo[1], lo[2], lo[3], b2, b3);
+        }
+        __syncwarp();                                        // every lane has read the values that the next copies replace
+        issue();
+    }
+    l0 += __shfl_xor_sync(0xffffffffu, l0, 1); l1 += __shfl_xor_sync(0xffffffffu, l1, 1);
+    l0 += __shfl_xor_sync(0xffffffffu, l0, 2); l1 += __shfl_xor_sync(0xffffffffu, l1, 2);
+    copy_wait<0>();
+    if (__any_sync(0xffffffffu, bad)) l0 = l1 = __int_as_float(0x7fc00000);         // a page that is none: the row has no answer
+    __syncthreads();                                         // the rings are empty: their memory holds the warps' sums
+    float *os = reinterpret_cast<float *>(smem);
+    __shared__ float2 ml[kAttWarps][16];
+    constexpr int kPitch = D + 4;
+#pragma unroll
+    for (int j = 0; j < D / 8; ++j) {
+        float *d0 = os + ((size_t)warp * 16 + row) * kPitch + j * 8 + quad * 2;
+        *reinterpret_cast<float2 *>(d0) = make_float2(o[j][0], o[j][1]);
+        if (both) *reinterpret_cast<float2 *>(d0 + 8 * kPitch) = make_float2(o[j][2], o[j][3]);
+    }
+    if (quad == 0u) { ml[warp][row] = make_float2(m0 - Ty::kLift, l0); ml[warp][row + 8u] = make_float2(m1 - Ty::kLift, l1); }
+    __syncthreads();
+    constexpr int kLanes = D / 4;                            // threads a row, four dimensions each
+    const uint32_t col = threadIdx.x % kLanes;
+    for (uint32_t r = threadIdx.x / kLanes; r < n_rows; r += kAttThreads / kLanes) {
+        float M = -INFINITY, L = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kAttWarps; ++w) M = fmaxf(M, ml[w][r].x);
+        const float z = M == -INFINITY ? 0.0f : M;
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int w = 0; w < kAttWarps; ++w) {
+            const float f = exp2_fast(ml[w][r].x - z);
+            const float4 x = *reinterpret_cast<const float4 *>(os + ((size_t)w * 16 + r) * kPitch + col * 4u);
+            L += f * ml[w][r].y; v.x += f * x.x; v.y += f * x.y; v.z += f * x.z; v.w += f * x.w;
+        }
+        uint32_t rb, rh;
+        place(r, rb, rh);
+        const size_t n = (size_t)rb * p.Hq + rh;
+        if (p.pieces == 1u) {
+            const float inv = L == 0.0f ? 0.0f : 1.0f / L;   // nothing to attend to: zeros
+            uint2 w2 = make_uint2(Ty::pack(v.x * inv, v.y * inv), Ty::pack(v.z * inv, v.w * inv));
+            *reinterpret_cast<uint2 *>(p.out + (int64_t)rb * p.out_row + (int64_t)rh * p.out_head + col * 4u) = w2;
+            if (p.lse && col == 0u) p.lse[n] = L == 0.0f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
+        } else {
+            const size_t rows = (size_t)p.B * p.Hq;
+            *reinterpret_cast<float4 *>(p.part_o + (slot_out * rows + n) * D + col * 4u) = v;
+            if (col == 0u) p.part_ml[slot_out * rows + n] = make_float2(M, L);
+        }
+    }
+}
+
+// Joins a row's pieces: a block a row, a piece a warp at a time.
+constexpr int kJoinWarps = 8;
+template <class Ty, int D>
+__global__ void __launch_bounds__(kJoinWarps * 32)
+k_attend_join(const __grid_constant__ AttnDev p) {
+    const uint32_t lane = lane_id(), warp = threadIdx.x >> 5, n = blockIdx.x;
+    constexpr int kEach = D / 32;
+    __shared__ float sm[kJoinWarps], sl[kJoinWarps], so[kJoinWarps][D];
+    const size_t rows = (size_t)p.B * p.Hq;
+    pdl_wait();
+    float M = -INFINITY, L = 0.0f, v[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) v[i] = 0.0f;
+#pragma unroll 4
+    for (uint32_t s = warp; s < p.pieces; s += kJoinWarps) {
+        float2 ml; float x[kEach];
+        asm volatile("ld.global.cg.v2.f32 {%0,%1}, [%2];" : "=f"(ml.x), "=f"(ml.y) : "l"(p.part_ml + s * rows + n));
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) asm volatile("ld.global.cg.f32 %0, [%1];" : "=f"(x[i]) : "l"(p.part_o + (s * rows + n) * D + i * 32 + lane));
+        if (ml.y == 0.0f) continue;                          // an empty piece
+        const float N = fmaxf(M, ml.x), z = N == -INFINITY ? 0.0f : N;
+        const float f = exp2_fast(M - z), g = exp2_fast(ml.x - z);
+        M = N; L = L * f + ml.y * g;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) v[i] = v[i] * f + x[i] * g;
+    }
+    if (lane == 0u) { sm[warp] = M; sl[warp] = L; }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) so[warp][i * 32 + lane] = v[i];
+    __syncthreads();
+    if (threadIdx.x >= D) return;
+    M = -INFINITY; L = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) M = fmaxf(M, sm[w]);
+    const float z = M == -INFINITY ? 0.0f : M;
+    float a = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) { const float f = exp2_fast(sm[w] - z); L += f * sl[w]; a += f * so[w][threadIdx.x]; }
+    const uint32_t b = n / p.Hq, h = n - b * p.Hq;
+    const float r = L == 0.0f ? 0.0f : a / L;
+    reinterpret_cast<typename Ty::type *>(p.out)[(int64_t)b * p.out_row + (int64_t)h * p.out_head + threadIdx.x] = Ty::from(r);
+    if (p.lse && threadIdx.x == 0) p.lse[n] = L == 0.0f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
+}
+
+// The records of what a step reads: every page of the prefix once, keys then values, then every request's own pages; the places of pages
+// that a request does not have hold records of one byte at address 0, outside every range.
+__global__ void __launch_bounds__(256)
+k_attend_accesses(const __grid_constant__ AttnDev p, uint32_t prefix_slots, uint32_t own_slots, uint32_t page_bytes, int64_t issue_ns, int64_t gap_ns,
+                  hbf_access_t *acc, uint64_t n) {
+    for (uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256u) {
+        const uint64_t page = i >> 1;
+        int32_t id = -1;
+        if (page < prefix_slots) id = p.prefix_pages[page];
+        else {
+            const uint64_t k = page - prefix_slots;
+            const uint32_t b = (uint32_t)(k / own_slots), s = (uint32_t)(k - (uint64_t)b * own_slots);
+            const int32_t len = p.own_len ? p.own_len[b] : 0;
+            if (len > 0 && (uint32_t)len <= p.max_own && s * p.page_tokens < (uint32_t)len) id = p.own_pages[(size_t)b * p.own_stride + s];
+        }
+        hbf_access_t v = {0, issue_ns + (int64_t)i * gap_ns, 1, 0};
+        if ((uint32_t)id < p.n_pages) {
+            v.addr = (uint64_t)(uintptr_t)((i & 1u ? p.v : p.k) + (int64_t)id * p.page_stride);
+            v.bytes = page_bytes;
+        }
+        acc[i] = v;
+    }
+}
+
+static bool kv_ok(const hbf_kv_t &c) {
+    if (c.n_pages == 0 || c.n_pages > 0x7fffffffu || c.page_tokens == 0 || c.page_tokens > (1u << 20) || c.kv_heads == 0 || c.kv_heads > 1024u) return false;
+    if ((c.head_dim != 64 && c.head_dim != 128) || c.dtype > HBF_FP16) return false;
+    return c.page_stride >= 0 && c.slot_stride >= 0 && c.head_stride >= 0 && c.page_stride % 8 == 0 && c.slot_stride % 8 == 0 && c.head_stride % 8 == 0;
+}
+static bool attention_ok(const hbf_attention_t *a) {
+    if (!a || !kv_ok(a->kv) || a->q_heads == 0 || a->q_heads % a->kv.kv_heads || a->q_heads > 65536u || a->batch > 65536u) return false;
+    if (a->prefix_len > HBF_ATTENTION_MAX_LEN || a->max_own_len > HBF_ATTENTION_MAX_LEN || !(a->scale - a->scale == 0.0f)) return false;
+    return (uint64_t)a->batch * a->q_heads <= (1u << 22);
+}
+static bool attention_pointers_ok(const hbf_attention_t *a) {
+    if (!a->kv.k || !a->kv.v || (uintptr_t)a->kv.k % 16 || (uintptr_t)a->kv.v % 16) return false;
+    if (a->prefix_len && (!a->prefix_pages || (uintptr_t)a->prefix_pages % 4)) return false;
+    if (a->max_own_len && (!a->own_pages || !a->own_len || (uintptr_t)a->own_pages % 4 || (uintptr_t)a->own_len % 4)) return false;
+    if (a->max_own_len && (uint64_t)a->own_pages_stride * a->kv.page_tokens < a->max_own_len) return false;
+    return true;
+}
+
+static uint32_t up_to(uint32_t v, uint32_t m) { return (v + m - 1u) / m * m; }
+
+// How the keys are cut.  A piece costs its start-up (about 2 us to the first values) and d * 4 bytes a row to join, so pieces are as long as
+// leaves about four blocks an SM: at least 64 keys, a multiple of 64, at most 512 of a request's own (whose lengths differ).
+static void attention_pieces(const hbf_attention_t *a, uint32_t n_sm, AttnDev &p) {
+    const uint32_t G = p.G, blocks = 4u * n_sm;
+    p.prefix_rows = 16u;
+    p.row_tiles = (p.B * G + p.prefix_rows - 1u) / p.prefix_rows;
+    p.group_tiles = (G + 15u) / 16u;
+    p.prefix_pieces = 0u; p.prefix_chunk = 64u;
+    if (a->prefix_len) {
+        const uint32_t pairs = p.row_tiles * p.Hk, most = (a->prefix_len + 63u) / 64u;
+        const uint32_t want = blocks > pairs ? blocks / pairs : 1u;
+        p.prefix_chunk = up_to((a->prefix_len + (want < most ? want : most) - 1u) / (want < most ? want : most), 64u);
+        p.prefix_pieces = (a->prefix_len + p.prefix_chunk - 1u) / p.prefix_chunk;
+    }
+    p.own_pieces = 0u; p.own_chunk = 64u;
+    if (a->max_own_len) {
+        const uint64_t lists = (uint64_t)p.B * p.Hk * p.group_tiles;
+        uint64_t chunk = ((uint64_t)a->max_own_len * lists + blocks - 1u) / blocks;
+        chunk = chunk < 64u ? 64u : chunk > 512u ? 512u : chunk;
+        p.own_chunk = up_to((uint32_t)chunk, 64u);
+        p.own_pieces = (a->max_own_len + p.own_chunk - 1u) / p.own_chunk;
+    }
+    p.n_prefix_items = p.prefix_pieces * p.row_tiles * p.Hk;
+    p.pieces = p.own_pieces + p.prefix_pieces;
+}
+
+static AttnDev attention_dev(const hbf_attention_t *a, uint32_t n_sm) {
+    AttnDev p = {};
+    p.k = static_cast<const uint16_t *>(a->kv.k); p.v = static_cast<const uint16_t *>(a->kv.v);
+    p.page_stride = a->kv.page_stride; p.slot_stride = a->kv.slot_stride; p.head_stride = a->kv.head_stride;
+    p.n_pages = a->kv.n_pages; p.Hk = a->kv.kv_heads; p.Hq = a->q_heads; p.G = p.Hq / p.Hk; p.B = a->batch;
+    p.page_tokens = a->kv.page_tokens; p.div_page = make_div32(p.page_tokens);
+    p.q = static_cast<const uint16_t *>(a->q); p.q_row = a->q_row_stride; p.q_head = a->q_head_stride;
+    p.out = static_cast<uint16_t *>(a->out); p.out_row = a->out_row_stride; p.out_head = a->out_head_stride;
+    p.lse = a->lse; p.scale_log2 = a->scale * 1.4426950408889634f;
+    p.prefix_len = a->prefix_len; p.max_own = a->max_own_len; p.own_stride = a->own_pages_stride;
+    p.prefix_pages = a->prefix_pages; p.own_pages = a->own_pages; p.own_len = a->own_len;
+    attention_pieces(a, n_sm, p);
+    return p;
+}
+static size_t attention_bytes(const AttnDev &p, uint32_t dim) {
+    if (p.pieces <= 1u) return 256u;
+    return ((size_t)p.pieces * p.B * p.Hq * (dim * 4u + 8u) + 255u) / 256u * 256u;
+}
+
+template <class Ty, int D>
+static cudaError_t launch_attention(const AttnDev &p, cudaStream_t st) {
+    const uint64_t items = p.n_prefix_items + (uint64_t)p.B * p.Hk * p.group_tiles * p.own_pieces;
+    cudaError_t e = cudaSuccess;
+    if (items) {
+        if ((e = ensure_dyn_smem((const void *)k_attend<Ty, D>, att_smem<D>())) != cudaSuccess) return e;
+        k_attend<Ty, D><<<(unsigned)items, kAttThreads, att_smem<D>(), st>>>(p);
+        g_kernel_launches += 1;
+        if ((e = cudaGetLastError()) != cudaSuccess || p.pieces == 1u) return e;
+    }
+    g_kernel_launches += 1;
+    return launch_pdl(k_attend_join<Ty, D>, p.B * p.Hq, kJoinWarps * 32, 0, st, p);
+}
+
+}  // namespace hbf
+
+using namespace hbf;
+
+extern "C" size_t hbf_attention_workspace_bytes(const hbf_attention_t *a) {
+    uint32_t n_sm = 0;
+    if (!attention_ok(a) || sm_count(&n_sm) != HBF_OK) return 0;
+    return attention_bytes(attention_dev(a, n_sm), a->kv.head_dim);
+}
+
+extern "C" int hbf_prefix_attention(const hbf_attention_t *a, void *d_workspace, size_t workspace_bytes, void *cuda_stream) {
+    if (!attention_ok(a)) return HBF_E_INVAL;
+    if (a->batch == 0) return HBF_OK;
+    if (!attention_pointers_ok(a) || !a->q || !a->out || (uintptr_t)a->q % 16 || (uintptr_t)a->out % 16 || (uintptr_t)a->lse % 4) return HBF_E_INVAL;
+    if (a->q_row_stride % 8 || a->q_head_stride % 8 || a->out_row_stride % 8 || a->out_head_stride % 8) return HBF_E_INVAL;
+    uint32_t n_sm = 0;
+    const int rc = device_of(a->kv.k, &n_sm);
+    if (rc != HBF_OK) return rc;
+    AttnDev p = attention_dev(a, n_sm);
+    if (!d_workspace || (uintptr_t)d_workspace % 256 || workspace_bytes < attention_bytes(p, a->kv.head_dim)) return HBF_E_WORKSPACE;
+    p.part_o = static_cast<float *>(d_workspace);
+    p.part_ml = reinterpret_cast<float2 *>(p.part_o + (size_t)p.pieces * p.B * p.Hq * a->kv.head_dim);
+    const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    cudaError_t e;
+    if (a->kv.dtype == HBF_BF16) e = a->kv.head_dim == 128 ? launch_attention<Bf16, 128>(p, st) : launch_attention<Bf16, 64>(p, st);
+    else e = a->kv.head_dim == 128 ? launch_attention<Fp16, 128>(p, st) : launch_attention<Fp16, 64>(p, st);
+    return e == cudaSuccess ? HBF_OK : HBF_E_CUDA;
+}
+
+static uint64_t attention_records(const hbf_attention_t *a) {
+    const uint64_t own = (a->max_own_len + a->kv.page_tokens - 1) / a->kv.page_tokens, prefix = (a->prefix_len + a->kv.page_tokens - 1) / a->kv.page_tokens;
+    return 2 * (prefix + own * a->batch);
+}
+extern "C" uint64_t hbf_attention_access_count(const hbf_attention_t *a) { return attention_ok(a) ? attention_records(a) : 0; }
+
+extern "C" int hbf_attention_accesses(const hbf_attention_t *a, int64_t issue_ns, int64_t gap_ns, hbf_access_t *d_acc, uint64_t n, void *cuda_stream) {
+    if (!attention_ok(a) || issue_ns < 0 || gap_ns < 0 || n != attention_records(a) || n > HBF_MAX_BATCH) return HBF_E_INVAL;
+    // a page is one stretch of memory, slots and heads side by side in either order
+    const int64_t dim = a->kv.head_dim, slots = a->kv.page_tokens, heads = a->kv.kv_heads;
+    const bool by_slot = a->kv.head_stride == dim && a->kv.slot_stride == dim * heads, by_head = a->kv.slot_stride == dim && a->kv.head_stride == dim * slots;
+    const int64_t bytes = dim * slots * heads * 2;
+    if ((!by_slot && !by_head) || bytes > 0xffffffffll) return HBF_E_INVAL;
+    if (n == 0) return HBF_OK;
+    if (!attention_pointers_ok(a) || !d_acc || (uintptr_t)d_acc % 8) return HBF_E_INVAL;
+    uint32_t n_sm = 0;
+    const int rc = device_of(a->kv.k, &n_sm);
+    if (rc != HBF_OK) return rc;
+    const uint32_t own = (uint32_t)((a->max_own_len + slots - 1) / slots), prefix = (uint32_t)((a->prefix_len + slots - 1) / slots);
+    const uint64_t blocks = (n + 255) / 256;
+    k_attend_accesses<<<(unsigned)(blocks < 8u * n_sm ? blocks : 8u * n_sm), 256, 0, static_cast<cudaStream_t>(cuda_stream)>>>(
+        attention_dev(a, n_sm), prefix, own ? own : 1u, (uint32_t)bytes, issue_ns, gap_ns, d_acc, n);
+    g_kernel_launches += 1;
+    return cudaGetLastError() == cudaSuccess ? HBF_OK : HBF_E_CUDA;
+}

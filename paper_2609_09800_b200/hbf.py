@@ -35,7 +35,11 @@ EXPORTS = ("hbf_create", "hbf_destroy", "hbf_register_range", "hbf_clear_ranges"
            "hbf_rom_create", "hbf_rom_destroy", "hbf_rom_reset", "hbf_rom_step", "hbf_rom_get_state",
            "hbf_attach_rom", "hbf_get_rom_temps",
            "hbf_enable_retention", "hbf_retention_advance", "hbf_retention_decay", "hbf_get_retention_blocks",
-           "hbf_get_retention_plan", "hbf_get_retention_totals")
+           "hbf_get_retention_plan", "hbf_get_retention_totals",
+           "hbf_attention_workspace_bytes", "hbf_prefix_attention", "hbf_attention_access_count", "hbf_attention_accesses",
+           "hbf_moe_workspace_bytes", "hbf_moe_layer", "hbf_moe_access_count", "hbf_moe_accesses",
+           "hbf_pages_workspace_bytes", "hbf_pages_copy", "hbf_pages_fork", "hbf_pages_free", "hbf_pages_compact", "hbf_pages_accesses")
+BF16, FP16 = 0, 1
 STATIC_MAX_CELLS = 65536
 PROF_STAGES = ("begin", "classify", "plan_hist", "sort", "scan", "finish", "inorder", "thermal")
 
@@ -50,6 +54,31 @@ class hbf_retention_config_t(C.Structure):
 class hbf_retention_totals_t(C.Structure):
     _fields_ = [(k, C.c_uint64) for k in ("n_blocks", "planned", "claimed", "decayed", "commits", "worn_blocks",
                                           "waiting_blocks")] + [("epoch", C.c_uint32), ("pad", C.c_uint32)]
+
+
+class hbf_kv_t(C.Structure):
+    _fields_ = [(k, C.c_uint32) for k in ("n_pages", "page_tokens", "kv_heads", "head_dim", "dtype", "pad")] + \
+               [("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64), ("slot_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class hbf_attention_t(C.Structure):
+    _fields_ = [("kv", hbf_kv_t)] + [(k, C.c_uint32) for k in ("batch", "q_heads", "prefix_len", "max_own_len", "own_pages_stride")] + \
+               [("scale", C.c_float), ("prefix_pages", C.c_void_p), ("own_pages", C.c_void_p), ("own_len", C.c_void_p),
+                ("q", C.c_void_p), ("q_row_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("out", C.c_void_p), ("out_row_stride", C.c_int64), ("out_head_stride", C.c_int64), ("lse", C.c_void_p)]
+
+
+class hbf_moe_t(C.Structure):
+    _fields_ = [(k, C.c_uint32) for k in ("tokens", "hidden", "inter", "n_experts", "top_k", "dtype", "renormalise", "pad")] + \
+               [("x", C.c_void_p), ("x_stride", C.c_int64), ("scores", C.c_void_p), ("scores_stride", C.c_int64),
+                ("experts", C.c_void_p), ("expert_stride", C.c_int64), ("out", C.c_void_p), ("out_stride", C.c_int64),
+                ("chosen", C.c_void_p), ("weights", C.c_void_p)]
+
+
+class hbf_pages_t(C.Structure):
+    _fields_ = [("base", C.c_void_p)] + [(k, C.c_uint64) for k in ("page_bytes", "page_stride", "slab_stride")] + \
+               [(k, C.c_uint32) for k in ("n_slabs", "n_pages", "page_tokens", "rows", "table_cols", "pad")] + \
+               [("table_stride", C.c_int64), ("refs", C.c_void_p), ("lens", C.c_void_p), ("tables", C.c_void_p)]
 
 
 class hbf_config_t(C.Structure):
@@ -149,6 +178,23 @@ def lib():
         L.hbf_kernel_launches.argtypes = []
         L.hbf_kernel_launches.restype = u64
         L.hbf_euler_substeps_static.argtypes = [vp, vp, vp, vp, vp, vp, vp, u32, u32, u32, C.c_float, vp]
+        sz = C.c_size_t
+        for name in ("attention", "moe", "pages"):
+            f = getattr(L, "hbf_%s_workspace_bytes" % name)
+            f.argtypes, f.restype = [vp], sz
+        L.hbf_prefix_attention.argtypes = [vp, vp, sz, vp]
+        L.hbf_attention_access_count.argtypes = [vp]
+        L.hbf_attention_access_count.restype = u64
+        L.hbf_attention_accesses.argtypes = [vp, i64, i64, vp, u64, vp]
+        L.hbf_moe_layer.argtypes = [vp, vp, sz, vp]
+        L.hbf_moe_access_count.argtypes = [vp, u32]
+        L.hbf_moe_access_count.restype = u64
+        L.hbf_moe_accesses.argtypes = [vp, u32, i64, i64, vp, u64, vp]
+        L.hbf_pages_copy.argtypes = [vp, vp, vp, u32, vp, vp, sz, vp]
+        L.hbf_pages_fork.argtypes = [vp, vp, vp, u32, vp, vp, sz, vp]
+        L.hbf_pages_free.argtypes = [vp, vp, u32, vp, vp, sz, vp]
+        L.hbf_pages_compact.argtypes = [vp, vp, vp, sz, vp]
+        L.hbf_pages_accesses.argtypes = [vp, vp, i64, i64, vp, u64, vp]
         L.hbf_strerror.argtypes = [C.c_int]
         L.hbf_strerror.restype = C.c_char_p
         _lib = L
@@ -287,6 +333,23 @@ class Context:
         return lib().hbf_submit_batch_paged(self._h, _ptr(d_acc), n, parts_capacity, _ptr(d_completion), _ptr(d_stall),
                                             _ptr(d_status), _ptr(d_die_stats), _ptr(d_workspace),
                                             d_workspace.numel() * d_workspace.element_size())
+
+    def serve(self, op, issue_ns: int = 0, gap_ns: int = 0):
+        """Serves the accesses of an operator's last call (``serving.PrefixAttention``, ``MoeLayer``, ``CachePages``, whose stream
+        has to be this context's): its records, ``hbf_submit_batch``.  Returns (records, completion, stall, die stats) as device tensors:
+        int64 [n, 3], [n], [n], [dies, 6]; the outcome is read with ``last_result``."""
+        torch = self._torch
+        if op.stream.cuda_stream != self.stream.cuda_stream:
+            raise ValueError("the operator runs on another stream than the context")
+        with torch.cuda.stream(self.stream):
+            acc = op.accesses(issue_ns, gap_ns)
+            n = acc.shape[0]
+            comp, stall = (torch.empty(n, dtype=torch.int64, device=acc.device) for _ in range(2))
+            stats = torch.empty(self.n_dies, 6, dtype=torch.int64, device=acc.device)
+            rc = self.submit_batch(acc, n, comp, stall, None, stats)
+        if rc != 0:
+            raise HbfError(rc, "hbf_submit_batch")
+        return acc, comp, stall, stats
 
     def attach_rom(self, rom, output_kind=None, dt_ns=0):
         """Thermal steps on a reduced-order model (a ``Rom`` created on this context's stream) instead of the grid;

@@ -1,0 +1,262 @@
+"""Operators of a served layer whose memory lies in registered ranges (``include/hbf.h``): thin classes over the C calls.
+
+An object keeps what a serving loop keeps between calls (the argument struct, the workspace); its calls run on the stream it was
+made for, like a ``Context``'s, allocate nothing when the outputs are given, and wait for nothing.  ``accesses`` gives the records of
+what the last call read and programmed, for ``Context.serve`` or ``Context.submit_batch``.  There is no CPU fallback.
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+from . import hbf
+
+_RECORD_WORDS = 3                                             # a 24-byte access record as int64
+
+
+def _check(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+class _Operator:
+    def __init__(self, anchor, stream):
+        import torch
+        if not torch.cuda.is_available():
+            raise RuntimeError("hbf needs a CUDA device; there is no CPU fallback")
+        self._torch = torch
+        self._lib = hbf.lib()
+        self.device = anchor.device
+        _check(anchor.is_cuda and self.device.index == torch.cuda.current_device(), "the operator's memory is not on the current CUDA device")
+        self.stream = stream if stream is not None else torch.cuda.current_stream()
+        _check(self.stream.device == self.device, "the stream belongs to another device")
+        self._st = self.stream.cuda_stream
+
+    def _int32(self, t, what, dims):
+        _check(t.dtype == self._torch.int32 and t.dim() == dims and t.device == self.device and (t.numel() == 0 or t.stride(-1) == 1),
+               "%s has to be an int32 tensor of %d dimension(s) on %s" % (what, dims, self.device))
+        return t
+
+    def _room(self, nbytes):
+        if nbytes == 0:
+            raise hbf.HbfError(hbf.E_INVAL, type(self).__name__)
+        with self._torch.cuda.stream(self.stream):
+            return self._torch.empty(nbytes, dtype=self._torch.uint8, device=self.device)
+
+    def _records(self, n):
+        with self._torch.cuda.stream(self.stream):
+            return self._torch.empty(n, _RECORD_WORDS, dtype=self._torch.int64, device=self.device)
+
+    def _raise(self, rc, what):
+        if rc != 0:
+            raise hbf.HbfError(rc, what)
+
+
+def _dtype_of(t, torch):
+    _check(t.dtype in (torch.bfloat16, torch.float16), "values have to be bfloat16 or float16")
+    return hbf.BF16 if t.dtype == torch.bfloat16 else hbf.FP16
+
+
+class PrefixAttention(_Operator):
+    """``hbf_prefix_attention``: one decode step's attention for a batch that shares a prefix.
+
+    k, v: [pages, page_tokens, kv_heads, head_dim], alike in strides, the last dimension dense (a view with pages of [kv_heads, page_tokens,
+    head_dim] transposed will do).  prefix_pages: int32 [>= ceil(prefix_len / page_tokens)].  own_pages: int32 [batch, columns], own_len: int32
+    [batch], both read anew at every call; max_own_len bounds the lengths.  scale defaults to head_dim ** -0.5."""
+
+    def __init__(self, k, v, batch, q_heads, prefix_pages=None, prefix_len=0, own_pages=None, own_len=None, max_own_len=0, scale=None, stream=None):
+        super().__init__(k, stream)
+        torch = self._torch
+        _check(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and v.device == self.device and k.stride(3) == 1,
+               "k and v have to be alike: [pages, page_tokens, kv_heads, head_dim], dense in the last dimension")
+        a = self._a = hbf.hbf_attention_t()
+        a.kv.n_pages, a.kv.page_tokens, a.kv.kv_heads, a.kv.head_dim = k.shape
+        a.kv.dtype = _dtype_of(k, torch)
+        a.kv.k, a.kv.v = k.data_ptr(), v.data_ptr()
+        a.kv.page_stride, a.kv.slot_stride, a.kv.head_stride = k.stride()[:3]
+        a.batch, a.q_heads, a.prefix_len, a.max_own_len = batch, q_heads, prefix_len, max_own_len
+        a.scale = scale if scale is not None else a.kv.head_dim ** -0.5
+        pages_for = lambda n: -(-n // a.kv.page_tokens)
+        if prefix_len:
+            self._int32(prefix_pages, "prefix_pages", 1)
+            _check(prefix_pages.numel() >= pages_for(prefix_len), "prefix_pages is shorter than the prefix")
+            a.prefix_pages = prefix_pages.data_ptr()
+        if max_own_len:
+            self._int32(own_pages, "own_pages", 2), self._int32(own_len, "own_len", 1)
+            _check(own_pages.shape[0] == batch and own_len.numel() == batch and own_pages.shape[1] >= pages_for(max_own_len) and
+                   (batch < 2 or own_pages.stride(0) >= own_pages.shape[1]), "own_pages or own_len does not hold the batch's own keys")
+            a.own_pages, a.own_len = own_pages.data_ptr(), own_len.data_ptr()
+            a.own_pages_stride = own_pages.stride(0) if batch > 1 else own_pages.shape[1]
+        self._keep = (k, v, prefix_pages, own_pages, own_len)
+        self._ref = C.byref(a)
+        self._ws = self._room(self._lib.hbf_attention_workspace_bytes(self._ref))
+        self._ws_ptr, self._ws_bytes = self._ws.data_ptr(), self._ws.numel()
+        self._shape, self._dtype = torch.Size((batch, q_heads, k.shape[3])), k.dtype
+
+    def __call__(self, q, out=None, lse=None):
+        """q: [batch, q_heads, head_dim]; returns out (made if not given).  lse: float32 [batch, q_heads], filled if given."""
+        if out is None:
+            with self._torch.cuda.stream(self.stream):
+                out = self._torch.empty(self._shape, dtype=self._dtype, device=self.device)
+        for t in (q, out):
+            if t.shape != self._shape or t.dtype != self._dtype or t.device != self.device or t.stride(2) != 1:
+                raise ValueError("q and out have to be [batch, q_heads, head_dim] of the cache's type, dense in the last dimension")
+        if lse is not None:
+            _check(lse.shape == self._shape[:2] and lse.dtype == self._torch.float32 and lse.device == self.device and lse.is_contiguous(), "lse has to be float32 [batch, q_heads]")
+        a = self._a
+        a.q, a.out, a.lse = q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr()
+        a.q_row_stride, a.q_head_stride, _ = q.stride()
+        a.out_row_stride, a.out_head_stride, _ = out.stride()
+        rc = self._lib.hbf_prefix_attention(self._ref, self._ws_ptr, self._ws_bytes, self._st)
+        if rc:
+            self._raise(rc, "hbf_prefix_attention")
+        return out
+
+    def access_count(self):
+        return self._lib.hbf_attention_access_count(self._ref)
+
+    def accesses(self, issue_ns=0, gap_ns=0, out=None):
+        """Records of the pages that a call reads, the prefix's once: int64 [n, 3]."""
+        n = self.access_count()
+        out = self._records(n) if out is None else out
+        self._raise(self._lib.hbf_attention_accesses(self._ref, issue_ns, gap_ns, out.data_ptr(), n, self._st), "hbf_attention_accesses")
+        return out
+
+
+class MoeLayer(_Operator):
+    """``hbf_moe_layer``: a mixture-of-experts layer for up to max_tokens (128 at most) tokens.
+
+    experts: [n_experts, >= 3 * inter * hidden], a row an expert's gate, up and down one behind the other.  tile_bytes: size of the
+    records that ``accesses`` writes."""
+
+    def __init__(self, experts, hidden, inter, top_k, max_tokens, renormalise=True, tile_bytes=65536, stream=None):
+        super().__init__(experts, stream)
+        _check(experts.dim() == 2 and experts.shape[1] >= 3 * hidden * inter and experts.stride(1) == 1, "experts has to be [n_experts, >= 3 * inter * hidden], rows dense")
+        m = self._m = hbf.hbf_moe_t()
+        m.tokens, m.hidden, m.inter, m.n_experts, m.top_k = max_tokens, hidden, inter, experts.shape[0], top_k
+        m.dtype, m.renormalise = _dtype_of(experts, self._torch), 1 if renormalise else 0
+        m.experts, m.expert_stride = experts.data_ptr(), experts.stride(0) if experts.shape[0] > 1 else max(experts.stride(0), 3 * hidden * inter)
+        self._keep = experts
+        self._ref = C.byref(m)
+        _check(max_tokens >= 1, "max_tokens has to be at least 1")
+        self._ws = self._room(self._lib.hbf_moe_workspace_bytes(self._ref))
+        self._ws_ptr, self._ws_bytes = self._ws.data_ptr(), self._ws.numel()
+        self._dtype, self.max_tokens, self.tile_bytes = experts.dtype, max_tokens, tile_bytes
+        self._last = None
+
+    def __call__(self, x, scores, out=None, chosen=None, weights=None):
+        """x: [tokens, hidden]; scores: float32 [tokens, n_experts]; returns out (made if not given).  chosen (int32) and weights (float32), both
+        [tokens, top_k] and contiguous, are filled if given."""
+        torch, m = self._torch, self._m
+        if out is None:
+            with torch.cuda.stream(self.stream):
+                out = torch.empty(x.shape, dtype=self._dtype, device=self.device)
+        n = x.shape[0]
+        for t in (x, out):
+            if t.dim() != 2 or t.shape[0] != n or t.shape[1] != m.hidden or n > self.max_tokens or t.dtype != self._dtype or t.device != self.device or t.stride(1) != 1:
+                raise ValueError("x and out have to be [tokens <= max_tokens, hidden] of the experts' type, rows dense")
+        if scores.shape != (n, m.n_experts) or scores.dtype != torch.float32 or scores.device != self.device or scores.stride(1) != 1:
+            raise ValueError("scores has to be float32 [tokens, n_experts], rows dense")
+        for t, dt in ((chosen, torch.int32), (weights, torch.float32)):
+            if t is not None and (t.shape != (n, m.top_k) or t.dtype != dt or t.device != self.device or not t.is_contiguous()):
+                raise ValueError("chosen (int32) and weights (float32) have to be [tokens, top_k], contiguous")
+        m.tokens = n
+        m.x, m.x_stride = x.data_ptr(), x.stride(0) if n > 1 else m.hidden
+        m.scores, m.scores_stride = scores.data_ptr(), scores.stride(0) if n > 1 else m.n_experts
+        m.out, m.out_stride = out.data_ptr(), out.stride(0) if n > 1 else m.hidden
+        m.chosen, m.weights = None if chosen is None else chosen.data_ptr(), None if weights is None else weights.data_ptr()
+        rc = self._lib.hbf_moe_layer(self._ref, self._ws_ptr, self._ws_bytes, self._st)
+        if rc:
+            self._raise(rc, "hbf_moe_layer")
+        self._last = scores                                  # `accesses` makes the choice again
+        return out
+
+    def access_count(self):
+        return self._lib.hbf_moe_access_count(self._ref, self.tile_bytes) if self._last is not None else 0
+
+    def accesses(self, issue_ns=0, gap_ns=0, out=None):
+        """Records of the experts that the last call read, from its scores as they are now: int64 [n, 3]."""
+        n = self.access_count()
+        out = self._records(n) if out is None else out
+        self._raise(self._lib.hbf_moe_accesses(self._ref, self.tile_bytes, issue_ns, gap_ns, out.data_ptr(), n, self._st) if n else 0, "hbf_moe_accesses")
+        return out
+
+
+class CachePages(_Operator):
+    """``hbf_pages_*``: the pages of a key/value cache, with the bookkeeping of who holds them.
+
+    data: [slabs, pages, ...], a page dense; refs: int32 [pages]; tables: int32 [rows, columns]; lens: int32 [rows]; all changed in place.  Calls
+    are asynchronous; ``result`` waits for the last one and raises if it was refused."""
+
+    def __init__(self, data, refs, tables, lens, page_tokens, stream=None):
+        super().__init__(data, stream)
+        torch = self._torch
+        _check(data.dim() >= 3 and data[0, 0].is_contiguous(), "data has to be [slabs, pages, ...] with dense pages")
+        self._int32(refs, "refs", 1), self._int32(tables, "tables", 2), self._int32(lens, "lens", 1)
+        _check(refs.numel() == data.shape[1] and lens.numel() == tables.shape[0], "refs has to hold the pages, lens the rows")
+        p = self._p = hbf.hbf_pages_t()
+        size = data.element_size()
+        p.base, p.page_bytes = data.data_ptr(), data[0, 0].numel() * size
+        p.n_slabs, p.n_pages, p.page_tokens = data.shape[0], data.shape[1], page_tokens
+        p.page_stride = data.stride(1) * size if p.n_pages > 1 else p.page_bytes
+        p.slab_stride = data.stride(0) * size if p.n_slabs > 1 else p.page_bytes * p.n_pages
+        p.rows, p.table_cols = tables.shape
+        p.table_stride = tables.stride(0) if p.rows > 1 else p.table_cols
+        p.refs, p.lens, p.tables = refs.data_ptr(), lens.data_ptr(), tables.data_ptr()
+        self._keep = (data, refs, tables, lens)
+        self._ref = C.byref(p)
+        self._ws = self._room(self._lib.hbf_pages_workspace_bytes(self._ref))
+        self._ws_ptr, self._ws_bytes = self._ws.data_ptr(), self._ws.numel()
+        with torch.cuda.stream(self.stream):
+            self._result = torch.zeros(3, dtype=torch.int32, device=self.device)
+        self._res_ptr = self._result.data_ptr()
+        self._what, self._moves = "", 0
+
+    def _list(self, t, what):
+        if t.dtype != self._torch.int32 or t.dim() != 1 or t.device != self.device or not t.is_contiguous():
+            raise ValueError("%s has to be a contiguous int32 tensor of one dimension on %s" % (what, self.device))
+        return t.data_ptr()
+
+    def _done(self, rc, what, moves):
+        self._what, self._moves = what, moves
+        if rc:
+            self._raise(rc, what)
+
+    def copy(self, src, dst):
+        """Page src[i]'s bytes to page dst[i], in every slab."""
+        n = src.numel()
+        _check(dst.numel() == n, "src and dst differ in length")
+        self._done(self._lib.hbf_pages_copy(self._ref, self._list(src, "src"), self._list(dst, "dst"), n, self._res_ptr, self._ws_ptr, self._ws_bytes, self._st),
+                   "hbf_pages_copy", n)
+
+    def fork(self, parents, children):
+        """Row children[i], empty, becomes row parents[i]: full pages shared, a begun one copied."""
+        n = parents.numel()
+        _check(children.numel() == n, "parents and children differ in length")
+        self._done(self._lib.hbf_pages_fork(self._ref, self._list(parents, "parents"), self._list(children, "children"), n, self._res_ptr, self._ws_ptr,
+                                            self._ws_bytes, self._st), "hbf_pages_fork", n)
+
+    def free(self, rows):
+        """Gives the rows' pages back."""
+        self._done(self._lib.hbf_pages_free(self._ref, self._list(rows, "rows"), rows.numel(), self._res_ptr, self._ws_ptr, self._ws_bytes, self._st), "hbf_pages_free", 0)
+
+    def compact(self):
+        """Moves the pages in use to the lowest numbers."""
+        self._done(self._lib.hbf_pages_compact(self._ref, self._res_ptr, self._ws_ptr, self._ws_bytes, self._st), "hbf_pages_compact", self._p.n_pages // 2)
+
+    def result(self):
+        """Waits for the last call: {"moved": pages moved, "in_use": pages in use (compact only)}; HbfError if it was refused."""
+        with self._torch.cuda.stream(self.stream):
+            code, moved, in_use = self._result.tolist()
+        self._raise(code, self._what)
+        return {"moved": moved, "in_use": in_use}
+
+    def access_count(self):
+        return 2 * self._moves * self._p.n_slabs
+
+    def accesses(self, issue_ns=0, gap_ns=0, out=None):
+        """Records of the last call's moves, a read and a program for each page and slab: int64 [n, 3]; n is the most that the call can have
+        moved, places past its moves are native."""
+        n = self.access_count()
+        out = self._records(n) if out is None else out
+        self._raise(self._lib.hbf_pages_accesses(self._ref, self._ws_ptr, issue_ns, gap_ns, out.data_ptr(), n, self._st) if n else 0, "hbf_pages_accesses")
+        return out
