@@ -5,19 +5,16 @@
 //   k_moe_down  out[token] = sum over its experts of down h
 //
 // Bytes bound it: an expert's 6 * inter * hidden bytes are read once, whatever the number of its tokens (a few).  So the weights go
-// from HBM past L1 into rings of shared memory and from there, as they lie, into the A operand of m16n8k16 products whose
-// columns are tokens; no tile is ever padded to more than 8 tokens.  The order in which a product sums its 16-wide steps is free, so
-// every lane takes 16 consecutive bytes of its row (two steps' worth) from weights and activations alike, and reads back
-// only what it copied itself: no transposition, no barrier in the stream.
+// from HBM past L1 into rings of shared memory, 16 bytes a lane at a time, and from there, as they lie, into the A operand of m16n8k16
+// products whose columns are tokens; no tile is ever padded to more than 8 tokens.  The order in which a product sums its 16-wide steps
+// is free, so every lane takes 16 consecutive bytes of its row (two steps' worth) from weights and activations alike, and reads back only
+// what it copied itself: no transposition, no barrier in the stream.  (Bulk copies of a row's stretch by a warp of their own, which need fewer
+// instructions, were slower throughout: 64 tokens 556 us against 272, the copies of 0.5 to 1 KB leave the SM one after the other.)
 #include "tensor_ops.cuh"
 
 namespace hbf {
 
 constexpr int kMoeWarps = 16, kMoeThreads = kMoeWarps * 32;
-constexpr int kMoeChunk = 32;                                // tokens of one expert that an item of the up kernel takes
-constexpr int kUpRing = 5;                                   // 32-wide steps on their way, a warp: 80 KB of weights an SM
-constexpr int kDownRing = 8;                                 // 128 KB an SM
-constexpr int kUpStep = 1536, kDownStep = 1024;              // bytes a step: 16 rows of weights; 8 rows of activations
 
 struct MoeDev {
     uint32_t T, D, I, E, K, renorm;
@@ -28,20 +25,30 @@ struct MoeDev {
     int32_t *chosen; float *weights;
     uint16_t *h_hi, *h_lo;                                   // [pairs by expert, then token][I]
     uint32_t rows;                                           // of the down product that a block takes, at most 16
-    Div32 div_slices, div_steps;                             // ceil(I / 8); ceil(I / 32)
+    Div32 div_slices, div_k;                                 // I / 8; K
 };
 
-// What the choice leaves in shared memory, the same in every block that makes it.
+// What the choice leaves in shared memory, the same in every block that makes it.  An entry is an expert in use with up to `chunk` of its
+// tokens; entries by expert, pairs (expert, token) by entry.
+template <int kTokens>
 struct Route {
-    uint32_t mask[HBF_MOE_MAX_EXPERTS][HBF_MOE_MAX_TOKENS / 32];     // tokens of each expert
+    static constexpr int kWords = (kTokens + 31) / 32, kPairs = kTokens * HBF_MOE_MAX_TOP_K, kEntries = HBF_MOE_MAX_EXPERTS + kPairs / 8;
+    uint32_t mask[HBF_MOE_MAX_EXPERTS][kWords];                      // tokens of each expert
     uint16_t base[HBF_MOE_MAX_EXPERTS];                              // pairs of the experts before it
     uint16_t active[HBF_MOE_MAX_EXPERTS];                            // experts in use, ascending
-    uint16_t entry[HBF_MOE_MAX_EXPERTS + HBF_MOE_MAX_TOKENS * HBF_MOE_MAX_TOP_K / kMoeChunk];   // expert * 8 + chunk of its tokens
-    uint8_t token[HBF_MOE_MAX_TOKENS * HBF_MOE_MAX_TOP_K];           // of each pair
-    float weight[HBF_MOE_MAX_TOKENS * HBF_MOE_MAX_TOP_K];
-    uint32_t bad[HBF_MOE_MAX_TOKENS / 32];                           // tokens with a NaN among their scores
+    uint16_t expert[kEntries], pair0[kEntries];
+    uint8_t count[kEntries];
+    uint8_t token[kPairs];                                           // of each pair
+    float weight[kPairs];
+    uint32_t bad[kWords];                                            // tokens with a NaN among their scores
     uint32_t n_active, n_entries, scan[kMoeWarps][3];
 };
+template <int kTokens>
+struct RouteTemp {                                                   // of the choice itself; the memory is used again behind it
+    uint16_t expert[kTokens * HBF_MOE_MAX_TOP_K];
+    float weight[kTokens * HBF_MOE_MAX_TOP_K];
+};
+template <int kTokens> constexpr uint32_t kRouteBytes = (sizeof(Route<kTokens>) + 127u) / 128u * 128u;
 
 __device__ __forceinline__ uint32_t ordered(float f) {              // larger scores, larger keys; -inf (never chosen): 0
     const uint32_t u = __float_as_uint(f + 0.0f);           // (-0 and 0 tie)
@@ -55,85 +62,120 @@ __device__ __forceinline__ float warp_sum_f(float v) {
     return v;
 }
 
-// One token's choice by one warp: lane j < K holds the j-th chosen expert (-1: none left) and its weight.  Sixteen keys a lane at most.
-__device__ __forceinline__ bool choose(const MoeDev &m, uint32_t t, int &expert, float &weight) {
-    constexpr int kMost = HBF_MOE_MAX_EXPERTS / 32;
+// The choice of kTok tokens t0, t0 + step, ... by one warp, kKeys neighbouring scores a lane.  A turn finds the largest score left (the lowest lane
+// that has it, and the lowest of its experts, win a tie); the tokens' turns do not depend on one another, so several of them hide
+// each other's latency.  Left in `tmp`: the chosen experts (0xffff: none left), and their scores' keys as the bits of the weights.
+template <int kKeys, int kTok, int kTokens>
+__device__ __forceinline__ void choose(const MoeDev &m, Route<kTokens> &r, RouteTemp<kTokens> &tmp, uint32_t t0, uint32_t step, bool write) {
     const uint32_t lane = lane_id();
-    const float *s = m.scores + (int64_t)t * m.scores_stride;
-    uint32_t key[kMost];
-    bool nan = false;
+    uint32_t key[kTok][kKeys], first[kTok];
+    float all[kTok];
+    bool live[kTok];
 #pragma unroll
-    for (int i = 0; i < kMost; ++i) {
-        key[i] = 0u;
-        if (i * 32u < m.E) {
-            const uint32_t e = i * 32u + lane;
-            if (e < m.E) { const float f = s[e]; nan |= f != f; key[i] = ordered(f); }
+    for (int t = 0; t < kTok; ++t) {
+        const uint32_t tok = t0 + t * step;
+        const float *s = m.scores + (int64_t)tok * m.scores_stride;
+#pragma unroll
+        for (int i = 0; i < kKeys; ++i) {
+            const uint32_t e = lane * kKeys + i;
+            key[t][i] = __float_as_uint(tok < m.T && e < m.E ? s[e] : -INFINITY);
         }
     }
-    expert = -1; weight = 0.0f;
-    if (__any_sync(0xffffffffu, nan)) return false;
-    float all = 0.0f;
-    uint32_t mine = 0u, first = 0u;
+#pragma unroll
+    for (int t = 0; t < kTok; ++t) {
+        bool nan = false;
+#pragma unroll
+        for (int i = 0; i < kKeys; ++i) { const float f = __uint_as_float(key[t][i]); nan |= f != f; key[t][i] = ordered(f); }
+        nan = __any_sync(0xffffffffu, nan);
+        const uint32_t tok = t0 + t * step;
+        live[t] = tok < m.T && !nan;
+        if (nan && lane == 0u) atomicOr(&r.bad[tok >> 5], 1u << (tok & 31u));
+        first[t] = 0u; all[t] = 0.0f;
+        if (tok < m.T && lane < m.K) tmp.expert[tok * m.K + lane] = 0xffffu;
+    }
+    __syncwarp();
+#pragma unroll 1
     for (uint32_t j = 0; j < m.K; ++j) {
-        uint32_t best = 0u;
+        uint32_t best[kTok];
 #pragma unroll
-        for (int i = 0; i < kMost; ++i) best = max(best, key[i]);
-        best = __reduce_max_sync(0xffffffffu, best);
-        if (best == 0u) break;
-        uint32_t at = 0xffffffffu;
+        for (int t = 0; t < kTok; ++t) {
+            best[t] = key[t][0];
 #pragma unroll
-        for (int i = kMost - 1; i >= 0; --i) if (key[i] == best) at = i * 32u + lane;
-        at = __reduce_min_sync(0xffffffffu, at);
-        if (j == 0) {
-            first = best;
-            if (!m.renorm) {
+            for (int i = 1; i < kKeys; ++i) best[t] = max(best[t], key[t][i]);
+        }
 #pragma unroll
-                for (int i = 0; i < kMost; ++i) if (key[i]) all += expf(from_ordered(key[i]) - from_ordered(first));
-                all = warp_sum_f(all);
+        for (int t = 0; t < kTok; ++t) best[t] = __reduce_max_sync(0xffffffffu, best[t]);
+#pragma unroll
+        for (int t = 0; t < kTok; ++t) {
+            if (j == 0u) {
+                first[t] = best[t];
+                if (!m.renorm)
+#pragma unroll
+                    for (int i = 0; i < kKeys; ++i) all[t] += key[t][i] ? expf(from_ordered(key[t][i]) - from_ordered(first[t])) : 0.0f;
+            }
+            uint32_t at = kKeys;
+#pragma unroll
+            for (int i = kKeys - 1; i >= 0; --i) if (key[t][i] == best[t]) at = i;
+            const unsigned has = __ballot_sync(0xffffffffu, at < kKeys);
+            if (live[t] && best[t] && lane == __ffs(has) - 1u) {
+                const uint32_t tok = t0 + t * step, e = lane * kKeys + at;
+                tmp.expert[tok * m.K + j] = (uint16_t)e; tmp.weight[tok * m.K + j] = __uint_as_float(best[t]);
+                atomicOr(&r.mask[e][tok >> 5], 1u << (tok & 31u));
+                if (m.renorm) all[t] += expf(from_ordered(best[t]) - from_ordered(first[t]));
+#pragma unroll
+                for (int i = 0; i < kKeys; ++i) if (i == (int)at) key[t][i] = 0u;
             }
         }
-        if (lane == j) { expert = (int)at; mine = best; }
-#pragma unroll
-        for (int i = 0; i < kMost; ++i) if (i * 32u + lane == at) key[i] = 0u;
     }
-    const float p = expert >= 0 ? expf(from_ordered(mine) - from_ordered(first)) : 0.0f;
-    if (m.renorm) all = warp_sum_f(p);
-    if (expert >= 0) weight = p / all;
-    return true;
+    __syncwarp();
+#pragma unroll
+    for (int t = 0; t < kTok; ++t) {
+        const uint32_t tok = t0 + t * step, at = tok * m.K + lane;
+        const float sum = warp_sum_f(all[t]);
+        if (tok < m.T && lane < m.K) {
+            const uint32_t e = tmp.expert[at];
+            const float w = e == 0xffffu ? 0.0f : expf(from_ordered(__float_as_uint(tmp.weight[at])) - from_ordered(first[t])) / sum;
+            tmp.weight[at] = w;
+            if (write) {
+                if (m.chosen) m.chosen[at] = e == 0xffffu ? -1 : (int32_t)e;
+                if (m.weights) m.weights[at] = w;
+            }
+        }
+    }
 }
 
-// The whole batch's choice: about 1 us for a token and 16 warps, hidden in the down kernel behind the kernel before it.
-__device__ void route(const MoeDev &m, Route &r, bool write) {
-    constexpr int kMine = HBF_MOE_MAX_TOKENS / kMoeWarps;
+// The whole batch's choice by a block.  Every block of both kernels makes it for itself, which costs less than a kernel of its
+// own in front would.
+template <int kKeys, int kTok, int kTokens>
+__device__ __forceinline__ void route_tokens(const MoeDev &m, Route<kTokens> &r, RouteTemp<kTokens> &tmp, bool write) {
+    constexpr uint32_t kWarps = kMoeWarps;
+#pragma unroll 1
+    for (uint32_t t = threadIdx.x >> 5; t < m.T; t += kWarps * kTok) choose<kKeys, kTok>(m, r, tmp, t, kWarps, write);
+}
+template <int kTokens>
+__device__ __forceinline__ void route(const MoeDev &m, Route<kTokens> &r, RouteTemp<kTokens> &tmp, uint32_t chunk, bool write) {
+    constexpr int kEach = HBF_MOE_MAX_EXPERTS / kMoeThreads, kWords = Route<kTokens>::kWords;  // experts a thread in the scan, side by side
     const uint32_t tid = threadIdx.x, lane = lane_id(), warp = tid >> 5;
-    for (uint32_t i = tid; i < m.E * 4u; i += kMoeThreads) r.mask[i >> 2][i & 3u] = 0u;
-    if (tid < HBF_MOE_MAX_TOKENS / 32) r.bad[tid] = 0u;
+    for (uint32_t i = tid; i < m.E * kWords; i += kMoeThreads) r.mask[0][i] = 0u;
+    if (tid < kWords) r.bad[tid] = 0u;
     __syncthreads();
-    int expert[kMine]; float weight[kMine];
+    if (m.E > 128u) route_tokens<HBF_MOE_MAX_EXPERTS / 32, 1>(m, r, tmp, write);
+    else if (kTokens > kMoeWarps && m.T > kMoeWarps) route_tokens<4, kTokens / kMoeWarps < 4 ? 1 : 4>(m, r, tmp, write);
+    else route_tokens<4, 1>(m, r, tmp, write);
+    __syncthreads();
+    // places of the experts in the list of pairs, of those in use, and of the entries: one scan over the experts
+    uint32_t count[kEach], a0 = 0u, b0 = 0u, c0 = 0u;
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-        const uint32_t t = i * kMoeWarps + warp;
-        expert[i] = -1; weight[i] = 0.0f;
-        if (t < m.T) {
-            const bool ok = choose(m, t, expert[i], weight[i]);
-            if (!ok && lane == 0) atomicOr(&r.bad[t >> 5], 1u << (t & 31u));
-            if (expert[i] >= 0) atomicOr(&r.mask[expert[i]][t >> 5], 1u << (t & 31u));
-            if (write && lane < m.K) {
-                if (m.chosen) m.chosen[(size_t)t * m.K + lane] = expert[i];
-                if (m.weights) m.weights[(size_t)t * m.K + lane] = weight[i];
-            }
+    for (int i = 0; i < kEach; ++i) {
+        const uint32_t e = tid * kEach + i;
+        count[i] = 0u;
+        if (e < m.E) {
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) count[i] += __popc(r.mask[e][w]);
         }
+        a0 += count[i]; b0 += count[i] ? 1u : 0u; c0 += (count[i] + chunk - 1u) / chunk;
     }
-    __syncthreads();
-    // places of the experts in the list of pairs, of those in use, and of the items' entries: one scan over the experts
-    uint32_t count = 0u, chunks = 0u;
-    if (tid < m.E) {
-#pragma unroll
-        for (int w = 0; w < HBF_MOE_MAX_TOKENS / 32; ++w) count += __popc(r.mask[tid][w]);
-        chunks = (count + kMoeChunk - 1) / kMoeChunk;
-    }
-    const uint32_t used = count ? 1u : 0u;
-    uint32_t a = count, b = used, c = chunks;
+    uint32_t a = a0, b = b0, c = c0;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const uint32_t pa = __shfl_up_sync(0xffffffffu, a, o), pb = __shfl_up_sync(0xffffffffu, b, o), pc = __shfl_up_sync(0xffffffffu, c, o);
@@ -141,39 +183,43 @@ __device__ void route(const MoeDev &m, Route &r, bool write) {
     }
     if (lane == 31u) { r.scan[warp][0] = a; r.scan[warp][1] = b; r.scan[warp][2] = c; }
     __syncthreads();
+#pragma unroll 1
     for (uint32_t w = 0; w < warp; ++w) { a += r.scan[w][0]; b += r.scan[w][1]; c += r.scan[w][2]; }
     if (tid == kMoeThreads - 1) { r.n_active = b; r.n_entries = c; }
-    if (tid < m.E) {
-        r.base[tid] = (uint16_t)(a - count);
-        if (used) {
-            r.active[b - 1u] = (uint16_t)tid;
-            for (uint32_t k = 0; k < chunks; ++k) r.entry[c - chunks + k] = (uint16_t)(tid * 8u + k);
+    a -= a0; b -= b0; c -= c0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const uint32_t e = tid * kEach + i;
+        if (e >= m.E) break;
+        r.base[e] = (uint16_t)a;
+        if (count[i]) r.active[b++] = (uint16_t)e;
+#pragma unroll 1
+        for (uint32_t k = 0; k < count[i]; k += chunk, ++c) {
+            r.expert[c] = (uint16_t)e; r.pair0[c] = (uint16_t)(a + k); r.count[c] = (uint8_t)min(chunk, count[i] - k);
         }
+        a += count[i];
     }
     __syncthreads();
+#pragma unroll 1
+    for (uint32_t i = tid; i < m.T * m.K; i += kMoeThreads) {
+        const uint32_t e = tmp.expert[i], t = div32(i, m.div_k);
+        if (e == 0xffffu) continue;
+        uint32_t at = r.base[e];
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-        const uint32_t t = i * kMoeWarps + warp;
-        if (expert[i] >= 0) {
-            uint32_t at = r.base[expert[i]];
-#pragma unroll
-            for (int w = 0; w < HBF_MOE_MAX_TOKENS / 32; ++w) {
-                const uint32_t below = (uint32_t)w < (t >> 5) ? 0xffffffffu : (uint32_t)w == (t >> 5) ? (1u << (t & 31u)) - 1u : 0u;
-                at += __popc(r.mask[expert[i]][w] & below);
-            }
-            r.token[at] = (uint8_t)t; r.weight[at] = weight[i];
-        }
+        for (int w = 0; w < kWords; ++w)
+            at += __popc(r.mask[e][w] & ((uint32_t)w < (t >> 5) ? 0xffffffffu : (uint32_t)w == (t >> 5) ? (1u << (t & 31u)) - 1u : 0u));
+        r.token[at] = (uint8_t)t; r.weight[at] = tmp.weight[i];
     }
     __syncthreads();
 }
-static_assert(HBF_MOE_MAX_EXPERTS <= kMoeThreads, "an expert a thread in the scan");
-static_assert(HBF_MOE_MAX_TOKENS / kMoeChunk <= 8 && HBF_MOE_MAX_EXPERTS * 8 <= 65536 && HBF_MOE_MAX_TOKENS <= 256, "packed fields");
+static_assert(HBF_MOE_MAX_EXPERTS % kMoeThreads == 0 && HBF_MOE_MAX_TOKENS == 128, "the scan and the masks");
 
 // Sixteen warps' sums of a 16 x 8 n product, left as they lie in the accumulators: eight lanes for a column of the pile, two warps' parts
 // each, always in the same order.  f(tile, lane of the accumulator, its four sums) is called once for every column.
 template <class F>
 __device__ __forceinline__ void sum_over_warps(const float4 *pile, int tiles, F f) {
     const uint32_t lane = lane_id(), warp = threadIdx.x >> 5, part = lane >> 2;
+#pragma unroll 1
     for (uint32_t c0 = warp * 4u; c0 < (uint32_t)tiles * 32u; c0 += kMoeWarps * 4u) {
         const uint32_t col = c0 + (lane & 3u);
         float4 s = pile[(size_t)(part * 2u) * tiles * 32u + col];
@@ -188,95 +234,96 @@ __device__ __forceinline__ void sum_over_warps(const float4 *pile, int tiles, F 
     }
 }
 
+__device__ __forceinline__ uint4 ld_input(const uint16_t *p) { return __ldg(reinterpret_cast<const uint4 *>(p)); }
+__device__ __forceinline__ uint4 ld_after16(const uint16_t *p) {                            // (see ld_after)
+    uint4 v; asm volatile("ld.global.cg.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p)); return v;
+}
+
+// Shared memory of the up kernel: the choice, the pile of sums (twice where there is room), the rings.  kTiles: tiles of eight tokens that an
+// entry has at most.
+template <int kTiles> constexpr uint32_t kPiles = kTiles == 4 ? 1u : 2u;
+template <int kTiles, int kTokens> constexpr uint32_t kUpRingAt = kRouteBytes<kTokens> + kPiles<kTiles> * kMoeWarps * kTiles * 512u;
+template <int kTiles, int kTokens, int kRing> constexpr uint32_t up_smem() { return kUpRingAt<kTiles, kTokens> + kMoeWarps * kRing * 1024u; }
+
 // Items of eight gate rows and the same eight up rows (rows 0..7 and 8..15 of one product, so a thread's sums hold both), one item a
-// block at a time, the sum over `hidden` split among its warps; the ring runs on into the next item while an item's sums are joined.
-template <class Ty>
-__global__ void __launch_bounds__(kMoeThreads, 1)
+// block at a time, the sum over `hidden` split among its warps in steps of 32; the ring runs on into the next item while an item's sums
+// are joined.  Activations, which L1 or L2 holds, are asked for a step ahead.
+template <class Ty, int kTiles, int kTokens, int kRing, int kBlocks>
+__global__ void __launch_bounds__(kMoeThreads, kBlocks)
 k_moe_up(const __grid_constant__ MoeDev m) {
     extern __shared__ __align__(128) unsigned char smem[];
-    Route &r = *reinterpret_cast<Route *>(smem);
-    constexpr uint32_t kPileAt = (sizeof(Route) + 127u) / 128u * 128u, kRingAt = kPileAt + 2u * kMoeWarps * (kMoeChunk / 8) * 512u;
+    Route<kTokens> &r = *reinterpret_cast<Route<kTokens> *>(smem);
     const uint32_t lane = lane_id(), warp = threadIdx.x >> 5, row = lane >> 2, quad = lane & 3u;
     pdl_trigger();
-    route(m, r, blockIdx.x == 0);
-    const uint32_t slices = (m.I + 7u) / 8u, n_items = r.n_entries * slices;
+    route(m, r, *reinterpret_cast<RouteTemp<kTokens> *>(smem + kRouteBytes<kTokens>), kTiles * 8u, blockIdx.x == 0);
+    const uint32_t slices = m.I / 8u, n_items = r.n_entries * slices;
     const uint32_t steps = ((m.D + 31u) / 32u + kMoeWarps - 1u) / kMoeWarps;               // of a warp, an item
-    const uint32_t ring = smem_addr(smem) + kRingAt + warp * (kUpRing * kUpStep) + lane * 16u;
+    const uint32_t ring = smem_addr(smem) + kUpRingAt<kTiles, kTokens> + warp * (kRing * 1024u) + lane * 16u, k0 = warp * 32u + quad * 8u;
+    constexpr uint32_t kStride = kMoeWarps * 32u;
 
-    uint32_t in_item = blockIdx.x, in_step = 0u, in_slot = 0u;
-    const uint16_t *gate = nullptr, *up = nullptr, *xrow = nullptr;
-    bool has_row = false, has_x = false;
-    auto enter = [&]() {                                     // where this lane's rows of the item begin
+    uint32_t in_item = blockIdx.x, in_k = k0, in_left = steps, in_slot = 0u;
+    const uint16_t *gate = m.experts;
+    auto place = [&]() {                                     // where this lane's rows of the item begin
         if (in_item >= n_items) return;
-        const uint32_t en = div32(in_item, m.div_slices), sl = in_item - en * slices;
-        const uint32_t e = r.entry[en] >> 3, chunk = r.entry[en] & 7u, i = sl * 8u + row;
-        const uint16_t *w = m.experts + (int64_t)e * m.expert_stride;
-        has_row = i < m.I;
-        gate = w + (size_t)i * m.D; up = gate + (size_t)m.I * m.D;
-        uint32_t n = 0u;
-#pragma unroll
-        for (int k = 0; k < HBF_MOE_MAX_TOKENS / 32; ++k) n += __popc(r.mask[e][k]);
-        has_x = chunk * kMoeChunk + row < n;
-        if (has_x) xrow = m.x + (int64_t)r.token[r.base[e] + chunk * kMoeChunk + row] * m.x_stride;
+        const uint32_t en = div32(in_item, m.div_slices), i = (in_item - en * slices) * 8u + row;
+        gate = m.experts + (int64_t)r.expert[en] * m.expert_stride + (size_t)i * m.D;
     };
     auto issue = [&]() {
         if (in_item < n_items) {
-            const uint32_t k = (in_step * kMoeWarps + warp) * 32u + quad * 8u;
-            const bool in = k < m.D, ok = in && has_row, okx = in && has_x;
-            const uint32_t at = ring + in_slot * kUpStep;
-            copy_async16(at, ok ? gate + k : m.experts, ok);
-            copy_async16(at + 512u, ok ? up + k : m.experts, ok);
-            copy_async16_shared(at + 1024u, okx ? xrow + k : m.x, okx);
-            in_slot = in_slot + 1u == kUpRing ? 0u : in_slot + 1u;
-            if (++in_step == steps) { in_step = 0u; in_item += gridDim.x; enter(); }
+            const bool in = in_k < m.D;
+            const uint16_t *g = in ? gate + in_k : m.experts;
+            copy_async16(ring + in_slot * 1024u, g, in);
+            copy_async16(ring + in_slot * 1024u + 512u, in ? g + (size_t)m.I * m.D : g, in);
+            in_slot = in_slot + 1u == kRing ? 0u : in_slot + 1u;
+            in_k += kStride;
+            if (--in_left == 0u) { in_left = steps; in_k = k0; in_item += gridDim.x; place(); }
         }
         copy_commit();
     };
-    enter();
-#pragma unroll
-    for (int i = 0; i < kUpRing; ++i) issue();
+    place();
+#pragma unroll 1
+    for (int i = 0; i < kRing; ++i) issue();
 
     uint32_t slot = 0u, turn = 0u;
     for (uint32_t item = blockIdx.x; item < n_items; item += gridDim.x, turn ^= 1u) {
-        const uint32_t en = div32(item, m.div_slices), sl = item - en * slices;
-        const uint32_t e = r.entry[en] >> 3, pair0 = r.base[e] + (r.entry[en] & 7u) * kMoeChunk;
-        uint32_t n = 0u;
-#pragma unroll
-        for (int k = 0; k < HBF_MOE_MAX_TOKENS / 32; ++k) n += __popc(r.mask[e][k]);
-        n = min(n - (r.entry[en] & 7u) * kMoeChunk, (uint32_t)kMoeChunk);
+        const uint32_t en = div32(item, m.div_slices), sl = item - en * slices, n = r.count[en], pair0 = r.pair0[en];
         const int tiles = (int)((n + 7u) / 8u);
-        const uint16_t *more[kMoeChunk / 8 - 1];             // activations of the tokens past the first eight come straight from L1 or L2
+        const uint16_t *x[kTiles];
+        uint4 now[kTiles];
+        const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+        float acc[kTiles][4];
 #pragma unroll
-        for (int j = 1; j < kMoeChunk / 8; ++j) more[j - 1] = j * 8u + row < n ? m.x + (int64_t)r.token[pair0 + j * 8u + row] * m.x_stride : nullptr;
-        float acc[kMoeChunk / 8][4];
+        for (int j = 0; j < kTiles; ++j) {
+            x[j] = j * 8u + row < n ? m.x + (int64_t)r.token[pair0 + j * 8u + row] * m.x_stride : nullptr;
+            now[j] = x[j] && k0 < m.D ? ld_input(x[j] + k0) : zero;
+            acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
+        }
+#pragma unroll 1
+        for (uint32_t s = 0, k = k0 + kStride; s < steps; ++s, k += kStride) {
+            uint4 next[kTiles];
 #pragma unroll
-        for (int j = 0; j < kMoeChunk / 8; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
-        for (uint32_t s = 0; s < steps; ++s) {
-            copy_wait<kUpRing - 1>();
-            const uint32_t at = ring + slot * kUpStep;
-            const uint4 g = ld_shared16(at), u = ld_shared16(at + 512u), x = ld_shared16(at + 1024u);
-            slot = slot + 1u == kUpRing ? 0u : slot + 1u;
-            Ty::mma(acc[0], g.x, u.x, g.y, u.y, x.x, x.y);
-            Ty::mma(acc[0], g.z, u.z, g.w, u.w, x.z, x.w);
-            const uint32_t k = (s * kMoeWarps + warp) * 32u + quad * 8u;
+            for (int j = 0; j < kTiles; ++j) next[j] = x[j] && k < m.D && s + 1u < steps ? ld_input(x[j] + k) : zero;
+            copy_wait<kRing - 1>();
+            const uint4 g = ld_shared16(ring + slot * 1024u), u = ld_shared16(ring + slot * 1024u + 512u);
+            slot = slot + 1u == kRing ? 0u : slot + 1u;
 #pragma unroll
-            for (int j = 1; j < kMoeChunk / 8; ++j)
+            for (int j = 0; j < kTiles; ++j)
                 if (j < tiles) {
-                    const uint4 v = more[j - 1] && k < m.D ? __ldg(reinterpret_cast<const uint4 *>(more[j - 1] + k)) : make_uint4(0u, 0u, 0u, 0u);
-                    Ty::mma(acc[j], g.x, u.x, g.y, u.y, v.x, v.y);
-                    Ty::mma(acc[j], g.z, u.z, g.w, u.w, v.z, v.w);
+                    Ty::mma(acc[j], g.x, u.x, g.y, u.y, now[j].x, now[j].y);
+                    Ty::mma(acc[j], g.z, u.z, g.w, u.w, now[j].z, now[j].w);
                 }
             issue();
+#pragma unroll
+            for (int j = 0; j < kTiles; ++j) now[j] = next[j];
         }
         // two piles in turn: a warp that is ahead writes the other one, and passes the next barrier only with all
-        float4 *pile = reinterpret_cast<float4 *>(smem + kPileAt) + (size_t)turn * kMoeWarps * (kMoeChunk / 8) * 32u;
+        float4 *pile = reinterpret_cast<float4 *>(smem + kRouteBytes<kTokens>) + (kPiles<kTiles> == 2u ? (size_t)turn * kMoeWarps * kTiles * 32u : 0u);
 #pragma unroll
-        for (int j = 0; j < kMoeChunk / 8; ++j)
+        for (int j = 0; j < kTiles; ++j)
             if (j < tiles) pile[((size_t)warp * tiles + j) * 32u + lane] = make_float4(acc[j][0], acc[j][1], acc[j][2], acc[j][3]);
         __syncthreads();
         sum_over_warps(pile, tiles, [&](uint32_t tile, uint32_t l, const float4 &v) {
             const uint32_t i = sl * 8u + (l >> 2);
-            if (i >= m.I) return;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const uint32_t rank = tile * 8u + (l & 3u) * 2u + k;
@@ -291,97 +338,153 @@ k_moe_up(const __grid_constant__ MoeDev m) {
                 reinterpret_cast<typename Ty::type *>(m.h_lo)[at] = isfinite(Ty::to(hi)) ? lo : Ty::from(0.0f);
             }
         });
+        if (kPiles<kTiles> == 1u) __syncthreads();
     }
     copy_wait<0>();
 }
 
-__device__ __forceinline__ uint4 ld_l2(const uint16_t *p) {
-    uint4 v; asm volatile("ld.global.cg.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p)); return v;
+// Shared memory of the down kernel: the choice, every warp's sums of 16 rows for all tokens, the rings.
+__host__ __device__ constexpr uint32_t down_sums(uint32_t tokens) { return kMoeWarps * tokens * 64u; }
+template <int kTokens, int kRing, int kWide> constexpr uint32_t down_smem(uint32_t tokens) {
+    const uint32_t more = down_sums(tokens) + kMoeWarps * kRing * kWide * 1024u, tmp = (sizeof(RouteTemp<kTokens>) + 127u) / 128u * 128u;
+    return kRouteBytes<kTokens> + (more > tmp ? more : tmp);
 }
 
-// A block keeps up to 16 rows of the output for all tokens (columns of the products) and walks the experts in use; the steps of all
-// experts, 32 wide, go to its warps in turn.  A column's sums grow only by the experts its token chose: what another token's expert holds,
-// an infinity among it, cannot reach it through a zero.  The first weights are on their way while the kernel before still runs.
-template <class Ty, int kTiles>
-__global__ void __launch_bounds__(kMoeThreads, 1)
+// A block keeps up to 16 rows of the output for all tokens and walks the steps of the entries in use, 32 kWide each, a stretch of
+// them a warp.  An entry's products have its tokens as columns; a warp adds them to its sums in shared memory when it comes to the next entry:
+// a token's sums grow only by what its own experts hold, and in the order of the experts.  The ring's first weights are on their way while the
+// kernel before still runs; activations, which L2 holds, are asked for a step ahead.
+template <class Ty, int kTiles, int kTokens, int kRing, int kWide, int kBlocks>
+__global__ void __launch_bounds__(kMoeThreads, kBlocks)
 k_moe_down(const __grid_constant__ MoeDev m) {
     extern __shared__ __align__(128) unsigned char smem[];
-    Route &r = *reinterpret_cast<Route *>(smem);
-    constexpr uint32_t kRingAt = (sizeof(Route) + 127u) / 128u * 128u;
-    const uint32_t lane = lane_id(), warp = threadIdx.x >> 5, row = lane >> 2, quad = lane & 3u;
-    route(m, r, false);
-    const uint32_t steps = (m.I + 31u) / 32u, n_steps = r.n_active * steps;
-    const uint32_t ring = smem_addr(smem) + kRingAt + warp * (kDownRing * kDownStep) + lane * 16u;
+    Route<kTokens> &r = *reinterpret_cast<Route<kTokens> *>(smem);
+    const uint32_t tid = threadIdx.x, lane = lane_id(), warp = tid >> 5, row = lane >> 2, quad = lane & 3u;
+    route(m, r, *reinterpret_cast<RouteTemp<kTokens> *>(smem + kRouteBytes<kTokens>), kTiles * 8u, false);
+    float *sums = reinterpret_cast<float *>(smem + kRouteBytes<kTokens>);                   // [warp][token][16]
+    float *mine = sums + (size_t)warp * m.T * 16u;
+    constexpr uint32_t kStep = kWide * 32u, kSlot = kWide * 1024u;
+    const uint32_t steps = (m.I + kStep - 1u) / kStep, n_steps = r.n_entries * steps;
+    const uint32_t first = (uint32_t)((uint64_t)n_steps * warp / kMoeWarps), last = (uint32_t)((uint64_t)n_steps * (warp + 1u) / kMoeWarps);
+    const uint32_t en0 = first / steps, s0 = first - en0 * steps;
+    const uint32_t ring = smem_addr(smem) + kRouteBytes<kTokens> + down_sums(m.T) + warp * (kRing * kSlot) + lane * 16u;
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
     bool waited = false;
     for (uint32_t d0 = blockIdx.x * m.rows; d0 < m.D; d0 += gridDim.x * m.rows) {
         const uint32_t rows = min(m.rows, m.D - d0);
-        uint32_t in = warp, in_slot = 0u;
+        const bool row0 = row < rows, row1 = row + 8u < rows;
+        const uint16_t *down = m.experts + (size_t)2 * m.I * m.D + (size_t)(d0 + row) * m.I;
+        uint32_t in_left = last - first, in_en = en0, in_s = s0, in_slot = 0u;
+        const uint16_t *w = down;
+        auto place = [&]() { if (in_left) w = down + (int64_t)r.expert[in_en] * m.expert_stride; };
         auto issue = [&]() {
-            if (in < n_steps) {
-                const uint32_t a = div32(in, m.div_steps), k = (in - a * steps) * 32u + quad * 8u;
-                const uint16_t *w = m.experts + (int64_t)r.active[a] * m.expert_stride + (size_t)2 * m.I * m.D + (size_t)(d0 + row) * m.I + k;
-                const bool ok0 = k < m.I && row < rows, ok1 = k < m.I && row + 8u < rows;
-                const uint32_t at = ring + in_slot * kDownStep;
-                copy_async16(at, ok0 ? w : m.experts, ok0);
-                copy_async16(at + 512u, ok1 ? w + (size_t)8 * m.I : m.experts, ok1);
-                in_slot = in_slot + 1u == kDownRing ? 0u : in_slot + 1u;
-                in += kMoeWarps;
+            if (in_left) {
+#pragma unroll
+                for (int b = 0; b < kWide; ++b) {
+                    const uint32_t k = in_s * kStep + b * 32u + quad * 8u, at = ring + in_slot * kSlot + b * 1024u;
+                    const bool in = k < m.I;
+                    copy_async16(at, in && row0 ? w + k : m.experts, in && row0);
+                    copy_async16(at + 512u, in && row1 ? w + (size_t)8 * m.I + k : m.experts, in && row1);
+                }
+                in_slot = in_slot + 1u == kRing ? 0u : in_slot + 1u;
+                --in_left;
+                if (++in_s == steps) { in_s = 0u; ++in_en; place(); }
             }
             copy_commit();
         };
-#pragma unroll
-        for (int i = 0; i < kDownRing; ++i) issue();
+        place();
+#pragma unroll 1
+        for (int i = 0; i < kRing; ++i) issue();
+        for (uint32_t i = lane; i < m.T * 16u; i += 32u) mine[i] = 0.0f;
+        __syncwarp();
         if (!waited) { pdl_wait(); waited = true; }
-        float acc[kTiles][4];
-#pragma unroll
-        for (int j = 0; j < kTiles; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
-        uint32_t slot = 0u;
-        for (uint32_t st = warp; st < n_steps; st += kMoeWarps) {
-            const uint32_t a = div32(st, m.div_steps), k = (st - a * steps) * 32u + quad * 8u, e = r.active[a];
-            copy_wait<kDownRing - 1>();
-            const uint32_t at = ring + slot * kDownStep;
-            const uint4 w0 = ld_shared16(at), w1 = ld_shared16(at + 512u);
-            slot = slot + 1u == kDownRing ? 0u : slot + 1u;
-            uint32_t below = r.base[e];
+        uint32_t en = en0, s = s0, slot = 0u, n = 0u, pair0 = 0u;
+        uint4 now[kTiles][kWide][2];
+        const uint16_t *h = m.h_hi;                          // this lane's row of the entry's first tile
+        const size_t h_lo = (size_t)(m.h_lo - m.h_hi);
+        auto enter = [&]() { n = r.count[en]; pair0 = r.pair0[en]; h = m.h_hi + (size_t)(pair0 + row) * m.I; };
+        auto load = [&](uint4 (&v)[kTiles][kWide][2], uint32_t step) {
 #pragma unroll
             for (int j = 0; j < kTiles; ++j) {
-                const uint32_t mine = (r.mask[e][j >> 2] >> ((j & 3) * 8)) & 0xffu;
-                if (mine == 0u) continue;
-                const bool there = ((mine >> row) & 1u) != 0u && k < m.I;
-                const size_t h = (size_t)(below + __popc(mine & ((1u << row) - 1u))) * m.I + k;
-                const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-                const uint4 hi = there ? ld_l2(m.h_hi + h) : zero, lo = there ? ld_l2(m.h_lo + h) : zero;
-                below += __popc(mine);
-                float p[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                Ty::mma(p, w0.x, w1.x, w0.y, w1.y, hi.x, hi.y);
-                Ty::mma(p, w0.z, w1.z, w0.w, w1.w, hi.z, hi.w);
-                Ty::mma(p, w0.x, w1.x, w0.y, w1.y, lo.x, lo.y);
-                Ty::mma(p, w0.z, w1.z, w0.w, w1.w, lo.z, lo.w);
-                const bool c0 = (mine >> (quad * 2u)) & 1u, c1 = (mine >> (quad * 2u + 1u)) & 1u;
-                if (c0) { acc[j][0] += p[0]; acc[j][2] += p[2]; }
-                if (c1) { acc[j][1] += p[1]; acc[j][3] += p[3]; }
-            }
-            issue();
-        }
-        copy_wait<0>();
-        __syncthreads();                                     // the rings are empty: their memory is the pile's
-        float4 *pile = reinterpret_cast<float4 *>(smem + kRingAt);
+                if (j && j * 8u >= n) break;
+                const bool there = j * 8u + row < n;
 #pragma unroll
-        for (int j = 0; j < kTiles; ++j) pile[((size_t)warp * kTiles + j) * 32u + lane] = make_float4(acc[j][0], acc[j][1], acc[j][2], acc[j][3]);
-        __syncthreads();
-        sum_over_warps(pile, kTiles, [&](uint32_t tile, uint32_t l, const float4 &v) {
-            const float sums[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const uint32_t t = tile * 8u + (l & 3u) * 2u + (c & 1), d = (l >> 2) + (c >> 1) * 8u;
-                if (t < m.T && d < rows) {
-                    const float v1 = (r.bad[t >> 5] >> (t & 31u)) & 1u ? __int_as_float(0x7fc00000) : sums[c];
-                    reinterpret_cast<typename Ty::type *>(m.out)[(int64_t)t * m.out_stride + d0 + d] = Ty::from(v1);
+                for (int b = 0; b < kWide; ++b) {
+                    const uint32_t k = step * kStep + b * 32u + quad * 8u;
+                    const bool in = there && k < m.I;
+                    const uint16_t *at = h + j * 8u * m.I + k;
+                    v[j][b][0] = in ? ld_after16(at) : zero;
+                    v[j][b][1] = in ? ld_after16(at + h_lo) : zero;
                 }
             }
-        });
+        };
+        if (first < last) { enter(); load(now, s); }
+        float acc[kTiles][2][4];                             // two chains of products each
+        auto clear = [&]() {
+#pragma unroll
+            for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) acc[j][0][c] = acc[j][1][c] = 0.0f;
+        };
+        clear();
+        uint32_t left = last - first;
+        auto turn = [&](uint4 (&cur)[kTiles][kWide][2], uint4 (&next)[kTiles][kWide][2]) {
+            const uint32_t n_now = n, pair_now = pair0;
+            const bool done = ++s == steps || left == 1u;    // the entry is done, or this warp's part of it
+            if (s == steps) { s = 0u; ++en; if (left > 1u) enter(); }
+            if (left > 1u) load(next, s);
+            copy_wait<kRing - 1>();
+#pragma unroll
+            for (int b = 0; b < kWide; ++b) {
+                const uint4 w0 = ld_shared16(ring + slot * kSlot + b * 1024u), w1 = ld_shared16(ring + slot * kSlot + b * 1024u + 512u);
+#pragma unroll
+                for (int j = 0; j < kTiles; ++j)
+                    if (j == 0 || j * 8u < n_now) {
+                        const uint4 hi = cur[j][b][0], lo = cur[j][b][1];
+                        Ty::mma(acc[j][0], w0.x, w1.x, w0.y, w1.y, hi.x, hi.y);
+                        Ty::mma(acc[j][1], w0.x, w1.x, w0.y, w1.y, lo.x, lo.y);
+                        Ty::mma(acc[j][0], w0.z, w1.z, w0.w, w1.w, hi.z, hi.w);
+                        Ty::mma(acc[j][1], w0.z, w1.z, w0.w, w1.w, lo.z, lo.w);
+                    }
+            }
+            slot = slot + 1u == kRing ? 0u : slot + 1u;
+            issue();
+            if (done) {
+#pragma unroll
+                for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const uint32_t rank = j * 8u + quad * 2u + c;
+                        if (rank < n_now) {
+                            float *to = mine + r.token[pair_now + rank] * 16u + row;
+                            to[0] += acc[j][0][c] + acc[j][1][c];
+                            to[8] += acc[j][0][c + 2] + acc[j][1][c + 2];
+                        }
+                    }
+                clear();
+                __syncwarp();
+            }
+            --left;
+        };
+        uint4 then[kTiles][kWide][2];
+#pragma unroll 1
+        while (left) {
+            turn(now, then);
+            if (left) turn(then, now);
+        }
+        __syncthreads();
+        for (uint32_t i = tid; i < m.T * 16u; i += kMoeThreads) {
+            const uint32_t t = i >> 4, d = i & 15u;
+            if (d >= rows) continue;
+            float v = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kMoeWarps; ++k) v += sums[(size_t)k * m.T * 16u + i];
+            if ((r.bad[t >> 5] >> (t & 31u)) & 1u) v = __int_as_float(0x7fc00000);
+            reinterpret_cast<typename Ty::type *>(m.out)[(int64_t)t * m.out_stride + d0 + d] = Ty::from(v);
+        }
         __syncthreads();
     }
+    copy_wait<0>();
     if (!waited) pdl_wait();
 }
 
@@ -391,8 +494,9 @@ __global__ void __launch_bounds__(kMoeThreads)
 k_moe_accesses(const __grid_constant__ MoeDev m, uint64_t expert_bytes, uint32_t tile_bytes, uint32_t tiles, int64_t issue_ns, int64_t gap_ns,
                hbf_access_t *acc, uint64_t n) {
     extern __shared__ __align__(128) unsigned char smem[];
-    Route &r = *reinterpret_cast<Route *>(smem);
-    route(m, r, false);
+    constexpr int kTokens = HBF_MOE_MAX_TOKENS;
+    Route<kTokens> &r = *reinterpret_cast<Route<kTokens> *>(smem);
+    route(m, r, *reinterpret_cast<RouteTemp<kTokens> *>(smem + kRouteBytes<kTokens>), 8u, false);
     for (uint64_t i = (uint64_t)blockIdx.x * kMoeThreads + threadIdx.x; i < n; i += (uint64_t)gridDim.x * kMoeThreads) {
         const uint32_t a = (uint32_t)(i / tiles), t = (uint32_t)(i - (uint64_t)a * tiles);
         hbf_access_t v = {0, issue_ns + (int64_t)i * gap_ns, 1, 0};
@@ -423,33 +527,40 @@ static MoeDev moe_dev(const hbf_moe_t *m) {
     d.scores = m->scores; d.scores_stride = m->scores_stride;
     d.experts = static_cast<const uint16_t *>(m->experts); d.expert_stride = m->expert_stride;
     d.out = static_cast<uint16_t *>(m->out); d.out_stride = m->out_stride;
-    d.chosen = m->chosen; d.weights = m->weights;
+    d.chosen = m->chosen; d.weights = m->weights; d.div_k = make_div32(d.K);
     return d;
 }
 
+// Up to 8 tokens a layer is a few tens of microseconds, and what counts is that nothing waits: both kernels fit an SM together, so
+// that the second has made its choice and has its first weights on their way when the first one ends.  Beyond, each has the SM to itself,
+// with longer rings; two tiles an entry where an expert has 16 tokens or fewer on average, else four.
+template <class Ty, int kTiles, int kTokens, int kUpRing, int kDownRing, int kWide, int kBlocks>
+static cudaError_t launch_moe_as(const MoeDev &d, uint32_t n_sm, cudaStream_t st) {
+    constexpr uint32_t up = up_smem<kTiles, kTokens, kUpRing>(), most_down = down_smem<kTokens, kDownRing, kWide>(kTokens);
+    static_assert(up <= 227 * 1024 && most_down <= 227 * 1024 && kRouteBytes<kTokens> + sizeof(RouteTemp<kTokens>) <= up, "shared memory");
+    static_assert(kBlocks == 1 || up + most_down <= 226 * 1024, "both kernels on an SM");
+    const auto up_k = k_moe_up<Ty, kTiles, kTokens, kUpRing, kBlocks>;
+    const auto down_k = k_moe_down<Ty, kTiles, kTokens, kDownRing, kWide, kBlocks>;
+    cudaError_t e = ensure_dyn_smem((const void *)up_k, up);
+    if (e == cudaSuccess) e = ensure_dyn_smem((const void *)down_k, most_down);
+    if (e != cudaSuccess) return e;
+    const uint64_t pairs = (uint64_t)d.T * d.K, most = (pairs < d.E + pairs / (kTiles * 8) ? pairs : d.E + pairs / (kTiles * 8)) * (d.I / 8u);
+    up_k<<<(unsigned)(most < n_sm ? most : n_sm), kMoeThreads, up, st>>>(d);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    const uint32_t blocks = (d.D + d.rows - 1u) / d.rows;
+    g_kernel_launches += 2;
+    return launch_pdl(down_k, blocks < n_sm ? blocks : n_sm, kMoeThreads, down_smem<kTokens, kDownRing, kWide>(d.T), st, d);
+}
 template <class Ty>
 static cudaError_t launch_moe(MoeDev d, uint32_t n_sm, cudaStream_t st) {
-    constexpr size_t kRoute = (sizeof(Route) + 127u) / 128u * 128u;
-    constexpr size_t up_smem = kRoute + 2u * kMoeWarps * (kMoeChunk / 8) * 512u + (size_t)kMoeWarps * kUpRing * kUpStep;
-    static_assert(up_smem <= 227 * 1024, "shared memory of the up kernel");
-    const uint32_t slices = (d.I + 7u) / 8u;
-    d.div_slices = make_div32(slices); d.div_steps = make_div32((d.I + 31u) / 32u);
+    d.div_slices = make_div32(d.I / 8u);
     // an even share of the output's rows to every SM, 16 at most: 2,048 rows are 14 a block on 147 blocks
     const uint32_t rounds = (d.D + 16u * n_sm - 1u) / (16u * n_sm);
     d.rows = (d.D + rounds * n_sm - 1u) / (rounds * n_sm);
-    const uint32_t down_blocks = min(n_sm, (d.D + d.rows - 1u) / d.rows);
-    const uint64_t most = (uint64_t)min(d.E + d.T * d.K / kMoeChunk, d.T * d.K) * slices;
-    cudaError_t e = ensure_dyn_smem((const void *)k_moe_up<Ty>, up_smem);
-    if (e != cudaSuccess) return e;
-    k_moe_up<Ty><<<(unsigned)(most < n_sm ? most : n_sm), kMoeThreads, up_smem, st>>>(d);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    const uint32_t tiles = d.T <= 8u ? 1u : d.T <= 16u ? 2u : d.T <= 32u ? 4u : d.T <= 64u ? 8u : 16u;
-    const size_t ring = (size_t)kMoeWarps * kDownRing * kDownStep, pile = (size_t)kMoeWarps * tiles * 512u;
-    const size_t down_smem = kRoute + (ring > pile ? ring : pile);
-    void (*down)(MoeDev) = tiles == 1u ? k_moe_down<Ty, 1> : tiles == 2u ? k_moe_down<Ty, 2> : tiles == 4u ? k_moe_down<Ty, 4> : tiles == 8u ? k_moe_down<Ty, 8> : k_moe_down<Ty, 16>;
-    if ((e = ensure_dyn_smem((const void *)down, down_smem)) != cudaSuccess) return e;
-    g_kernel_launches += 2;
-    return launch_pdl(down, down_blocks, kMoeThreads, down_smem, st, d);
+    if (d.T <= 8u) return launch_moe_as<Ty, 1, 8, 5, 4, 1, 2>(d, n_sm, st);
+    if (d.T <= 64u && d.T * d.K <= 16u * d.E) return launch_moe_as<Ty, 2, 64, 8, 4, 2, 1>(d, n_sm, st);
+    if (d.T * d.K <= 16u * d.E) return launch_moe_as<Ty, 2, HBF_MOE_MAX_TOKENS, 8, 2, 2, 1>(d, n_sm, st);
+    return launch_moe_as<Ty, 4, HBF_MOE_MAX_TOKENS, 8, 4, 1, 1>(d, n_sm, st);
 }
 
 }  // namespace hbf
@@ -493,8 +604,9 @@ extern "C" int hbf_moe_accesses(const hbf_moe_t *m, uint32_t tile_bytes, int64_t
     if (rc != HBF_OK) return rc;
     const uint64_t bytes = 6ull * m->hidden * m->inter;
     const uint64_t blocks = (n + kMoeThreads * 4 - 1) / (kMoeThreads * 4);
-    if (ensure_dyn_smem((const void *)k_moe_accesses, sizeof(Route)) != cudaSuccess) return HBF_E_CUDA;
-    k_moe_accesses<<<(unsigned)(blocks < n_sm ? blocks : n_sm), kMoeThreads, sizeof(Route), static_cast<cudaStream_t>(cuda_stream)>>>(
+    constexpr size_t smem = kRouteBytes<HBF_MOE_MAX_TOKENS> + sizeof(RouteTemp<HBF_MOE_MAX_TOKENS>);
+    if (ensure_dyn_smem((const void *)k_moe_accesses, smem) != cudaSuccess) return HBF_E_CUDA;
+    k_moe_accesses<<<(unsigned)(blocks < n_sm ? blocks : n_sm), kMoeThreads, smem, static_cast<cudaStream_t>(cuda_stream)>>>(
         moe_dev(m), bytes, tile_bytes, (uint32_t)((bytes + tile_bytes - 1) / tile_bytes), issue_ns, gap_ns, d_acc, n);
     g_kernel_launches += 1;
     return cudaGetLastError() == cudaSuccess ? HBF_OK : HBF_E_CUDA;
