@@ -318,20 +318,25 @@ static bool attention_pointers_ok(const hbf_attention_t *a) {
     return true;
 }
 
+// Rows (of all requests, for one key head) up to which the prefix goes through k_attend, which reads it again, from L2, for every 16 rows.
+constexpr uint32_t kPrefixRowsSmall = 32u;
+
 static uint32_t up_to(uint32_t v, uint32_t m) { return (v + m - 1u) / m * m; }
 
 // How the keys are cut.  A piece costs its start-up (about 2 us to the first values) and d * 4 bytes a row to join, so pieces are as long as
 // leaves about four blocks an SM: at least 64 keys, a multiple of 64, at most 512 of a request's own (whose lengths differ).
 static void attention_pieces(const hbf_attention_t *a, uint32_t n_sm, AttnDev &p) {
     const uint32_t G = p.G, blocks = 4u * n_sm;
-    p.prefix_rows = 16u;
+    p.prefix_rows = p.B * G > kPrefixRowsSmall ? 256u : 16u;
     p.row_tiles = (p.B * G + p.prefix_rows - 1u) / p.prefix_rows;
     p.group_tiles = (G + 15u) / 16u;
     p.prefix_pieces = 0u; p.prefix_chunk = 64u;
     if (a->prefix_len) {
-        const uint32_t pairs = p.row_tiles * p.Hk, most = (a->prefix_len + 63u) / 64u;
-        const uint32_t want = blocks > pairs ? blocks / pairs : 1u;
-        p.prefix_chunk = up_to((a->prefix_len + (want < most ? want : most) - 1u) / (want < most ? want : most), 64u);
+        // (k_prefix_tiles: a block an SM, tiles of 128 keys)
+        const uint32_t step = p.prefix_rows == 256u ? 128u : 64u, there = p.prefix_rows == 256u ? n_sm : blocks;
+        const uint32_t pairs = p.row_tiles * p.Hk, most = (a->prefix_len + step - 1u) / step;
+        const uint32_t want = there > pairs ? there / pairs : 1u;
+        p.prefix_chunk = up_to((a->prefix_len + (want < most ? want : most) - 1u) / (want < most ? want : most), step);
         p.prefix_pieces = (a->prefix_len + p.prefix_chunk - 1u) / p.prefix_chunk;
     }
     p.own_pieces = 0u; p.own_chunk = 64u;
@@ -366,16 +371,22 @@ static size_t attention_bytes(const AttnDev &p, uint32_t dim) {
 }
 
 template <class Ty, int D>
-static cudaError_t launch_attention(const AttnDev &p, cudaStream_t st) {
-    const uint64_t items = p.n_prefix_items + (uint64_t)p.B * p.Hk * p.group_tiles * p.own_pieces;
+static cudaError_t launch_attention(AttnDev p, bool bf16, cudaStream_t st) {
+    const bool tiles = p.prefix_rows == 256u && p.n_prefix_items;
+    AttnDev own = p;
+    if (tiles) own.n_prefix_items = 0u;
+    const uint64_t items = own.n_prefix_items + (uint64_t)p.B * p.Hk * p.group_tiles * p.own_pieces;
     cudaError_t e = cudaSuccess;
     if (items) {
         if ((e = ensure_dyn_smem((const void *)k_attend<Ty, D>, att_smem<D>())) != cudaSuccess) return e;
-        k_attend<Ty, D><<<(unsigned)items, kAttThreads, att_smem<D>(), st>>>(p);
+        k_attend<Ty, D><<<(unsigned)items, kAttThreads, att_smem<D>(), st>>>(own);
         g_kernel_launches += 1;
-        if ((e = cudaGetLastError()) != cudaSuccess || p.pieces == 1u) return e;
+        if ((e = cudaGetLastError()) != cudaSuccess) return e;
     }
+    if (tiles && (e = launch_prefix_tiles(p, D, bf16, items != 0u, st)) != cudaSuccess) return e;
+    if (p.pieces == 1u) return e;
     g_kernel_launches += 1;
+    if (p.pieces == 0u) { k_attend_join<Ty, D><<<p.B * p.Hq, kJoinWarps * 32, 0, st>>>(p); return cudaGetLastError(); }
     return launch_pdl(k_attend_join<Ty, D>, p.B * p.Hq, kJoinWarps * 32, 0, st, p);
 }
 
@@ -398,13 +409,14 @@ extern "C" int hbf_prefix_attention(const hbf_attention_t *a, void *d_workspace,
     const int rc = device_of(a->kv.k, &n_sm);
     if (rc != HBF_OK) return rc;
     AttnDev p = attention_dev(a, n_sm);
+    if ((uint64_t)p.B * p.Hk * p.group_tiles * p.own_pieces + p.n_prefix_items > 0x7fffffffull) return HBF_E_INVAL;
     if (!d_workspace || (uintptr_t)d_workspace % 256 || workspace_bytes < attention_bytes(p, a->kv.head_dim)) return HBF_E_WORKSPACE;
     p.part_o = static_cast<float *>(d_workspace);
     p.part_ml = reinterpret_cast<float2 *>(p.part_o + (size_t)p.pieces * p.B * p.Hq * a->kv.head_dim);
     const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     cudaError_t e;
-    if (a->kv.dtype == HBF_BF16) e = a->kv.head_dim == 128 ? launch_attention<Bf16, 128>(p, st) : launch_attention<Bf16, 64>(p, st);
-    else e = a->kv.head_dim == 128 ? launch_attention<Fp16, 128>(p, st) : launch_attention<Fp16, 64>(p, st);
+    if (a->kv.dtype == HBF_BF16) e = a->kv.head_dim == 128 ? launch_attention<Bf16, 128>(p, true, st) : launch_attention<Bf16, 64>(p, true, st);
+    else e = a->kv.head_dim == 128 ? launch_attention<Fp16, 128>(p, false, st) : launch_attention<Fp16, 64>(p, false, st);
     return e == cudaSuccess ? HBF_OK : HBF_E_CUDA;
 }
 

@@ -1,0 +1,314 @@
+// The shared prefix for many rows: tiles of 128 query rows (of any requests) against 128 keys at a time on the 5th-generation tensor
+// cores.  For a tile of rows and one of keys: S = Q K^T into tensor memory, weights P = exp2(S - z) from there back into it (over S, in
+// the values' type), O += P V with P read from tensor memory.  A block has two tiles of rows, so that one tile's products run while the
+// other's weights are worked out: 2 x 512 cycles of products for a tile of keys against 1,024 of exponentials, which all
+// eight warps of both tiles share.  The keys are read once for 256 rows; the products bound it from about 64 rows on.
+//
+// Warps 0 to 3 and 4 to 7: a row each thread, of the first and the second tile.  8 to 11: gather keys and values from their pages into the
+// swizzled layout that the tensor cores read.  12: one thread issues the products.
+#include "attention.cuh"
+
+namespace hbf {
+
+constexpr int kPfThreads = 13 * 32, kPfTile = 128, kPfSlots = 4;
+constexpr float kPfGrow = 8.0f;                              // sums are scaled again only when a row's maximum has grown by more (in powers of two)
+
+// What lies in shared memory behind the tiles.
+struct PfShared {
+    uint64_t kv_full[kPfSlots], kv_empty[kPfSlots], q_full, s_full[2], p_full[2], o_full[2];
+    int64_t place[2][kPfTile];                               // offset of each key of a tile; -1: none
+    uint32_t tmem, bad;
+};
+template <int D> constexpr uint32_t kPfTileBytes = kPfTile * D * 2;
+template <int D> constexpr uint32_t pf_smem() { return (2u + kPfSlots) * kPfTileBytes<D> + sizeof(PfShared) + 1024u; }
+
+// matrices in shared memory: rows of 64 values (128 bytes) in groups of eight, 16-byte columns permuted by the row's number, the next 64 values of
+// all rows behind.  Rows as the products' rows or columns (the sum along a row): `next8` is the way to the next eight rows; the sum along
+// the rows' numbers: also `next64` to the next 64 values.
+__device__ __forceinline__ uint64_t tile_desc(uint32_t addr, uint32_t next64, uint32_t next8) {
+    return (uint64_t)((addr >> 4) & 0x3fffu) | (uint64_t)((next64 >> 4) & 0x3fffu) << 16 | (uint64_t)((next8 >> 4) & 0x3fffu) << 32 | 1ull << 46 | 2ull << 61;
+}
+__device__ __forceinline__ uint32_t product_desc(bool bf16, bool b_by_rows, uint32_t m, uint32_t n) {
+    const uint32_t type = bf16 ? 1u : 0u;
+    return 1u << 4 | type << 7 | type << 10 | (b_by_rows ? 1u << 16 : 0u) | (n >> 3) << 17 | (m >> 4) << 24;
+}
+__device__ __forceinline__ void product_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+    asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+    asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+__device__ __forceinline__ void products_arrive(uint32_t bar) {              // when all products issued so far are done
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tensor_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tensor_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+#define HBF_R8(v, i) "=r"(v[i]), "=r"(v[i + 1]), "=r"(v[i + 2]), "=r"(v[i + 3]), "=r"(v[i + 4]), "=r"(v[i + 5]), "=r"(v[i + 6]), "=r"(v[i + 7])
+#define HBF_I8(v, i) "r"(v[i]), "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3]), "r"(v[i + 4]), "r"(v[i + 5]), "r"(v[i + 6]), "r"(v[i + 7])
+// 32 columns of this warp's 32 lanes of tensor memory, a lane a thread
+__device__ __forceinline__ void tensor_load(uint32_t addr, uint32_t (&v)[32]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : HBF_R8(v, 0), HBF_R8(v, 8), HBF_R8(v, 16), HBF_R8(v, 24) : "r"(addr));
+}
+__device__ __forceinline__ void tensor_loaded(uint32_t (&v)[32]) {           // (the values may be used behind this)
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(v[i]));
+}
+__device__ __forceinline__ void tensor_store16(uint32_t addr, const uint32_t (&v)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr), HBF_I8(v, 0), HBF_I8(v, 8) : "memory");
+}
+__device__ __forceinline__ void tensor_store32(uint32_t addr, const uint32_t (&v)[32]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+                 ::"r"(addr), HBF_I8(v, 0), HBF_I8(v, 8), HBF_I8(v, 16), HBF_I8(v, 24) : "memory");
+}
+__device__ __forceinline__ void tensor_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+template <class Ty, int D, bool kBf16>
+__global__ void __launch_bounds__(kPfThreads, 1)
+k_prefix_tiles(const __grid_constant__ AttnDev p) {
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
+    PfShared &sh = *reinterpret_cast<PfShared *>(smem_raw + (base - smem_addr(smem_raw)) + (2u + kPfSlots) * kPfTileBytes<D>);
+    constexpr uint32_t kBytes = kPfTileBytes<D>;
+    const uint32_t q_at = base, kv_at = base + 2u * kBytes;
+    const uint32_t tid = threadIdx.x, lane = lane_id(), warp = tid >> 5;
+    pdl_trigger();
+    // the piece: `row_tiles` counts pairs of tiles here
+    uint32_t item = blockIdx.x;
+    const uint32_t piece = item % p.prefix_pieces; item /= p.prefix_pieces;
+    const uint32_t pair = item % p.row_tiles, head = item / p.row_tiles;
+    const uint32_t begin = piece * p.prefix_chunk, end = min(p.prefix_len, begin + p.prefix_chunk);
+    const uint32_t n_tiles = (end - begin + kPfTile - 1u) / kPfTile, all_rows = p.B * p.G, row0 = pair * 2u * kPfTile;
+    const bool two = row0 + kPfTile < all_rows;
+    if (tid == 0) {
+        for (int i = 0; i < kPfSlots; ++i) { bar_init(smem_addr(&sh.kv_full[i]), 128u); bar_init(smem_addr(&sh.kv_empty[i]), 1u); }
+        bar_init(smem_addr(&sh.q_full), 128u);
+        for (int t = 0; t < 2; ++t) { bar_init(smem_addr(&sh.s_full[t]), 1u); bar_init(smem_addr(&sh.p_full[t]), 128u); bar_init(smem_addr(&sh.o_full[t]), 1u); }
+        sh.bad = 0u;
+        bar_init_done();
+    }
+    if (warp == 12u) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&sh.tmem)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        tensor_fence_before();
+    }
+    __syncthreads();
+    tensor_fence_after();
+    const uint32_t tmem = sh.tmem;                           // S (and P) of both tiles, then O of both
+    bool live = true;
+
+    if (warp >= 8u && warp < 12u) {
+        // ---- keys and values: eight lanes a row of 128 bytes
+        const uint32_t t = tid - 256u, col = t & 7u, row = t >> 3;
+        auto swizzled = [&](uint32_t r) { return r * 128u + ((col ^ (r & 7u)) * 16u); };
+        for (uint32_t h = 0; h < (two ? 2u : 1u); ++h)
+#pragma unroll 1
+            for (uint32_t r = row; r < kPfTile; r += 16u) {
+                const uint32_t n = row0 + h * kPfTile + r;
+                const bool ok = n < all_rows;
+                const uint32_t b = n / p.G, g = n - b * p.G;
+                const uint16_t *src = ok ? p.q + (int64_t)b * p.q_row + (int64_t)(head * p.G + g) * p.q_head + col * 8u : p.q;
+#pragma unroll
+                for (int x = 0; x < D / 64; ++x) copy_async16(q_at + h * kBytes + x * 16384u + swizzled(r), ok ? src + x * 64 : src, ok);
+            }
+        copy_commit();
+        auto find = [&](uint32_t i) {                        // thread t: key t of tile i
+            const uint32_t k = begin + i * kPfTile + t;
+            int64_t at = -1;
+            if (k < end) {
+                const uint32_t n = div32(k, p.div_page);
+                const int32_t page = p.prefix_pages[n];
+                if (!key_place(p, page, k - n * p.page_tokens, at)) { at = -1; sh.bad = 1u; }
+            }
+            sh.place[i & 1u][t] = at;
+        };
+        find(0);
+        barrier_of(1, 128);
+        uint32_t done = 0u;                                  // tiles (of keys or values) that were said to be there
+        auto arrive = [&](uint32_t bar) { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); bar_arrive(bar); };
+        for (uint32_t i = 0; i < n_tiles; ++i) {
+            if (i + 1u < n_tiles) find(i + 1u);
+            for (uint32_t kv = 0; kv < 2u; ++kv) {
+                const uint32_t n = 2u * i + kv, slot = n % kPfSlots;
+                live = bar_wait(smem_addr(&sh.kv_empty[slot]), ((n / kPfSlots) & 1u) ^ 1u, live);
+                const uint32_t dst = kv_at + slot * kBytes;
+                const uint16_t *src = (kv ? p.v : p.k) + (int64_t)head * p.head_stride + col * 8u;
+#pragma unroll
+                for (uint32_t r0 = 0; r0 < kPfTile; r0 += 16u) {
+                    const int64_t at = sh.place[i & 1u][r0 + row];
+                    const uint16_t *from = at >= 0 ? src + at : p.k;
+#pragma unroll
+                    for (int x = 0; x < D / 64; ++x) copy_async16(dst + x * 16384u + swizzled(r0 + row), at >= 0 ? from + x * 64 : from, at >= 0);
+                }
+                copy_commit();
+                if (n == 0u) { copy_wait<1>(); arrive(smem_addr(&sh.q_full)); }
+                if (n >= 2u) { copy_wait<2>(); arrive(smem_addr(&sh.kv_full[done % kPfSlots])); ++done; }
+            }
+            barrier_of(1, 128);                              // the next tile's places are there, this one's are done with
+        }
+        copy_wait<1>(); arrive(smem_addr(&sh.kv_full[done % kPfSlots])); ++done;
+        copy_wait<0>(); arrive(smem_addr(&sh.kv_full[done % kPfSlots]));
+    } else if (warp == 12u) {
+        // ---- the products
+        if (lane == 0u) {
+            const uint32_t id_s = product_desc(kBf16, false, 128u, 128u), id_o = product_desc(kBf16, true, 128u, D);
+            const uint32_t tiles = two ? 2u : 1u;
+            auto scores = [&](uint32_t t, uint32_t slot) {
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k)
+                    product_ss(tmem + t * 128u, tile_desc(q_at + t * kBytes + (k >> 2) * 16384u + (k & 3) * 32u, 16u, 1024u),
+                               tile_desc(kv_at + slot * kBytes + (k >> 2) * 16384u + (k & 3) * 32u, 16u, 1024u), id_s, k ? 1u : 0u);
+                products_arrive(smem_addr(&sh.s_full[t]));
+            };
+            live = bar_wait(smem_addr(&sh.q_full), 0u, live);
+            live = bar_wait(smem_addr(&sh.kv_full[0]), 0u, live);
+            tensor_fence_after();
+            for (uint32_t t = 0; t < tiles; ++t) scores(t, 0u);
+            products_arrive(smem_addr(&sh.kv_empty[0]));
+            for (uint32_t i = 0; i < n_tiles; ++i) {
+                const uint32_t nv = 2u * i + 1u, sv = nv % kPfSlots, nk = 2u * i + 2u, sk = nk % kPfSlots;
+                const bool more = i + 1u < n_tiles;
+                live = bar_wait(smem_addr(&sh.kv_full[sv]), (nv / kPfSlots) & 1u, live);
+                if (more) live = bar_wait(smem_addr(&sh.kv_full[sk]), (nk / kPfSlots) & 1u, live);
+                for (uint32_t t = 0; t < tiles; ++t) {
+                    live = bar_wait(smem_addr(&sh.p_full[t]), i & 1u, live);
+                    tensor_fence_after();
+#pragma unroll
+                    for (int k = 0; k < kPfTile / 16; ++k)
+                        product_ts(tmem + 256u + t * 128u, tmem + t * 128u + k * 8u, tile_desc(kv_at + sv * kBytes + k * 2048u, 16384u, 1024u), id_o, i || k ? 1u : 0u);
+                    products_arrive(smem_addr(&sh.o_full[t]));
+                    if (more) scores(t, sk);
+                }
+                products_arrive(smem_addr(&sh.kv_empty[sv]));
+                if (more) products_arrive(smem_addr(&sh.kv_empty[sk]));
+            }
+            if (!live) sh.bad = 1u;
+        }
+        __syncwarp();
+    } else if (warp < 4u || two) {
+        // ---- weights: a row a thread
+        const uint32_t t = warp >> 2, r = tid & 127u;
+        const uint32_t s_at = tmem + t * 128u + (((warp & 3u) * 32u) << 16), o_at = s_at + 256u;
+        const float scale = p.scale_log2, lift = kBf16 ? 0.0f : 7.0f;         // weights are at most 2^8, in fp16 2^15
+        float m = -INFINITY, l = 0.0f;
+        for (uint32_t i = 0; i < n_tiles; ++i) {
+            live = bar_wait(smem_addr(&sh.s_full[t]), i & 1u, live);
+            __syncwarp();
+            tensor_fence_after();
+            const uint32_t valid = min((uint32_t)kPfTile, end - begin - i * kPfTile);
+            float best = -INFINITY;
+            uint32_t v[32];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                tensor_load(s_at + c * 32u, v);
+                tensor_loaded(v);
+                if (c * 32u + 32u <= valid) {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) best = fmaxf(best, __uint_as_float(v[k]) * scale);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) if (c * 32u + k < valid) best = fmaxf(best, __uint_as_float(v[k]) * scale);
+                }
+            }
+            const bool grow = m != -INFINITY && best > m + kPfGrow;
+            if (__any_sync(0xffffffffu, grow)) {             // the sums so far, scaled to the new maximum: when the products before are done
+                const float f = grow ? exp2_fast(m - best) : 1.0f;
+                live = bar_wait(smem_addr(&sh.o_full[t]), (i - 1u) & 1u, live);
+                __syncwarp();
+                tensor_fence_after();
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    tensor_load(o_at + c * 32u, v);
+                    tensor_loaded(v);
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * f);
+                    tensor_store32(o_at + c * 32u, v);
+                }
+                l *= f;
+            }
+            if (grow || m == -INFINITY) m = best;
+            const float z = m == -INFINITY ? 0.0f : m - lift;
+            float sum = 0.0f;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t w[16];
+                tensor_load(s_at + c * 32u, v);
+                tensor_loaded(v);
+#pragma unroll
+                for (int k = 0; k < 32; k += 2) {
+                    float a = exp2_fast(fmaf(__uint_as_float(v[k]), scale, -z)), b = exp2_fast(fmaf(__uint_as_float(v[k + 1]), scale, -z));
+                    if (c * 32u + k >= valid) a = 0.0f;
+                    if (c * 32u + k + 1u >= valid) b = 0.0f;
+                    sum += a + b;
+                    w[k / 2] = Ty::pack(a, b);
+                }
+                tensor_store16(s_at + c * 16u, w);           // over scores that were read: columns 16 c to 16 c + 15 of 32 c + 32
+            }
+            l += sum;
+            tensor_stored();
+            tensor_fence_before();
+            bar_arrive(smem_addr(&sh.p_full[t]));
+        }
+        live = bar_wait(smem_addr(&sh.o_full[t]), (n_tiles - 1u) & 1u, live);
+        __syncwarp();
+        tensor_fence_after();
+        if (!live || *(volatile uint32_t *)&sh.bad) l = __int_as_float(0x7fc00000);
+        const uint32_t n = row0 + t * kPfTile + r;
+        const bool mine = n < all_rows;
+        const uint32_t b = n / p.G, h = head * p.G + (n - b * p.G);
+        const size_t rows = (size_t)p.B * p.Hq, at = (size_t)(p.own_pieces + piece) * rows + (size_t)b * p.Hq + h;
+        const float z = m - lift, inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+            uint32_t v[32];
+            __syncwarp();
+            tensor_load(o_at + c * 32u, v);
+            tensor_loaded(v);
+            if (mine && p.pieces == 1u) {
+                uint4 *to = reinterpret_cast<uint4 *>(p.out + (int64_t)b * p.out_row + (int64_t)h * p.out_head + c * 32);
+#pragma unroll
+                for (int k = 0; k < 32; k += 8) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = l == 0.0f ? 0u : Ty::pack(__uint_as_float(v[k + 2 * e]) * inv, __uint_as_float(v[k + 2 * e + 1]) * inv);
+                    to[k / 8] = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            } else if (mine) {
+                uint4 *to = reinterpret_cast<uint4 *>(p.part_o + at * D + c * 32);
+#pragma unroll
+                for (int k = 0; k < 32; k += 4) to[k / 4] = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+            }
+        }
+        if (mine) {
+            if (p.pieces > 1u) p.part_ml[at] = make_float2(z, l);
+            else if (p.lse) p.lse[(size_t)b * p.Hq + h] = l == 0.0f ? -INFINITY : (z + log2f(l)) * 0.69314718055994531f;
+        }
+        tensor_fence_before();
+    }
+    pdl_wait();                                              // a kernel behind this one counts on what came before it, too
+    __syncthreads();
+    __syncwarp();
+    if (warp == 12u) {
+        tensor_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    }
+}
+
+template <class Ty, int D, bool kBf16>
+static cudaError_t launch_tiles(const AttnDev &p, bool behind, cudaStream_t st) {
+    const auto k = k_prefix_tiles<Ty, D, kBf16>;
+    cudaError_t e = ensure_dyn_smem((const void *)k, pf_smem<D>());
+    if (e != cudaSuccess) return e;
+    g_kernel_launches += 1;
+    if (behind) return launch_pdl(k, p.n_prefix_items, kPfThreads, pf_smem<D>(), st, p);
+    k<<<p.n_prefix_items, kPfThreads, pf_smem<D>(), st>>>(p);
+    return cudaGetLastError();
+}
+cudaError_t launch_prefix_tiles(const AttnDev &p, uint32_t dim, bool bf16, bool behind, cudaStream_t st) {
+    if (bf16) return dim == 128u ? launch_tiles<Bf16, 128, true>(p, behind, st) : launch_tiles<Bf16, 64, true>(p, behind, st);
+    return dim == 128u ? launch_tiles<Fp16, 128, false>(p, behind, st) : launch_tiles<Fp16, 64, false>(p, behind, st);
+}
+
+}  // namespace hbf
