@@ -226,54 +226,87 @@ k_attend(const __grid_constant__ AttnDev p) {
             if (p.lse && col == 0u) p.lse[n] = L == 0.0f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
         } else {
             const size_t rows = (size_t)p.B * p.Hq;
-            *reinterpret_cast<float4 *>(p.part_o + (slot_out * rows + n) * D + col * 4u) = v;
+            if (L != 0.0f) *reinterpret_cast<float4 *>(p.part_o + (slot_out * rows + n) * D + col * 4u) = v;
             if (col == 0u) p.part_ml[slot_out * rows + n] = make_float2(M, L);
         }
     }
 }
 
-// Joins a row's pieces: a block a row, a piece a warp at a time.
+// Joins the rows' pieces: kPer warps a row.  First the pieces' shares of the whole, exp2(m - M), by a thread each; then their sums, four of a
+// warp's pieces on their way at a time.
 constexpr int kJoinWarps = 8;
-template <class Ty, int D>
+constexpr uint32_t kMostPieces = 1024;
+template <class Ty, int D, int kPer>
 __global__ void __launch_bounds__(kJoinWarps * 32)
 k_attend_join(const __grid_constant__ AttnDev p) {
-    const uint32_t lane = lane_id(), warp = threadIdx.x >> 5, n = blockIdx.x;
-    constexpr int kEach = D / 32;
-    __shared__ float sm[kJoinWarps], sl[kJoinWarps], so[kJoinWarps][D];
+    constexpr int kRows = kJoinWarps / kPer, kEach = D / 32;
+    __shared__ float share[kRows][kMostPieces / kRows], red[kJoinWarps][2], so[kJoinWarps][D];
+    const uint32_t lane = lane_id(), warp = threadIdx.x >> 5, group = warp / kPer, part = warp % kPer;
     const size_t rows = (size_t)p.B * p.Hq;
+    const uint32_t n = blockIdx.x * kRows + group;
+    const bool there = n < rows;
+    float *f = share[group];
     pdl_wait();
-    float M = -INFINITY, L = 0.0f, v[kEach];
+    float M = -INFINITY, L = 0.0f;
+    if (there)
+        for (uint32_t s = part * 32u + lane; s < p.pieces; s += kPer * 32u) {
+            float2 ml;
+            asm volatile("ld.global.cg.v2.f32 {%0,%1}, [%2];" : "=f"(ml.x), "=f"(ml.y) : "l"(p.part_ml + s * rows + n));
+            if (ml.y == 0.0f) ml.x = -INFINITY;              // an empty piece
+            const float N = fmaxf(M, ml.x), z = N == -INFINITY ? 0.0f : N;
+            L = L * exp2_fast(M - z) + ml.y * exp2_fast(ml.x - z);
+            M = N; f[s] = ml.x;
+        }
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) v[i] = 0.0f;
-#pragma unroll 4
-    for (uint32_t s = warp; s < p.pieces; s += kJoinWarps) {
-        float2 ml; float x[kEach];
-        asm volatile("ld.global.cg.v2.f32 {%0,%1}, [%2];" : "=f"(ml.x), "=f"(ml.y) : "l"(p.part_ml + s * rows + n));
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) asm volatile("ld.global.cg.f32 %0, [%1];" : "=f"(x[i]) : "l"(p.part_o + (s * rows + n) * D + i * 32 + lane));
-        if (ml.y == 0.0f) continue;                          // an empty piece
-        const float N = fmaxf(M, ml.x), z = N == -INFINITY ? 0.0f : N;
-        const float f = exp2_fast(M - z), g = exp2_fast(ml.x - z);
-        M = N; L = L * f + ml.y * g;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) v[i] = v[i] * f + x[i] * g;
+    for (int o = 16; o > 0; o >>= 1) {
+        const float m2 = __shfl_xor_sync(0xffffffffu, M, o), l2 = __shfl_xor_sync(0xffffffffu, L, o), N = fmaxf(M, m2), z = N == -INFINITY ? 0.0f : N;
+        L = L * exp2_fast(M - z) + l2 * exp2_fast(m2 - z);
+        M = N;
     }
-    if (lane == 0u) { sm[warp] = M; sl[warp] = L; }
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) so[warp][i * 32 + lane] = v[i];
+    if (lane == 0u) { red[warp][0] = M; red[warp][1] = L; }
     __syncthreads();
-    if (threadIdx.x >= D) return;
     M = -INFINITY; L = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) M = fmaxf(M, sm[w]);
+    for (int w = 0; w < kPer; ++w) M = fmaxf(M, red[group * kPer + w][0]);
     const float z = M == -INFINITY ? 0.0f : M;
-    float a = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) { const float f = exp2_fast(sm[w] - z); L += f * sl[w]; a += f * so[w][threadIdx.x]; }
+    for (int w = 0; w < kPer; ++w) L += exp2_fast(red[group * kPer + w][0] - z) * red[group * kPer + w][1];
+    float v[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) v[i] = 0.0f;
+    if (there)
+        for (uint32_t s0 = part; s0 < p.pieces; s0 += kPer * 4u) {
+            float x[4][kEach], g[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t s = s0 + k * kPer;
+                g[k] = s < p.pieces ? exp2_fast(f[s] - z) : 0.0f;
+                const float *from = p.part_o + (s * rows + n) * D + lane * kEach;
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) x[k][i] = 0.0f;
+                if (g[k] != 0.0f) {
+                    if (kEach == 4) asm volatile("ld.global.cg.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x[k][0]), "=f"(x[k][1]), "=f"(x[k][kEach - 2]), "=f"(x[k][kEach - 1]) : "l"(from));
+                    else asm volatile("ld.global.cg.v2.f32 {%0,%1}, [%2];" : "=f"(x[k][0]), "=f"(x[k][1]) : "l"(from));
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) v[i] += g[k] * x[k][i];
+        }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) so[warp][lane * kEach + i] = v[i];
+    __syncthreads();
+    if (!there) return;
     const uint32_t b = n / p.Hq, h = n - b * p.Hq;
-    const float r = L == 0.0f ? 0.0f : a / L;
-    reinterpret_cast<typename Ty::type *>(p.out)[(int64_t)b * p.out_row + (int64_t)h * p.out_head + threadIdx.x] = Ty::from(r);
-    if (p.lse && threadIdx.x == 0) p.lse[n] = L == 0.0f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
+    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+    for (uint32_t d = (part * 32u + lane) * 2u; d < (uint32_t)D; d += kPer * 64u) {
+        float a0 = 0.0f, a1 = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kPer; ++w) { a0 += so[group * kPer + w][d]; a1 += so[group * kPer + w][d + 1u]; }
+        *reinterpret_cast<uint32_t *>(p.out + (int64_t)b * p.out_row + (int64_t)h * p.out_head + d) = L == 0.0f ? 0u : Ty::pack(a0 * inv, a1 * inv);
+    }
+    if (p.lse && part == 0u && lane == 0u) p.lse[n] = L == 0.0f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
 }
 
 // The records of what a step reads: every page of the prefix once, keys then values, then every request's own pages; the places of pages
@@ -335,7 +368,7 @@ static void attention_pieces(const hbf_attention_t *a, uint32_t n_sm, AttnDev &p
         // (k_prefix_tiles: a block an SM, tiles of 128 keys)
         const uint32_t step = p.prefix_rows == 256u ? 128u : 64u, there = p.prefix_rows == 256u ? n_sm : blocks;
         const uint32_t pairs = p.row_tiles * p.Hk, most = (a->prefix_len + step - 1u) / step;
-        const uint32_t want = there > pairs ? there / pairs : 1u;
+        const uint32_t want = there <= pairs ? 1u : there / pairs < kMostPieces / 4u ? there / pairs : kMostPieces / 4u;
         p.prefix_chunk = up_to((a->prefix_len + (want < most ? want : most) - 1u) / (want < most ? want : most), step);
         p.prefix_pieces = (a->prefix_len + p.prefix_chunk - 1u) / p.prefix_chunk;
     }
@@ -344,6 +377,8 @@ static void attention_pieces(const hbf_attention_t *a, uint32_t n_sm, AttnDev &p
         const uint64_t lists = (uint64_t)p.B * p.Hk * p.group_tiles;
         uint64_t chunk = ((uint64_t)a->max_own_len * lists + blocks - 1u) / blocks;
         chunk = chunk < 64u ? 64u : chunk > 512u ? 512u : chunk;
+        const uint64_t least = ((uint64_t)a->max_own_len + kMostPieces / 4u - 1u) / (kMostPieces / 4u);
+        if (chunk < least) chunk = least;
         p.own_chunk = up_to((uint32_t)chunk, 64u);
         p.own_pieces = (a->max_own_len + p.own_chunk - 1u) / p.own_chunk;
     }
@@ -386,8 +421,11 @@ static cudaError_t launch_attention(AttnDev p, bool bf16, cudaStream_t st) {
     if (tiles && (e = launch_prefix_tiles(p, D, bf16, items != 0u, st)) != cudaSuccess) return e;
     if (p.pieces == 1u) return e;
     g_kernel_launches += 1;
-    if (p.pieces == 0u) { k_attend_join<Ty, D><<<p.B * p.Hq, kJoinWarps * 32, 0, st>>>(p); return cudaGetLastError(); }
-    return launch_pdl(k_attend_join<Ty, D>, p.B * p.Hq, kJoinWarps * 32, 0, st, p);
+    const bool few = p.pieces <= 32u;                        // 64 requests, 18 pieces each: two warps a row 5.3 us, eight 10.1
+    const auto join = few ? k_attend_join<Ty, D, 2> : k_attend_join<Ty, D, kJoinWarps>;
+    const uint32_t blocks = few ? (p.B * p.Hq + kJoinWarps / 2 - 1u) / (kJoinWarps / 2) : p.B * p.Hq;
+    if (p.pieces == 0u) { join<<<blocks, kJoinWarps * 32, 0, st>>>(p); return cudaGetLastError(); }
+    return launch_pdl(join, blocks, kJoinWarps * 32, 0, st, p);
 }
 
 }  // namespace hbf

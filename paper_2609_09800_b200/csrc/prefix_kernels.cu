@@ -4,13 +4,14 @@
 // other's weights are worked out: 2 x 512 cycles of products for a tile of keys against 1,024 of exponentials, which all
 // eight warps of both tiles share.  The keys are read once for 256 rows; the products bound it from about 64 rows on.
 //
-// Warps 0 to 3 and 4 to 7: a row each thread, of the first and the second tile.  8 to 11: gather keys and values from their pages into the
-// swizzled layout that the tensor cores read.  12: one thread issues the products.
+// Warps 0 to 3 and 4 to 7: a row each thread, of the first and the second tile; they take most of the registers, for a row's 128 scores at
+// once.  8 to 11: gather keys and values from their pages into the swizzled layout that the tensor cores read.  12: one thread issues
+// the products.
 #include "attention.cuh"
 
 namespace hbf {
 
-constexpr int kPfThreads = 13 * 32, kPfTile = 128, kPfSlots = 4;
+constexpr int kPfThreads = 16 * 32, kPfTile = 128, kPfSlots = 4;
 constexpr float kPfGrow = 8.0f;                              // sums are scaled again only when a row's maximum has grown by more (in powers of two)
 
 // What lies in shared memory behind the tiles.
@@ -65,6 +66,33 @@ __device__ __forceinline__ void tensor_store32(uint32_t addr, const uint32_t (&v
 }
 __device__ __forceinline__ void tensor_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// Two numbers at a time.
+__device__ __forceinline__ uint64_t two_of(float a, float b) { uint64_t v; asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); return v; }
+__device__ __forceinline__ void of_two(uint64_t v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma_two(uint64_t a, uint64_t b, uint64_t c) { uint64_t d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c)); return d; }
+__device__ __forceinline__ uint64_t add_two(uint64_t a, uint64_t b) { uint64_t d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
+__device__ __forceinline__ float max3_nan(float a, float b, float c) { float d; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d; }
+__device__ __forceinline__ float min3_nan(float a, float b, float c) { float d; asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d; }
+// exp2 of two numbers on the multiply-add units, for x <= 100, at least 2^-126: x = n + f, |f| <= 1/2; 2^f by the polynomial of degree 5 with the
+// least largest relative error there (7.5e-8, found by the exchange algorithm of Remez), n added to the exponent.  The exponential unit
+// gives 16 results a cycle and SM, as long for a tile of keys as the products take: every fourth pair goes this way.
+__device__ __forceinline__ void exp2_two(uint64_t x, float &a, float &b) {
+    float x0, x1;
+    of_two(x, x0, x1);
+    x = two_of(fmaxf(x0, -126.0f), fmaxf(x1, -126.0f));
+    const uint64_t r = add_two(x, two_of(12582912.0f, 12582912.0f));         // 1.5 * 2^23: n in the low bits
+    const uint64_t f = add_two(x, fma_two(r, two_of(-1.0f, -1.0f), two_of(12582912.0f, 12582912.0f)));
+    uint64_t y = two_of(0.0013276472454890609f, 0.0013276472454890609f);
+    y = fma_two(y, f, two_of(0.009675540961325169f, 0.009675540961325169f));
+    y = fma_two(y, f, two_of(0.05550713092088699f, 0.05550713092088699f));
+    y = fma_two(y, f, two_of(0.24022120237350464f, 0.24022120237350464f));
+    y = fma_two(y, f, two_of(0.6931469440460205f, 0.6931469440460205f));
+    y = fma_two(y, f, two_of(1.0000001192092896f, 1.0000001192092896f));
+    float r0, r1, y0, y1;
+    of_two(r, r0, r1); of_two(y, y0, y1);
+    a = __uint_as_float(__float_as_uint(y0) + (__float_as_uint(r0) << 23)); b = __uint_as_float(__float_as_uint(y1) + (__float_as_uint(r1) << 23));
+}
+
 template <class Ty, int D, bool kBf16>
 __global__ void __launch_bounds__(kPfThreads, 1)
 k_prefix_tiles(const __grid_constant__ AttnDev p) {
@@ -99,7 +127,9 @@ k_prefix_tiles(const __grid_constant__ AttnDev p) {
     const uint32_t tmem = sh.tmem;                           // S (and P) of both tiles, then O of both
     bool live = true;
 
+    // the registers that the block was launched with, 128 a thread, as 192 for the weights, 80 for the copies, 48 for the products
     if (warp >= 8u && warp < 12u) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
         // ---- keys and values: eight lanes a row of 128 bytes
         const uint32_t t = tid - 256u, col = t & 7u, row = t >> 3;
         auto swizzled = [&](uint32_t r) { return r * 128u + ((col ^ (r & 7u)) * 16u); };
@@ -150,9 +180,10 @@ k_prefix_tiles(const __grid_constant__ AttnDev p) {
         }
         copy_wait<1>(); arrive(smem_addr(&sh.kv_full[done % kPfSlots])); ++done;
         copy_wait<0>(); arrive(smem_addr(&sh.kv_full[done % kPfSlots]));
-    } else if (warp == 12u) {
+    } else if (warp >= 12u) {
         // ---- the products
-        if (lane == 0u) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        if (warp == 12u && lane == 0u) {
             const uint32_t id_s = product_desc(kBf16, false, 128u, 128u), id_o = product_desc(kBf16, true, 128u, D);
             const uint32_t tiles = two ? 2u : 1u;
             auto scores = [&](uint32_t t, uint32_t slot) {
@@ -187,66 +218,96 @@ k_prefix_tiles(const __grid_constant__ AttnDev p) {
             if (!live) sh.bad = 1u;
         }
         __syncwarp();
-    } else if (warp < 4u || two) {
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+        if (warp < 4u || two) {
         // ---- weights: a row a thread
         const uint32_t t = warp >> 2, r = tid & 127u;
         const uint32_t s_at = tmem + t * 128u + (((warp & 3u) * 32u) << 16), o_at = s_at + 256u;
         const float scale = p.scale_log2, lift = kBf16 ? 0.0f : 7.0f;         // weights are at most 2^8, in fp16 2^15
+        const uint64_t scales = two_of(scale, scale);
         float m = -INFINITY, l = 0.0f;
         for (uint32_t i = 0; i < n_tiles; ++i) {
             live = bar_wait(smem_addr(&sh.s_full[t]), i & 1u, live);
             __syncwarp();
             tensor_fence_after();
             const uint32_t valid = min((uint32_t)kPfTile, end - begin - i * kPfTile);
-            float best = -INFINITY;
-            uint32_t v[32];
+            uint32_t v[4][32];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                tensor_load(s_at + c * 32u, v);
-                tensor_loaded(v);
-                if (c * 32u + 32u <= valid) {
+            for (int c = 0; c < 4; ++c) tensor_load(s_at + c * 32u, v[c]);
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) best = fmaxf(best, __uint_as_float(v[k]) * scale);
-                } else {
+            for (int c = 0; c < 4; ++c) tensor_loaded(v[c]);
+            if (valid < (uint32_t)kPfTile) {                 // behind the prefix's end: the score that weighs nothing
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) if (c * 32u + k < valid) best = fmaxf(best, __uint_as_float(v[k]) * scale);
-                }
+                for (int k = 0; k < kPfTile; ++k) if ((uint32_t)k >= valid) v[k / 32][k % 32] = __float_as_uint(scale < 0.0f ? INFINITY : -INFINITY);
             }
+            float e[4];
+            if (scale >= 0.0f) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    e[c] = __uint_as_float(v[c][0]);
+#pragma unroll
+                    for (int k = 1; k < 31; k += 2) e[c] = max3_nan(e[c], __uint_as_float(v[c][k]), __uint_as_float(v[c][k + 1]));
+                    e[c] = max3_nan(e[c], e[c], __uint_as_float(v[c][31]));
+                }
+                e[0] = max3_nan(e[0], e[1], max3_nan(e[2], e[2], e[3]));
+            } else {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    e[c] = __uint_as_float(v[c][0]);
+#pragma unroll
+                    for (int k = 1; k < 31; k += 2) e[c] = min3_nan(e[c], __uint_as_float(v[c][k]), __uint_as_float(v[c][k + 1]));
+                    e[c] = min3_nan(e[c], e[c], __uint_as_float(v[c][31]));
+                }
+                e[0] = min3_nan(e[0], e[1], min3_nan(e[2], e[2], e[3]));
+            }
+            const float best = e[0] * scale;
+            if (!(best < INFINITY)) l = __int_as_float(0x7fc00000);           // a NaN or an infinity among the scores: the row has no weights
             const bool grow = m != -INFINITY && best > m + kPfGrow;
             if (__any_sync(0xffffffffu, grow)) {             // the sums so far, scaled to the new maximum: when the products before are done
                 const float f = grow ? exp2_fast(m - best) : 1.0f;
                 live = bar_wait(smem_addr(&sh.o_full[t]), (i - 1u) & 1u, live);
                 __syncwarp();
                 tensor_fence_after();
-#pragma unroll
+#pragma unroll 1
                 for (int c = 0; c < D / 32; ++c) {
-                    tensor_load(o_at + c * 32u, v);
-                    tensor_loaded(v);
+                    uint32_t o[32];
+                    tensor_load(o_at + c * 32u, o);
+                    tensor_loaded(o);
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * f);
-                    tensor_store32(o_at + c * 32u, v);
+                    for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                    tensor_store32(o_at + c * 32u, o);
                 }
                 l *= f;
             }
             if (grow || m == -INFINITY) m = best;
             const float z = m == -INFINITY ? 0.0f : m - lift;
-            float sum = 0.0f;
+            const uint64_t minus_z = two_of(-z, -z);
+            uint64_t sum[2] = {0ull, 0ull};
+            const bool whole = valid == (uint32_t)kPfTile;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 uint32_t w[16];
-                tensor_load(s_at + c * 32u, v);
-                tensor_loaded(v);
 #pragma unroll
                 for (int k = 0; k < 32; k += 2) {
-                    float a = exp2_fast(fmaf(__uint_as_float(v[k]), scale, -z)), b = exp2_fast(fmaf(__uint_as_float(v[k + 1]), scale, -z));
-                    if (c * 32u + k >= valid) a = 0.0f;
-                    if (c * 32u + k + 1u >= valid) b = 0.0f;
-                    sum += a + b;
+                    const uint64_t x = fma_two(two_of(__uint_as_float(v[c][k]), __uint_as_float(v[c][k + 1])), scales, minus_z);
+                    float a, b;
+                    if ((k / 2) % 4 == 3) {
+                        exp2_two(x, a, b);
+                    } else {
+                        float x0, x1;
+                        of_two(x, x0, x1);
+                        a = exp2_fast(x0); b = exp2_fast(x1);
+                    }
+                    if (!whole) { if (c * 32u + k >= valid) a = 0.0f; if (c * 32u + k + 1u >= valid) b = 0.0f; }
+                    sum[(k / 2) & 1] = add_two(sum[(k / 2) & 1], two_of(a, b));
                     w[k / 2] = Ty::pack(a, b);
                 }
-                tensor_store16(s_at + c * 16u, w);           // over scores that were read: columns 16 c to 16 c + 15 of 32 c + 32
+                tensor_store16(s_at + c * 16u, w);
             }
-            l += sum;
+            float s0, s1;
+            of_two(add_two(sum[0], sum[1]), s0, s1);
+            if (m != -INFINITY) l += s0 + s1;
             tensor_stored();
             tensor_fence_before();
             bar_arrive(smem_addr(&sh.p_full[t]));
@@ -286,6 +347,7 @@ k_prefix_tiles(const __grid_constant__ AttnDev p) {
             else if (p.lse) p.lse[(size_t)b * p.Hq + h] = l == 0.0f ? -INFINITY : (z + log2f(l)) * 0.69314718055994531f;
         }
         tensor_fence_before();
+        }
     }
     pdl_wait();                                              // a kernel behind this one counts on what came before it, too
     __syncthreads();
