@@ -26,9 +26,14 @@ template <int D> constexpr uint32_t pf_smem() { return (2u + kPfSlots) * kPfTile
 // matrices in shared memory: rows of 64 values (128 bytes) in groups of eight, 16-byte columns permuted by the row's number, the next 64 values of
 // all rows behind.  Rows as the products' rows or columns (the sum along a row): `next8` is the way to the next eight rows; the sum along
 // the rows' numbers: also `next64` to the next 64 values.
-__device__ __forceinline__ uint64_t tile_desc(uint32_t addr, uint32_t next64, uint32_t next8) {
-    return (uint64_t)((addr >> 4) & 0x3fffu) | (uint64_t)((next64 >> 4) & 0x3fffu) << 16 | (uint64_t)((next8 >> 4) & 0x3fffu) << 32 | 1ull << 46 | 2ull << 61;
-}
+struct TileDesc {
+    uint32_t lo, hi;
+    __device__ __forceinline__ TileDesc(uint32_t addr, uint32_t next64, uint32_t next8)
+        : lo((addr >> 4) | (next64 >> 4) << 16), hi(next8 >> 4 | 1u << 14 | 2u << 29) {}
+    __device__ __forceinline__ uint64_t at(uint32_t bytes) const {           // (shared memory ends below 2^18: no carry into the next field)
+        uint64_t d; asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo + (bytes >> 4)), "r"(hi)); return d;
+    }
+};
 __device__ __forceinline__ uint32_t product_desc(bool bf16, bool b_by_rows, uint32_t m, uint32_t n) {
     const uint32_t type = bf16 ? 1u : 0u;
     return 1u << 4 | type << 7 | type << 10 | (b_by_rows ? 1u << 16 : 0u) | (n >> 3) << 17 | (m >> 4) << 24;
@@ -156,12 +161,14 @@ k_prefix_tiles(const __grid_constant__ AttnDev p) {
         };
         find(0);
         barrier_of(1, 128);
-        uint32_t done = 0u;                                  // tiles (of keys or values) that were said to be there
         auto arrive = [&](uint32_t bar) { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); bar_arrive(bar); };
         for (uint32_t i = 0; i < n_tiles; ++i) {
             if (i + 1u < n_tiles) find(i + 1u);
             for (uint32_t kv = 0; kv < 2u; ++kv) {
                 const uint32_t n = 2u * i + kv, slot = n % kPfSlots;
+                // what has come is said to be there before the wait for a free slot, which needs it to be used
+                if (n == 1u) { copy_wait<1>(); arrive(smem_addr(&sh.q_full)); }
+                if (n >= 2u) { copy_wait<1>(); arrive(smem_addr(&sh.kv_full[(n - 2u) % kPfSlots])); }
                 live = bar_wait(smem_addr(&sh.kv_empty[slot]), ((n / kPfSlots) & 1u) ^ 1u, live);
                 const uint32_t dst = kv_at + slot * kBytes;
                 const uint16_t *src = (kv ? p.v : p.k) + (int64_t)head * p.head_stride + col * 8u;
@@ -173,25 +180,35 @@ k_prefix_tiles(const __grid_constant__ AttnDev p) {
                     for (int x = 0; x < D / 64; ++x) copy_async16(dst + x * 16384u + swizzled(r0 + row), at >= 0 ? from + x * 64 : from, at >= 0);
                 }
                 copy_commit();
-                if (n == 0u) { copy_wait<1>(); arrive(smem_addr(&sh.q_full)); }
-                if (n >= 2u) { copy_wait<2>(); arrive(smem_addr(&sh.kv_full[done % kPfSlots])); ++done; }
             }
             barrier_of(1, 128);                              // the next tile's places are there, this one's are done with
         }
-        copy_wait<1>(); arrive(smem_addr(&sh.kv_full[done % kPfSlots])); ++done;
-        copy_wait<0>(); arrive(smem_addr(&sh.kv_full[done % kPfSlots]));
+        copy_wait<1>(); arrive(smem_addr(&sh.kv_full[(2u * n_tiles - 2u) % kPfSlots]));
+        copy_wait<0>(); arrive(smem_addr(&sh.kv_full[(2u * n_tiles - 1u) % kPfSlots]));
     } else if (warp >= 12u) {
         // ---- the products
         asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         if (warp == 12u && lane == 0u) {
             const uint32_t id_s = product_desc(kBf16, false, 128u, 128u), id_o = product_desc(kBf16, true, 128u, D);
             const uint32_t tiles = two ? 2u : 1u;
+            const uint32_t s_full = smem_addr(sh.s_full), o_full = smem_addr(sh.o_full);
+            const TileDesc q0(q_at, 16u, 1024u), kv0(kv_at, 16u, 1024u), v0(kv_at, 16384u, 1024u);
+            // (one thread issues a product every 64 cycles: what can be is worked out before)
             auto scores = [&](uint32_t t, uint32_t slot) {
+                TileDesc q = q0, k0 = kv0;
+                q.lo += t * (kBytes >> 4); k0.lo += slot * (kBytes >> 4);
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k)
-                    product_ss(tmem + t * 128u, tile_desc(q_at + t * kBytes + (k >> 2) * 16384u + (k & 3) * 32u, 16u, 1024u),
-                               tile_desc(kv_at + slot * kBytes + (k >> 2) * 16384u + (k & 3) * 32u, 16u, 1024u), id_s, k ? 1u : 0u);
-                products_arrive(smem_addr(&sh.s_full[t]));
+                    product_ss(tmem + t * 128u, q.at((k >> 2) * 16384u + (k & 3) * 32u), k0.at((k >> 2) * 16384u + (k & 3) * 32u), id_s, k ? 1u : 0u);
+                products_arrive(s_full + t * 8u);
+            };
+            auto values = [&](uint32_t t, uint32_t slot, uint32_t add) {
+                TileDesc v = v0;
+                v.lo += slot * (kBytes >> 4);
+                const uint32_t d = tmem + 256u + t * 128u, a = tmem + t * 128u;
+#pragma unroll
+                for (int k = 0; k < kPfTile / 16; ++k) product_ts(d, a + k * 8u, v.at(k * 2048u), id_o, k ? 1u : add);
+                products_arrive(o_full + t * 8u);
             };
             live = bar_wait(smem_addr(&sh.q_full), 0u, live);
             live = bar_wait(smem_addr(&sh.kv_full[0]), 0u, live);
@@ -206,10 +223,7 @@ k_prefix_tiles(const __grid_constant__ AttnDev p) {
                 for (uint32_t t = 0; t < tiles; ++t) {
                     live = bar_wait(smem_addr(&sh.p_full[t]), i & 1u, live);
                     tensor_fence_after();
-#pragma unroll
-                    for (int k = 0; k < kPfTile / 16; ++k)
-                        product_ts(tmem + 256u + t * 128u, tmem + t * 128u + k * 8u, tile_desc(kv_at + sv * kBytes + k * 2048u, 16384u, 1024u), id_o, i || k ? 1u : 0u);
-                    products_arrive(smem_addr(&sh.o_full[t]));
+                    values(t, sv, i ? 1u : 0u);
                     if (more) scores(t, sk);
                 }
                 products_arrive(smem_addr(&sh.kv_empty[sv]));
