@@ -5,8 +5,11 @@
 // eight warps of both tiles share.  The keys are read once for 256 rows; the products bound it from about 64 rows on.
 //
 // Warps 0 to 3 and 4 to 7: a row each thread, of the first and the second tile; they take most of the registers, for a row's 128 scores at
-// once.  8 to 11: gather keys and values from their pages into the swizzled layout that the tensor cores read.  12: one thread issues
-// the products.
+// once.  8 to 11: keys and values from their pages into the swizzled layout that the tensor cores read: a tensor copy for every stretch of
+// slots of a page where pages are multiples of eight slots, else, and in a tile that the prefix ends in (behind its end there must be
+// zeros), 16 bytes a thread at a time, which take 1,150 cycles a tile against the 512 of its products.  12: one thread issues the products.
+#include <cuda.h>
+
 #include "attention.cuh"
 
 namespace hbf {
@@ -71,6 +74,12 @@ __device__ __forceinline__ void tensor_store32(uint32_t addr, const uint32_t (&v
 }
 __device__ __forceinline__ void tensor_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// A box of 64 values by some slots of one page and head, to the swizzled layout.
+__device__ __forceinline__ void tensor_copy(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t slot, int32_t head, int32_t page, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(slot), "r"(head), "r"(page), "r"(bar) : "memory");
+}
+
 // Two numbers at a time.
 __device__ __forceinline__ uint64_t two_of(float a, float b) { uint64_t v; asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); return v; }
 __device__ __forceinline__ void of_two(uint64_t v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
@@ -100,7 +109,7 @@ __device__ __forceinline__ void exp2_two(uint64_t x, float &a, float &b) {
 
 template <class Ty, int D, bool kBf16>
 __global__ void __launch_bounds__(kPfThreads, 1)
-k_prefix_tiles(const __grid_constant__ AttnDev p) {
+k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, uint32_t box) {
     extern __shared__ unsigned char smem_raw[];
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
     PfShared &sh = *reinterpret_cast<PfShared *>(smem_raw + (base - smem_addr(smem_raw)) + (2u + kPfSlots) * kPfTileBytes<D>);
@@ -159,32 +168,70 @@ k_prefix_tiles(const __grid_constant__ AttnDev p) {
             }
             sh.place[i & 1u][t] = at;
         };
-        find(0);
-        barrier_of(1, 128);
         auto arrive = [&](uint32_t bar) { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); bar_arrive(bar); };
-        for (uint32_t i = 0; i < n_tiles; ++i) {
-            if (i + 1u < n_tiles) find(i + 1u);
-            for (uint32_t kv = 0; kv < 2u; ++kv) {
-                const uint32_t n = 2u * i + kv, slot = n % kPfSlots;
-                // what has come is said to be there before the wait for a free slot, which needs it to be used
-                if (n == 1u) { copy_wait<1>(); arrive(smem_addr(&sh.q_full)); }
-                if (n >= 2u) { copy_wait<1>(); arrive(smem_addr(&sh.kv_full[(n - 2u) % kPfSlots])); }
-                live = bar_wait(smem_addr(&sh.kv_empty[slot]), ((n / kPfSlots) & 1u) ^ 1u, live);
-                const uint32_t dst = kv_at + slot * kBytes;
-                const uint16_t *src = (kv ? p.v : p.k) + (int64_t)head * p.head_stride + col * 8u;
+        // boxes of `box` slots (0: none): whole tiles; warp w takes the boxes w, w + 4, ...
+        const uint32_t whole = box ? (end - begin) / kPfTile : 0u, boxes = box ? kPfTile / box : 0u, my_boxes = boxes > warp - 8u ? (boxes - (warp - 8u) + 3u) / 4u : 0u;
+        if (whole) {
+            copy_wait<0>(); arrive(smem_addr(&sh.q_full));
+            int32_t page = 0;                                // lane l: that of this warp's box l
+            uint32_t slot0 = 0u;
+            auto look = [&](uint32_t i) {
+                if (lane >= my_boxes || i >= whole) return;
+                const uint32_t k = begin + i * kPfTile + (warp - 8u + lane * 4u) * box, n = div32(k, p.div_page);
+                page = p.prefix_pages[n]; slot0 = k - n * p.page_tokens;
+                if ((uint32_t)page >= p.n_pages) { sh.bad = 1u; page = -1; }              // (such a box is zeros)
+            };
+            look(0);
+            for (uint32_t i = 0; i < whole; ++i) {
+                const int32_t page_now = page;
+                const uint32_t slot_now = slot0;
+                look(i + 1u);
+#pragma unroll 1
+                for (uint32_t kv = 0; kv < 2u; ++kv) {
+                    const uint32_t n = 2u * i + kv, slot = n % kPfSlots, full = smem_addr(&sh.kv_full[slot]);
+                    live = bar_wait(smem_addr(&sh.kv_empty[slot]), ((n / kPfSlots) & 1u) ^ 1u, live);
+                    __syncwarp();
+                    if (lane == 0u) bar_arrive_bytes(full, live ? my_boxes * box * D * 2u : 0u);
+                    else bar_arrive(full);
+                    for (uint32_t j = 0; j < my_boxes; ++j) {
+                        const int32_t pg = __shfl_sync(0xffffffffu, page_now, j);
+                        const int32_t sl = (int32_t)__shfl_sync(0xffffffffu, slot_now, j);
+                        if (lane == 0u && live) {
+                            const uint32_t dst = kv_at + slot * kBytes + (warp - 8u + j * 4u) * box * 128u;
 #pragma unroll
-                for (uint32_t r0 = 0; r0 < kPfTile; r0 += 16u) {
-                    const int64_t at = sh.place[i & 1u][r0 + row];
-                    const uint16_t *from = at >= 0 ? src + at : p.k;
-#pragma unroll
-                    for (int x = 0; x < D / 64; ++x) copy_async16(dst + x * 16384u + swizzled(r0 + row), at >= 0 ? from + x * 64 : from, at >= 0);
+                            for (int x = 0; x < D / 64; ++x) tensor_copy(dst + x * 16384u, kv ? &v_map : &k_map, x * 64, sl, (int32_t)head, pg, full);
+                        }
+                    }
                 }
-                copy_commit();
             }
-            barrier_of(1, 128);                              // the next tile's places are there, this one's are done with
         }
-        copy_wait<1>(); arrive(smem_addr(&sh.kv_full[(2u * n_tiles - 2u) % kPfSlots]));
-        copy_wait<0>(); arrive(smem_addr(&sh.kv_full[(2u * n_tiles - 1u) % kPfSlots]));
+        if (whole < n_tiles) {
+            find(whole);
+            barrier_of(1, 128);
+            for (uint32_t i = whole; i < n_tiles; ++i) {
+                if (i + 1u < n_tiles) find(i + 1u);
+                for (uint32_t kv = 0; kv < 2u; ++kv) {
+                    const uint32_t n = 2u * i + kv, slot = n % kPfSlots, first = 2u * whole;
+                    // what has come is said to be there before the wait for a free slot, which needs it to be used
+                    if (n == 1u) { copy_wait<1>(); arrive(smem_addr(&sh.q_full)); }
+                    if (n >= first + 2u) { copy_wait<1>(); arrive(smem_addr(&sh.kv_full[(n - 2u) % kPfSlots])); }
+                    live = bar_wait(smem_addr(&sh.kv_empty[slot]), ((n / kPfSlots) & 1u) ^ 1u, live);
+                    const uint32_t dst = kv_at + slot * kBytes;
+                    const uint16_t *src = (kv ? p.v : p.k) + (int64_t)head * p.head_stride + col * 8u;
+#pragma unroll
+                    for (uint32_t r0 = 0; r0 < kPfTile; r0 += 16u) {
+                        const int64_t at = sh.place[i & 1u][r0 + row];
+                        const uint16_t *from = at >= 0 ? src + at : p.k;
+#pragma unroll
+                        for (int x = 0; x < D / 64; ++x) copy_async16(dst + x * 16384u + swizzled(r0 + row), at >= 0 ? from + x * 64 : from, at >= 0);
+                    }
+                    copy_commit();
+                }
+                barrier_of(1, 128);                          // the next tile's places are there, this one's are done with
+            }
+            copy_wait<1>(); arrive(smem_addr(&sh.kv_full[(2u * n_tiles - 2u) % kPfSlots]));
+            copy_wait<0>(); arrive(smem_addr(&sh.kv_full[(2u * n_tiles - 1u) % kPfSlots]));
+        }
     } else if (warp >= 12u) {
         // ---- the products
         asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
@@ -372,14 +419,41 @@ k_prefix_tiles(const __grid_constant__ AttnDev p) {
     }
 }
 
+// A map of one of the cache's two buffers: values, slots, heads, pages.  false: its strides are none that such a map can have.
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
+                                 CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+static EncodeTiled encode_tiled() {
+    static std::atomic<void *> known{nullptr};
+    void *f = known.load(std::memory_order_relaxed);
+    if (f) return reinterpret_cast<EncodeTiled>(f);
+    cudaDriverEntryPointQueryResult how;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &how) != cudaSuccess || how != cudaDriverEntryPointSuccess) return nullptr;
+    known.store(f, std::memory_order_relaxed);
+    return reinterpret_cast<EncodeTiled>(f);
+}
+static bool cache_map(CUtensorMap *map, const AttnDev &p, const uint16_t *base, uint32_t dim, bool bf16, uint32_t box) {
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    const cuuint64_t dims[4] = {dim, p.page_tokens, p.Hk, p.n_pages};
+    const cuuint64_t strides[3] = {(cuuint64_t)p.slot_stride * 2u, (cuuint64_t)p.head_stride * 2u, (cuuint64_t)p.page_stride * 2u};
+    const cuuint32_t boxes[4] = {64u, box, 1u, 1u}, steps[4] = {1u, 1u, 1u, 1u};
+    for (const cuuint64_t st : strides) if (st == 0u || st >= (1ull << 40)) return false;
+    return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<uint16_t *>(base), dims, strides, boxes, steps,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <class Ty, int D, bool kBf16>
 static cudaError_t launch_tiles(const AttnDev &p, bool behind, cudaStream_t st) {
     const auto k = k_prefix_tiles<Ty, D, kBf16>;
     cudaError_t e = ensure_dyn_smem((const void *)k, pf_smem<D>());
     if (e != cudaSuccess) return e;
     g_kernel_launches += 1;
-    if (behind) return launch_pdl(k, p.n_prefix_items, kPfThreads, pf_smem<D>(), st, p);
-    k<<<p.n_prefix_items, kPfThreads, pf_smem<D>(), st>>>(p);
+    CUtensorMap k_map = {}, v_map = {};
+    uint32_t box = p.page_tokens & (0u - p.page_tokens);     // the largest power of two that a page is a multiple of
+    if (box > (uint32_t)kPfTile) box = kPfTile;
+    if (box < 8u || !cache_map(&k_map, p, p.k, D, kBf16, box) || !cache_map(&v_map, p, p.v, D, kBf16, box)) box = 0u;
+    if (behind) return launch_pdl(k, p.n_prefix_items, kPfThreads, pf_smem<D>(), st, p, k_map, v_map, box);
+    k<<<p.n_prefix_items, kPfThreads, pf_smem<D>(), st>>>(p, k_map, v_map, box);
     return cudaGetLastError();
 }
 cudaError_t launch_prefix_tiles(const AttnDev &p, uint32_t dim, bool bf16, bool behind, cudaStream_t st) {
