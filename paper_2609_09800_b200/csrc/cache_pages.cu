@@ -3,7 +3,8 @@
 // State, all the caller's, in device memory: refs[page] (rows that hold the page; 0 = free), lens[row] (tokens) and tables[row][j] (page
 // of the tokens from j * page_tokens on; the first ceil(len / page_tokens) entries count).  A call is two kernels: a plan by one
 // block, which looks at everything that the call depends on and works out the pages that move, and one over the whole device that does it;
-// where the plan finds a fault, the second does nothing.  Which page goes where follows from the state alone (the lowest free
+// where the plan finds a fault, the second does nothing; what a block does in no more time than another launch takes, the plan's block does.
+// Which page goes where follows from the state alone (the lowest free
 // page first), so that the same calls give the same cache.  Bytes bound the moves (each page read once and written once); small calls
 // cost two launches.
 #include "tensor_ops.cuh"
@@ -11,6 +12,8 @@
 namespace hbf {
 
 constexpr int kPlanThreads = 1024, kMoveThreads = 256;
+
+enum { kDoCopy = 0, kDoFork = 1, kDoFree = 2, kDoCompact = 3 };
 
 struct PagesCtrl { int32_t code, moves, n_live; };   // the first words of the workspace
 
@@ -23,6 +26,8 @@ struct PagesDev {
 };
 
 __device__ __forceinline__ uint32_t held_pages(const PagesDev &p, int32_t len) { return ((uint32_t)len + p.page_tokens - 1u) / p.page_tokens; }
+
+__device__ __forceinline__ bool len_bad(const PagesDev &p, int32_t len) { return len < 0 || (uint64_t)len > (uint64_t)p.cols * p.page_tokens; }
 
 // exclusive sum over the block of one number a thread; the total for all
 __device__ uint32_t block_scan(uint32_t v, uint32_t *total, uint32_t *warps) {
@@ -44,184 +49,28 @@ __device__ uint32_t block_scan(uint32_t v, uint32_t *total, uint32_t *warps) {
     return s - v + (warp ? warps[warp - 1u] : 0u);
 }
 
-__device__ void finish_plan(const PagesDev &p, int code, uint32_t moves, uint32_t n_live) {
-    if (threadIdx.x != 0) return;
-    p.ctrl->code = code; p.ctrl->moves = code == HBF_OK ? (int32_t)moves : 0; p.ctrl->n_live = (int32_t)n_live;
-    if (p.result) { p.result[0] = code; p.result[1] = p.ctrl->moves; p.result[2] = (int32_t)n_live; }
-}
-
-// The listed pairs are sound if every page exists, no destination is named twice and none is a source too (their order would count).
-__global__ void __launch_bounds__(kPlanThreads)
-k_plan_copy(const __grid_constant__ PagesDev p, const int32_t *src, const int32_t *dst, uint32_t n) {
-    extern __shared__ uint32_t bits[];
-    pdl_trigger();
-    const uint32_t words = (p.n_pages + 31u) / 32u;
-    for (uint32_t i = threadIdx.x; i < words; i += kPlanThreads) bits[i] = 0u;
-    int bad = 0;
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < n; i += kPlanThreads) {
-        const uint32_t d = (uint32_t)dst[i];
-        if (d >= p.n_pages || (atomicOr(&bits[d >> 5], 1u << (d & 31u)) >> (d & 31u)) & 1u) bad = 1;
-    }
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < n; i += kPlanThreads) {
-        const uint32_t s = (uint32_t)src[i];
-        if (s >= p.n_pages || (bits[s >> 5] >> (s & 31u)) & 1u) bad = 1;
-        p.src[i] = (int32_t)s; p.dst[i] = dst[i];
-    }
-    bad = __syncthreads_or(bad);
-    finish_plan(p, bad ? HBF_E_INVAL : HBF_OK, n, 0u);
-}
-
-// A row's entries that count name pages in use.
-__device__ __forceinline__ int row_bad(const PagesDev &p, uint32_t row, int32_t len, uint32_t from, uint32_t step) {
-    int bad = 0;
-    const int32_t *t = p.tables + (int64_t)row * p.table_stride;
-    const uint32_t held = held_pages(p, len);
-#pragma unroll 4
-    for (uint32_t j = from; j < held; j += step) {
-        const uint32_t id = (uint32_t)t[j];
-        if (id >= p.n_pages || p.refs[id] <= 0) bad = 1;
-    }
-    return bad;
-}
-__device__ __forceinline__ bool len_bad(const PagesDev &p, int32_t len) { return len < 0 || (uint64_t)len > (uint64_t)p.cols * p.page_tokens; }
-
-// Rows that begin as other rows' tokens: full pages are shared, a begun page is copied into the lowest free one, in the order of the list.
-__global__ void __launch_bounds__(kPlanThreads)
-k_plan_fork(const __grid_constant__ PagesDev p, const int32_t *parents, const int32_t *children, uint32_t n) {
-    extern __shared__ uint32_t bits[];                       // rows named as children
-    __shared__ uint32_t warps[32];
-    __shared__ int s_bad;
-    pdl_trigger();
-    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = lane_id();
-    for (uint32_t i = tid; i < (p.rows + 31u) / 32u; i += kPlanThreads) bits[i] = 0u;
-    if (tid == 0) s_bad = 0;
-    __syncthreads();
-    int bad = 0;
-    for (uint32_t i = tid; i < n; i += kPlanThreads) {
-        const uint32_t a = (uint32_t)parents[i], c = (uint32_t)children[i];
-        if (a >= p.rows || c >= p.rows || len_bad(p, p.lens[a]) || p.lens[c] != 0) bad = 1;
-        else if ((atomicOr(&bits[c >> 5], 1u << (c & 31u)) >> (c & 31u)) & 1u) bad = 1;
-        else p.extra[i] = p.lens[a];
-    }
-    if (bad) s_bad = 1;
-    __syncthreads();
-    if (s_bad) { finish_plan(p, HBF_E_INVAL, 0u, 0u); return; }
-    // the parents' pages, a parent named several times in a row once: few parents by the whole block, many by a warp each
-    uint32_t runs = 0u;
-    for (uint32_t i = tid; i < n; i += kPlanThreads) runs += i == 0u || parents[i] != parents[i - 1u] ? 1u : 0u;
-    uint32_t all_runs;
-    block_scan(runs, &all_runs, warps);
-    const bool wide = all_runs <= 4u;
-    for (uint32_t i = wide ? 0u : warp; i < n; i += wide ? 1u : kPlanThreads / 32) {
-        if (i && parents[i] == parents[i - 1u]) continue;
-        bad |= row_bad(p, (uint32_t)parents[i], p.extra[i], wide ? tid : lane, wide ? kPlanThreads : 32u);
-    }
-    if (bad) s_bad = 1;
-    // the begun pages in the order of the list
-    uint32_t need = 0u;
-    for (uint32_t i0 = 0; i0 < n; i0 += kPlanThreads) {
-        const uint32_t i = i0 + tid;
-        const int32_t len = i < n ? p.extra[i] : 0;
-        const uint32_t begun = (uint32_t)len % p.page_tokens ? 1u : 0u;
-        uint32_t total;
-        const uint32_t at = need + block_scan(begun, &total, warps);
-        if (begun) {
-            p.src[at] = p.tables[(int64_t)parents[i] * p.table_stride + (uint32_t)len / p.page_tokens];
-            p.extra[n + i] = (int32_t)at;
-        }
-        need += total;
-    }
-    if (s_bad) { finish_plan(p, HBF_E_INVAL, 0u, 0u); return; }
-    // as many free pages, the lowest
-    uint32_t found = 0u;
-    for (uint32_t i0 = 0; i0 < p.n_pages && found < need; i0 += kPlanThreads) {
-        const uint32_t i = i0 + tid;
-        const bool free = i < p.n_pages && p.refs[i] == 0;
-        const unsigned b = __ballot_sync(0xffffffffu, free);
-        if (lane == 0u) warps[warp] = __popc(b);
-        __syncthreads();
-        const uint32_t all = warps[lane];
-        uint32_t s = all;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) { const uint32_t u = __shfl_up_sync(0xffffffffu, s, o); if (lane >= (uint32_t)o) s += u; }
-        const uint32_t at = found + __shfl_sync(0xffffffffu, s - all, warp) + __popc(b & lanemask_lt());
-        if (free && at < need) p.dst[at] = (int32_t)i;
-        found += __shfl_sync(0xffffffffu, s, 31);
-        __syncthreads();
-    }
-    finish_plan(p, found < need ? HBF_E_CAPACITY : HBF_OK, need, 0u);
-}
-
-__global__ void __launch_bounds__(kPlanThreads)
-k_plan_free(const __grid_constant__ PagesDev p, const int32_t *rows, uint32_t n) {
-    extern __shared__ uint32_t bits[];
-    __shared__ int s_bad;
-    pdl_trigger();
-    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = lane_id();
-    for (uint32_t i = tid; i < (p.rows + 31u) / 32u; i += kPlanThreads) bits[i] = 0u;
-    if (tid == 0) s_bad = 0;
-    __syncthreads();
-    int bad = 0;
-    for (uint32_t i = tid; i < n; i += kPlanThreads) {
-        const uint32_t r = (uint32_t)rows[i];
-        if (r >= p.rows || len_bad(p, p.lens[r])) bad = 1;
-        else if ((atomicOr(&bits[r >> 5], 1u << (r & 31u)) >> (r & 31u)) & 1u) bad = 1;
-        else p.extra[i] = p.lens[r];
-    }
-    if (bad) s_bad = 1;
-    __syncthreads();
-    if (!s_bad)
-        for (uint32_t i = warp; i < n; i += kPlanThreads / 32)
-            if (row_bad(p, (uint32_t)rows[i], p.extra[i], lane, 32u)) s_bad = 1;
-    __syncthreads();
-    finish_plan(p, s_bad ? HBF_E_INVAL : HBF_OK, 0u, 0u);
-}
-
-// The k-th page in use behind the first n_live moves into the k-th free one among them.
-__global__ void __launch_bounds__(kPlanThreads)
-k_plan_compact(const __grid_constant__ PagesDev p) {
-    extern __shared__ uint32_t bits[];                       // pages in use
-    __shared__ uint32_t warps[32];
-    pdl_trigger();
-    const uint32_t tid = threadIdx.x, lane = lane_id(), words = (p.n_pages + 31u) / 32u;
-    uint32_t mine = 0u;
-    for (uint32_t w = tid >> 5; w < words; w += kPlanThreads / 32) {
-        const uint32_t i = w * 32u + lane;
-        const unsigned b = __ballot_sync(0xffffffffu, i < p.n_pages && p.refs[i] > 0);
-        if (lane == 0u) { bits[w] = b; mine += __popc(b); }
-    }
-    uint32_t live;
-    block_scan(mine, &live, warps);                          // (its barriers also publish the bits)
-    const uint32_t each = (words + kPlanThreads - 1u) / kPlanThreads, w0 = min(words, tid * each), w1 = min(words, w0 + each);
-    uint32_t holes = 0u, movers = 0u;
-    auto below = [&](uint32_t w) { return w * 32u >= live ? 0u : live - w * 32u >= 32u ? 0xffffffffu : (1u << (live - w * 32u)) - 1u; };
-    for (uint32_t w = w0; w < w1; ++w) { holes += __popc(~bits[w] & below(w)); movers += __popc(bits[w] & ~below(w)); }
-    uint32_t total, moves;
-    uint32_t h = block_scan(holes, &total, warps), m = block_scan(movers, &moves, warps);
-    for (uint32_t w = w0; w < w1; ++w) {
-        for (uint32_t b = ~bits[w] & below(w); b; b &= b - 1u) p.dst[h++] = (int32_t)(w * 32u + __ffs(b) - 1u);
-        for (uint32_t b = bits[w] & ~below(w); b; b &= b - 1u) p.src[m++] = (int32_t)(w * 32u + __ffs(b) - 1u);
-    }
-    __syncthreads();
-    for (uint32_t i = live + tid; i < p.n_pages; i += kPlanThreads) p.extra[i] = -1;
-    __syncthreads();
-    for (uint32_t k = tid; k < moves; k += kPlanThreads) p.extra[p.src[k]] = p.dst[k];
-    finish_plan(p, HBF_OK, moves, live);
-}
-
-enum { kDoCopy = 0, kDoFork = 1, kDoFree = 2, kDoCompact = 3 };
-
-// What the plan found, over the whole device: the rows' tables and the references, then the pages' bytes, a page of a slab a block at a time.
+// Every thread of the plan's block ends with this; with `alone` the block goes on with what the other kernel would do.
+template <int kDo, uint32_t kThreads> __device__ __forceinline__ void apply_plan(const PagesDev &p, const int32_t *a, const int32_t *b, uint32_t n);
 template <int kDo>
-__global__ void __launch_bounds__(kMoveThreads)
-k_pages_apply(const __grid_constant__ PagesDev p, const int32_t *a, const int32_t *b, uint32_t n) {
-    pdl_wait();
+__device__ __forceinline__ void finish_plan(const PagesDev &p, int code, uint32_t moves, uint32_t n_live, const int32_t *a, const int32_t *b, uint32_t n, int alone) {
+    if (threadIdx.x == 0) {
+        const int32_t m = code == HBF_OK ? (int32_t)moves : 0;
+        p.ctrl->code = code; p.ctrl->moves = m; p.ctrl->n_live = (int32_t)n_live;
+        if (p.result) { p.result[0] = code; p.result[1] = m; p.result[2] = (int32_t)n_live; }
+    }
+    if (!alone) return;
+    __syncthreads();                                         // (the moves that other threads wrote are there, too)
+    apply_plan<kDo, kPlanThreads>(p, a, b, n);
+}
+
+
+// What the plan found: the rows' tables and the references, then the pages' bytes, a page of a slab a block at a time.
+template <int kDo, uint32_t kThreads>
+__device__ __forceinline__ void apply_plan(const PagesDev &p, const int32_t *a, const int32_t *b, uint32_t n) {
     const PagesCtrl c = *p.ctrl;
     if (c.code != HBF_OK) return;
     const uint32_t moves = (uint32_t)c.moves;
-    const uint64_t step = (uint64_t)gridDim.x * kMoveThreads, first = (uint64_t)blockIdx.x * kMoveThreads + threadIdx.x;
+    const uint64_t step = (uint64_t)gridDim.x * kThreads, first = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
     if (kDo == kDoFork || kDo == kDoFree) {
         for (uint64_t k = first; k < (uint64_t)n * p.cols; k += step) {
             const uint32_t i = (uint32_t)(k / p.cols), j = (uint32_t)(k - (uint64_t)i * p.cols);
@@ -265,20 +114,187 @@ k_pages_apply(const __grid_constant__ PagesDev p, const int32_t *a, const int32_
         unsigned char *to = p.base + s * p.slab_stride + (uint64_t)p.dst[k] * p.page_stride;
         const uint32_t n16 = (uint32_t)(p.page_bytes / 16u);
         constexpr uint32_t kEach = 4;
-        for (uint32_t i0 = threadIdx.x; i0 < n16; i0 += kMoveThreads * kEach) {
+        for (uint32_t i0 = threadIdx.x; i0 < n16; i0 += kThreads * kEach) {
             uint4 v[kEach];
 #pragma unroll
             for (uint32_t e = 0; e < kEach; ++e) {
-                const uint32_t i = i0 + e * kMoveThreads;
+                const uint32_t i = i0 + e * kThreads;
                 if (i < n16) asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v[e].x), "=r"(v[e].y), "=r"(v[e].z), "=r"(v[e].w) : "l"(from + (uint64_t)i * 16u));
             }
 #pragma unroll
             for (uint32_t e = 0; e < kEach; ++e) {
-                const uint32_t i = i0 + e * kMoveThreads;
+                const uint32_t i = i0 + e * kThreads;
                 if (i < n16) *reinterpret_cast<uint4 *>(to + (uint64_t)i * 16u) = v[e];
             }
         }
     }
+}
+
+template <int kDo>
+__global__ void __launch_bounds__(kMoveThreads)
+k_pages_apply(const __grid_constant__ PagesDev p, const int32_t *a, const int32_t *b, uint32_t n) {
+    pdl_wait();
+    apply_plan<kDo, kMoveThreads>(p, a, b, n);
+}
+
+// The listed pairs are sound if every page exists, no destination is named twice and none is a source too (their order would count).
+__global__ void __launch_bounds__(kPlanThreads)
+k_plan_copy(const __grid_constant__ PagesDev p, const int32_t *src, const int32_t *dst, uint32_t n, int alone) {
+    extern __shared__ uint32_t bits[];
+    pdl_trigger();
+    const uint32_t words = (p.n_pages + 31u) / 32u;
+    for (uint32_t i = threadIdx.x; i < words; i += kPlanThreads) bits[i] = 0u;
+    int bad = 0;
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < n; i += kPlanThreads) {
+        const uint32_t d = (uint32_t)dst[i];
+        if (d >= p.n_pages || (atomicOr(&bits[d >> 5], 1u << (d & 31u)) >> (d & 31u)) & 1u) bad = 1;
+    }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < n; i += kPlanThreads) {
+        const uint32_t s = (uint32_t)src[i];
+        if (s >= p.n_pages || (bits[s >> 5] >> (s & 31u)) & 1u) bad = 1;
+        p.src[i] = (int32_t)s; p.dst[i] = dst[i];
+    }
+    bad = __syncthreads_or(bad);
+    finish_plan<kDoCopy>(p, bad ? HBF_E_INVAL : HBF_OK, n, 0u, src, dst, n, alone);
+}
+
+// A row's entries that count name pages in use.
+__device__ __forceinline__ int row_bad(const PagesDev &p, uint32_t row, int32_t len, uint32_t from, uint32_t step) {
+    int bad = 0;
+    const int32_t *t = p.tables + (int64_t)row * p.table_stride;
+    const uint32_t held = held_pages(p, len);
+#pragma unroll 4
+    for (uint32_t j = from; j < held; j += step) {
+        const uint32_t id = (uint32_t)t[j];
+        if (id >= p.n_pages || p.refs[id] <= 0) bad = 1;
+    }
+    return bad;
+}
+
+// Rows that begin as other rows' tokens: full pages are shared, a begun page is copied into the lowest free one, in the order of the list.
+__global__ void __launch_bounds__(kPlanThreads)
+k_plan_fork(const __grid_constant__ PagesDev p, const int32_t *parents, const int32_t *children, uint32_t n, int alone) {
+    extern __shared__ uint32_t bits[];                       // rows named as children
+    __shared__ uint32_t warps[32];
+    __shared__ int s_bad;
+    pdl_trigger();
+    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = lane_id();
+    for (uint32_t i = tid; i < (p.rows + 31u) / 32u; i += kPlanThreads) bits[i] = 0u;
+    if (tid == 0) s_bad = 0;
+    __syncthreads();
+    int bad = 0;
+    for (uint32_t i = tid; i < n; i += kPlanThreads) {
+        const uint32_t a = (uint32_t)parents[i], c = (uint32_t)children[i];
+        if (a >= p.rows || c >= p.rows || len_bad(p, p.lens[a]) || p.lens[c] != 0) bad = 1;
+        else if ((atomicOr(&bits[c >> 5], 1u << (c & 31u)) >> (c & 31u)) & 1u) bad = 1;
+        else p.extra[i] = p.lens[a];
+    }
+    if (bad) s_bad = 1;
+    __syncthreads();
+    if (s_bad) { finish_plan<kDoFork>(p, HBF_E_INVAL, 0u, 0u, parents, children, n, 0); return; }
+    // the parents' pages, a parent named several times in a row once: few parents by the whole block, many by a warp each
+    uint32_t runs = 0u;
+    for (uint32_t i = tid; i < n; i += kPlanThreads) runs += i == 0u || parents[i] != parents[i - 1u] ? 1u : 0u;
+    uint32_t all_runs;
+    block_scan(runs, &all_runs, warps);
+    const bool wide = all_runs <= 4u;
+    for (uint32_t i = wide ? 0u : warp; i < n; i += wide ? 1u : kPlanThreads / 32) {
+        if (i && parents[i] == parents[i - 1u]) continue;
+        bad |= row_bad(p, (uint32_t)parents[i], p.extra[i], wide ? tid : lane, wide ? kPlanThreads : 32u);
+    }
+    if (bad) s_bad = 1;
+    // the begun pages in the order of the list
+    uint32_t need = 0u;
+    for (uint32_t i0 = 0; i0 < n; i0 += kPlanThreads) {
+        const uint32_t i = i0 + tid;
+        const int32_t len = i < n ? p.extra[i] : 0;
+        const uint32_t begun = (uint32_t)len % p.page_tokens ? 1u : 0u;
+        uint32_t total;
+        const uint32_t at = need + block_scan(begun, &total, warps);
+        if (begun) {
+            p.src[at] = p.tables[(int64_t)parents[i] * p.table_stride + (uint32_t)len / p.page_tokens];
+            p.extra[n + i] = (int32_t)at;
+        }
+        need += total;
+    }
+    if (s_bad) { finish_plan<kDoFork>(p, HBF_E_INVAL, 0u, 0u, parents, children, n, 0); return; }
+    // as many free pages, the lowest
+    uint32_t found = 0u;
+    for (uint32_t i0 = 0; i0 < p.n_pages && found < need; i0 += kPlanThreads) {
+        const uint32_t i = i0 + tid;
+        const bool free = i < p.n_pages && p.refs[i] == 0;
+        const unsigned b = __ballot_sync(0xffffffffu, free);
+        if (lane == 0u) warps[warp] = __popc(b);
+        __syncthreads();
+        const uint32_t all = warps[lane];
+        uint32_t s = all;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) { const uint32_t u = __shfl_up_sync(0xffffffffu, s, o); if (lane >= (uint32_t)o) s += u; }
+        const uint32_t at = found + __shfl_sync(0xffffffffu, s - all, warp) + __popc(b & lanemask_lt());
+        if (free && at < need) p.dst[at] = (int32_t)i;
+        found += __shfl_sync(0xffffffffu, s, 31);
+        __syncthreads();
+    }
+    finish_plan<kDoFork>(p, found < need ? HBF_E_CAPACITY : HBF_OK, need, 0u, parents, children, n, alone);
+}
+
+__global__ void __launch_bounds__(kPlanThreads)
+k_plan_free(const __grid_constant__ PagesDev p, const int32_t *rows, uint32_t n, int alone) {
+    extern __shared__ uint32_t bits[];
+    __shared__ int s_bad;
+    pdl_trigger();
+    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = lane_id();
+    for (uint32_t i = tid; i < (p.rows + 31u) / 32u; i += kPlanThreads) bits[i] = 0u;
+    if (tid == 0) s_bad = 0;
+    __syncthreads();
+    int bad = 0;
+    for (uint32_t i = tid; i < n; i += kPlanThreads) {
+        const uint32_t r = (uint32_t)rows[i];
+        if (r >= p.rows || len_bad(p, p.lens[r])) bad = 1;
+        else if ((atomicOr(&bits[r >> 5], 1u << (r & 31u)) >> (r & 31u)) & 1u) bad = 1;
+        else p.extra[i] = p.lens[r];
+    }
+    if (bad) s_bad = 1;
+    __syncthreads();
+    if (!s_bad)
+        for (uint32_t i = warp; i < n; i += kPlanThreads / 32)
+            if (row_bad(p, (uint32_t)rows[i], p.extra[i], lane, 32u)) s_bad = 1;
+    __syncthreads();
+    finish_plan<kDoFree>(p, s_bad ? HBF_E_INVAL : HBF_OK, 0u, 0u, rows, nullptr, n, alone);
+}
+
+// The k-th page in use behind the first n_live moves into the k-th free one among them.
+__global__ void __launch_bounds__(kPlanThreads)
+k_plan_compact(const __grid_constant__ PagesDev p, int alone) {
+    extern __shared__ uint32_t bits[];                       // pages in use
+    __shared__ uint32_t warps[32];
+    pdl_trigger();
+    const uint32_t tid = threadIdx.x, lane = lane_id(), words = (p.n_pages + 31u) / 32u;
+    uint32_t mine = 0u;
+    for (uint32_t w = tid >> 5; w < words; w += kPlanThreads / 32) {
+        const uint32_t i = w * 32u + lane;
+        const unsigned b = __ballot_sync(0xffffffffu, i < p.n_pages && p.refs[i] > 0);
+        if (lane == 0u) { bits[w] = b; mine += __popc(b); }
+    }
+    uint32_t live;
+    block_scan(mine, &live, warps);                          // (its barriers also publish the bits)
+    const uint32_t each = (words + kPlanThreads - 1u) / kPlanThreads, w0 = min(words, tid * each), w1 = min(words, w0 + each);
+    uint32_t holes = 0u, movers = 0u;
+    auto below = [&](uint32_t w) { return w * 32u >= live ? 0u : live - w * 32u >= 32u ? 0xffffffffu : (1u << (live - w * 32u)) - 1u; };
+    for (uint32_t w = w0; w < w1; ++w) { holes += __popc(~bits[w] & below(w)); movers += __popc(bits[w] & ~below(w)); }
+    uint32_t total, moves;
+    uint32_t h = block_scan(holes, &total, warps), m = block_scan(movers, &moves, warps);
+    for (uint32_t w = w0; w < w1; ++w) {
+        for (uint32_t b = ~bits[w] & below(w); b; b &= b - 1u) p.dst[h++] = (int32_t)(w * 32u + __ffs(b) - 1u);
+        for (uint32_t b = bits[w] & ~below(w); b; b &= b - 1u) p.src[m++] = (int32_t)(w * 32u + __ffs(b) - 1u);
+    }
+    __syncthreads();
+    for (uint32_t i = live + tid; i < p.n_pages; i += kPlanThreads) p.extra[i] = -1;
+    __syncthreads();
+    for (uint32_t k = tid; k < moves; k += kPlanThreads) p.extra[p.src[k]] = p.dst[k];
+    finish_plan<kDoCompact>(p, HBF_OK, moves, live, nullptr, nullptr, 0u, alone);
 }
 
 // The records of the moves of the call before: for each page and slab a read and a program; the places behind them hold records of one byte
@@ -332,7 +348,7 @@ static PagesDev pages_dev(const hbf_pages_t *p, void *ws, int32_t *result) {
 
 // the checks that all four calls share, the plan's launch and the apply kernel's
 template <int kDo, class Plan, class... Args>
-static int pages_call(const hbf_pages_t *p, const int32_t *a, const int32_t *b, uint32_t n, uint64_t work, uint32_t mark_bits, int32_t *result, void *ws, size_t ws_bytes,
+static int pages_call(const hbf_pages_t *p, const int32_t *a, const int32_t *b, uint32_t n, uint64_t work, uint64_t most_moves, uint64_t entries, uint32_t mark_bits, int32_t *result, void *ws, size_t ws_bytes,
                       void *stream, Plan plan, const Args &...args) {
     if ((uintptr_t)result % 4) return HBF_E_INVAL;
     if (!ws || (uintptr_t)ws % 256 || ws_bytes < pages_bytes(p)) return HBF_E_WORKSPACE;
@@ -343,8 +359,12 @@ static int pages_call(const hbf_pages_t *p, const int32_t *a, const int32_t *b, 
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const size_t smem = ((size_t)mark_bits + 31u) / 32u * 4u;
     if (ensure_dyn_smem((const void *)plan, smem) != cudaSuccess) return HBF_E_CUDA;
-    plan<<<1, kPlanThreads, smem, st>>>(d, args...);
+    // without pages to move, and with up to 32 entries a thread, one block is done before a second kernel would have begun (with pages it is
+    // not: three forks of 4 KB pages in four slabs took 14 us, with two kernels 10)
+    const int alone = most_moves == 0u && entries <= 32u * kPlanThreads;
+    plan<<<1, kPlanThreads, smem, st>>>(d, args..., alone);
     if (cudaGetLastError() != cudaSuccess) return HBF_E_CUDA;
+    if (alone) { g_kernel_launches += 1; return HBF_OK; }
     const uint64_t blocks = work < 1 ? 1 : work < 8ull * n_sm ? work : 8ull * n_sm;
     g_kernel_launches += 2;
     return launch_pdl(k_pages_apply<kDo>, (unsigned)blocks, kMoveThreads, 0, st, d, a, b, n) == cudaSuccess ? HBF_OK : HBF_E_CUDA;
@@ -359,26 +379,26 @@ extern "C" size_t hbf_pages_workspace_bytes(const hbf_pages_t *p) { return pages
 extern "C" int hbf_pages_copy(const hbf_pages_t *p, const int32_t *d_src, const int32_t *d_dst, uint32_t n, int32_t *d_result, void *d_workspace,
                               size_t workspace_bytes, void *cuda_stream) {
     if (!pages_ok(p) || n > p->n_pages || (n && (!d_src || !d_dst || (uintptr_t)d_src % 4 || (uintptr_t)d_dst % 4))) return HBF_E_INVAL;
-    return pages_call<kDoCopy>(p, d_src, d_dst, n, (uint64_t)n * p->n_slabs, p->n_pages, d_result, d_workspace, workspace_bytes, cuda_stream, k_plan_copy, d_src, d_dst, n);
+    return pages_call<kDoCopy>(p, d_src, d_dst, n, (uint64_t)n * p->n_slabs, n, 0, p->n_pages, d_result, d_workspace, workspace_bytes, cuda_stream, k_plan_copy, d_src, d_dst, n);
 }
 
 extern "C" int hbf_pages_fork(const hbf_pages_t *p, const int32_t *d_parents, const int32_t *d_children, uint32_t n, int32_t *d_result, void *d_workspace,
                               size_t workspace_bytes, void *cuda_stream) {
     if (!pages_ok(p) || !pages_state_ok(p) || n > p->rows || (n && (!d_parents || !d_children || (uintptr_t)d_parents % 4 || (uintptr_t)d_children % 4))) return HBF_E_INVAL;
     const uint64_t work = (uint64_t)n * p->n_slabs + (uint64_t)n * (p->rows ? p->table_cols : 0u) / kMoveThreads;
-    return pages_call<kDoFork>(p, d_parents, d_children, n, work, p->rows, d_result, d_workspace, workspace_bytes, cuda_stream, k_plan_fork, d_parents, d_children, n);
+    return pages_call<kDoFork>(p, d_parents, d_children, n, work, n, (uint64_t)n * (p->rows ? p->table_cols : 0u), p->rows, d_result, d_workspace, workspace_bytes, cuda_stream, k_plan_fork, d_parents, d_children, n);
 }
 
 extern "C" int hbf_pages_free(const hbf_pages_t *p, const int32_t *d_rows, uint32_t n, int32_t *d_result, void *d_workspace, size_t workspace_bytes,
                               void *cuda_stream) {
     if (!pages_ok(p) || !pages_state_ok(p) || n > p->rows || (n && (!d_rows || (uintptr_t)d_rows % 4))) return HBF_E_INVAL;
     const uint64_t work = ((uint64_t)n * (p->rows ? p->table_cols : 0u) + kMoveThreads - 1) / kMoveThreads;
-    return pages_call<kDoFree>(p, d_rows, nullptr, n, work, p->rows, d_result, d_workspace, workspace_bytes, cuda_stream, k_plan_free, d_rows, n);
+    return pages_call<kDoFree>(p, d_rows, nullptr, n, work, 0, (uint64_t)n * (p->rows ? p->table_cols : 0u), p->rows, d_result, d_workspace, workspace_bytes, cuda_stream, k_plan_free, d_rows, n);
 }
 
 extern "C" int hbf_pages_compact(const hbf_pages_t *p, int32_t *d_result, void *d_workspace, size_t workspace_bytes, void *cuda_stream) {
     if (!pages_ok(p) || !pages_state_ok(p)) return HBF_E_INVAL;
-    return pages_call<kDoCompact>(p, nullptr, nullptr, 0, (uint64_t)p->n_pages * p->n_slabs, p->n_pages, d_result, d_workspace, workspace_bytes, cuda_stream, k_plan_compact);
+    return pages_call<kDoCompact>(p, nullptr, nullptr, 0, (uint64_t)p->n_pages * p->n_slabs, p->n_pages / 2, (uint64_t)p->rows * (p->rows ? p->table_cols : 0u), p->n_pages, d_result, d_workspace, workspace_bytes, cuda_stream, k_plan_compact);
 }
 
 extern "C" int hbf_pages_accesses(const hbf_pages_t *p, const void *d_workspace, int64_t issue_ns, int64_t gap_ns, hbf_access_t *d_acc, uint64_t n, void *cuda_stream) {

@@ -1,26 +1,27 @@
 // The shared prefix for many rows: tiles of 128 query rows (of any requests) against 128 keys at a time on the 5th-generation tensor
 // cores.  For a tile of rows and one of keys: S = Q K^T into tensor memory, weights P = exp2(S - z) from there back into it (over S, in
 // the values' type), O += P V with P read from tensor memory.  A block has two tiles of rows, so that one tile's products run while the
-// other's weights are worked out: 2 x 512 cycles of products for a tile of keys against 1,024 of exponentials, which all
-// eight warps of both tiles share.  The keys are read once for 256 rows; the products bound it from about 64 rows on.
+// other's weights are worked out, and the keys are read once for 256 rows.
 //
-// Warps 0 to 3 and 4 to 7: a row each thread, of the first and the second tile; they take most of the registers, for a row's 128 scores at
-// once.  8 to 11: keys and values from their pages into the swizzled layout that the tensor cores read: a tensor copy for every stretch of
-// slots of a page where pages are multiples of eight slots, else, and in a tile that the prefix ends in (behind its end there must be
-// zeros), 16 bytes a thread at a time, which take 1,150 cycles a tile against the 512 of its products.  12: one thread issues the products.
+// Warps 0 to 7 and 8 to 15: the first and the second tile of rows, two threads a row (the time from a tile's scores to its weights is part of
+// the chain that bounds the kernel: with one thread a row it was 2,700 cycles of 5,000 for a tile of keys).  16 to 19: keys and values from
+// their pages into the swizzled layout that the tensor cores read: a tensor copy for every stretch of slots of a page where pages are
+// multiples of eight slots, else, and in a tile that the prefix ends in (behind its end there must be zeros), 16 bytes a thread at a
+// time, which take 1,150 cycles a tile.  20: one thread issues the products.
 #include <cuda.h>
 
 #include "attention.cuh"
 
 namespace hbf {
 
-constexpr int kPfThreads = 16 * 32, kPfTile = 128, kPfSlots = 4;
+constexpr int kPfThreads = 24 * 32, kPfRowThreads = 16 * 32, kPfTile = 128, kPfSlots = 4;
 constexpr float kPfGrow = 8.0f;                              // sums are scaled again only when a row's maximum has grown by more (in powers of two)
 
 // What lies in shared memory behind the tiles.
 struct PfShared {
     uint64_t kv_full[kPfSlots], kv_empty[kPfSlots], q_full, s_full[2], p_full[2], o_full[2];
     int64_t place[2][kPfTile];                               // offset of each key of a tile; -1: none
+    float other[2][2][kPfTile];                              // what the two threads of a row tell each other
     uint32_t tmem, bad;
 };
 template <int D> constexpr uint32_t kPfTileBytes = kPfTile * D * 2;
@@ -68,9 +69,11 @@ __device__ __forceinline__ void tensor_loaded(uint32_t (&v)[32]) {           // 
 __device__ __forceinline__ void tensor_store16(uint32_t addr, const uint32_t (&v)[16]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr), HBF_I8(v, 0), HBF_I8(v, 8) : "memory");
 }
-__device__ __forceinline__ void tensor_store32(uint32_t addr, const uint32_t (&v)[32]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
-                 ::"r"(addr), HBF_I8(v, 0), HBF_I8(v, 8), HBF_I8(v, 16), HBF_I8(v, 24) : "memory");
+__device__ __forceinline__ void tensor_load16(uint32_t addr, uint32_t (&v)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];" : HBF_R8(v, 0), HBF_R8(v, 8) : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) asm volatile("" : "+r"(v[i]));
 }
 __device__ __forceinline__ void tensor_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -87,25 +90,6 @@ __device__ __forceinline__ uint64_t fma_two(uint64_t a, uint64_t b, uint64_t c) 
 __device__ __forceinline__ uint64_t add_two(uint64_t a, uint64_t b) { uint64_t d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
 __device__ __forceinline__ float max3_nan(float a, float b, float c) { float d; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d; }
 __device__ __forceinline__ float min3_nan(float a, float b, float c) { float d; asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d; }
-// exp2 of two numbers on the multiply-add units, for x <= 100, at least 2^-126: x = n + f, |f| <= 1/2; 2^f by the polynomial of degree 5 with the
-// least largest relative error there (7.5e-8, found by the exchange algorithm of Remez), n added to the exponent.  The exponential unit
-// gives 16 results a cycle and SM, as long for a tile of keys as the products take: every fourth pair goes this way.
-__device__ __forceinline__ void exp2_two(uint64_t x, float &a, float &b) {
-    float x0, x1;
-    of_two(x, x0, x1);
-    x = two_of(fmaxf(x0, -126.0f), fmaxf(x1, -126.0f));
-    const uint64_t r = add_two(x, two_of(12582912.0f, 12582912.0f));         // 1.5 * 2^23: n in the low bits
-    const uint64_t f = add_two(x, fma_two(r, two_of(-1.0f, -1.0f), two_of(12582912.0f, 12582912.0f)));
-    uint64_t y = two_of(0.0013276472454890609f, 0.0013276472454890609f);
-    y = fma_two(y, f, two_of(0.009675540961325169f, 0.009675540961325169f));
-    y = fma_two(y, f, two_of(0.05550713092088699f, 0.05550713092088699f));
-    y = fma_two(y, f, two_of(0.24022120237350464f, 0.24022120237350464f));
-    y = fma_two(y, f, two_of(0.6931469440460205f, 0.6931469440460205f));
-    y = fma_two(y, f, two_of(1.0000001192092896f, 1.0000001192092896f));
-    float r0, r1, y0, y1;
-    of_two(r, r0, r1); of_two(y, y0, y1);
-    a = __uint_as_float(__float_as_uint(y0) + (__float_as_uint(r0) << 23)); b = __uint_as_float(__float_as_uint(y1) + (__float_as_uint(r1) << 23));
-}
 
 template <class Ty, int D, bool kBf16>
 __global__ void __launch_bounds__(kPfThreads, 1)
@@ -127,11 +111,11 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
     if (tid == 0) {
         for (int i = 0; i < kPfSlots; ++i) { bar_init(smem_addr(&sh.kv_full[i]), 128u); bar_init(smem_addr(&sh.kv_empty[i]), 1u); }
         bar_init(smem_addr(&sh.q_full), 128u);
-        for (int t = 0; t < 2; ++t) { bar_init(smem_addr(&sh.s_full[t]), 1u); bar_init(smem_addr(&sh.p_full[t]), 128u); bar_init(smem_addr(&sh.o_full[t]), 1u); }
+        for (int t = 0; t < 2; ++t) { bar_init(smem_addr(&sh.s_full[t]), 1u); bar_init(smem_addr(&sh.p_full[t]), 256u); bar_init(smem_addr(&sh.o_full[t]), 1u); }
         sh.bad = 0u;
         bar_init_done();
     }
-    if (warp == 12u) {
+    if (warp == 20u) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&sh.tmem)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
         tensor_fence_before();
@@ -141,11 +125,11 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
     const uint32_t tmem = sh.tmem;                           // S (and P) of both tiles, then O of both
     bool live = true;
 
-    // the registers that the block was launched with, 128 a thread, as 192 for the weights, 80 for the copies, 48 for the products
-    if (warp >= 8u && warp < 12u) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    // the registers that the block was launched with, 80 a thread, as 96 for the weights, 56 for the copies, 40 for the products
+    if (warp >= 16u && warp < 20u) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         // ---- keys and values: eight lanes a row of 128 bytes
-        const uint32_t t = tid - 256u, col = t & 7u, row = t >> 3;
+        const uint32_t t = tid - (uint32_t)kPfRowThreads, w4 = warp - 16u, col = t & 7u, row = t >> 3;
         auto swizzled = [&](uint32_t r) { return r * 128u + ((col ^ (r & 7u)) * 16u); };
         for (uint32_t h = 0; h < (two ? 2u : 1u); ++h)
 #pragma unroll 1
@@ -170,14 +154,14 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
         };
         auto arrive = [&](uint32_t bar) { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); bar_arrive(bar); };
         // boxes of `box` slots (0: none): whole tiles; warp w takes the boxes w, w + 4, ...
-        const uint32_t whole = box ? (end - begin) / kPfTile : 0u, boxes = box ? kPfTile / box : 0u, my_boxes = boxes > warp - 8u ? (boxes - (warp - 8u) + 3u) / 4u : 0u;
+        const uint32_t whole = box ? (end - begin) / kPfTile : 0u, boxes = box ? kPfTile / box : 0u, my_boxes = boxes > w4 ? (boxes - w4 + 3u) / 4u : 0u;
         if (whole) {
             copy_wait<0>(); arrive(smem_addr(&sh.q_full));
             int32_t page = 0;                                // lane l: that of this warp's box l
             uint32_t slot0 = 0u;
             auto look = [&](uint32_t i) {
                 if (lane >= my_boxes || i >= whole) return;
-                const uint32_t k = begin + i * kPfTile + (warp - 8u + lane * 4u) * box, n = div32(k, p.div_page);
+                const uint32_t k = begin + i * kPfTile + (w4 + lane * 4u) * box, n = div32(k, p.div_page);
                 page = p.prefix_pages[n]; slot0 = k - n * p.page_tokens;
                 if ((uint32_t)page >= p.n_pages) { sh.bad = 1u; page = -1; }              // (such a box is zeros)
             };
@@ -197,7 +181,7 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
                         const int32_t pg = __shfl_sync(0xffffffffu, page_now, j);
                         const int32_t sl = (int32_t)__shfl_sync(0xffffffffu, slot_now, j);
                         if (lane == 0u && live) {
-                            const uint32_t dst = kv_at + slot * kBytes + (warp - 8u + j * 4u) * box * 128u;
+                            const uint32_t dst = kv_at + slot * kBytes + (w4 + j * 4u) * box * 128u;
 #pragma unroll
                             for (int x = 0; x < D / 64; ++x) tensor_copy(dst + x * 16384u, kv ? &v_map : &k_map, x * 64, sl, (int32_t)head, pg, full);
                         }
@@ -232,10 +216,10 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
             copy_wait<1>(); arrive(smem_addr(&sh.kv_full[(2u * n_tiles - 2u) % kPfSlots]));
             copy_wait<0>(); arrive(smem_addr(&sh.kv_full[(2u * n_tiles - 1u) % kPfSlots]));
         }
-    } else if (warp >= 12u) {
+    } else if (warp >= 20u) {
         // ---- the products
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-        if (warp == 12u && lane == 0u) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (warp == 20u && lane == 0u) {
             const uint32_t id_s = product_desc(kBf16, false, 128u, 128u), id_o = product_desc(kBf16, true, 128u, D);
             const uint32_t tiles = two ? 2u : 1u;
             const uint32_t s_full = smem_addr(sh.s_full), o_full = smem_addr(sh.o_full);
@@ -280,140 +264,142 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
         }
         __syncwarp();
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
-        if (warp < 4u || two) {
-        // ---- weights: a row a thread
-        const uint32_t t = warp >> 2, r = tid & 127u;
-        const uint32_t s_at = tmem + t * 128u + (((warp & 3u) * 32u) << 16), o_at = s_at + 256u;
-        const float scale = p.scale_log2, lift = kBf16 ? 0.0f : 7.0f;         // weights are at most 2^8, in fp16 2^15
-        const uint64_t scales = two_of(scale, scale);
-        float m = -INFINITY, l = 0.0f;
-        for (uint32_t i = 0; i < n_tiles; ++i) {
-            live = bar_wait(smem_addr(&sh.s_full[t]), i & 1u, live);
-            __syncwarp();
-            tensor_fence_after();
-            const uint32_t valid = min((uint32_t)kPfTile, end - begin - i * kPfTile);
-            uint32_t v[4][32];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tensor_load(s_at + c * 32u, v[c]);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tensor_loaded(v[c]);
-            if (valid < (uint32_t)kPfTile) {                 // behind the prefix's end: the score that weighs nothing
-#pragma unroll
-                for (int k = 0; k < kPfTile; ++k) if ((uint32_t)k >= valid) v[k / 32][k % 32] = __float_as_uint(scale < 0.0f ? INFINITY : -INFINITY);
-            }
-            float e[4];
-            if (scale >= 0.0f) {
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    e[c] = __uint_as_float(v[c][0]);
-#pragma unroll
-                    for (int k = 1; k < 31; k += 2) e[c] = max3_nan(e[c], __uint_as_float(v[c][k]), __uint_as_float(v[c][k + 1]));
-                    e[c] = max3_nan(e[c], e[c], __uint_as_float(v[c][31]));
-                }
-                e[0] = max3_nan(e[0], e[1], max3_nan(e[2], e[2], e[3]));
-            } else {
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    e[c] = __uint_as_float(v[c][0]);
-#pragma unroll
-                    for (int k = 1; k < 31; k += 2) e[c] = min3_nan(e[c], __uint_as_float(v[c][k]), __uint_as_float(v[c][k + 1]));
-                    e[c] = min3_nan(e[c], e[c], __uint_as_float(v[c][31]));
-                }
-                e[0] = min3_nan(e[0], e[1], min3_nan(e[2], e[2], e[3]));
-            }
-            const float best = e[0] * scale;
-            if (!(best < INFINITY)) l = __int_as_float(0x7fc00000);           // a NaN or an infinity among the scores: the row has no weights
-            const bool grow = m != -INFINITY && best > m + kPfGrow;
-            if (__any_sync(0xffffffffu, grow)) {             // the sums so far, scaled to the new maximum: when the products before are done
-                const float f = grow ? exp2_fast(m - best) : 1.0f;
-                live = bar_wait(smem_addr(&sh.o_full[t]), (i - 1u) & 1u, live);
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
+        const uint32_t t = warp >> 3, half = (warp >> 2) & 1u, r = (warp & 3u) * 32u + lane;
+        if (t == 0u || two) {
+            // ---- weights: half a row a thread
+            constexpr int kHalf = kPfTile / 2;
+            const uint32_t lanes = ((warp & 3u) * 32u) << 16, s_at = tmem + t * 128u + lanes, o_at = tmem + 256u + t * 128u + half * (D / 2) + lanes;
+            const float scale = p.scale_log2, lift = kBf16 ? 0.0f : 7.0f;     // weights are at most 2^8, in fp16 2^15
+            const uint64_t scales = two_of(scale, scale);
+            float m = -INFINITY, l = 0.0f;
+            for (uint32_t i = 0; i < n_tiles; ++i) {
+                live = bar_wait(smem_addr(&sh.s_full[t]), i & 1u, live);
                 __syncwarp();
                 tensor_fence_after();
+                const uint32_t left = min((uint32_t)kPfTile, end - begin - i * kPfTile), valid = left > half * kHalf ? min(left - half * kHalf, (uint32_t)kHalf) : 0u;
+                uint32_t v[2][32];
+                tensor_load(s_at + half * kHalf, v[0]);
+                tensor_load(s_at + half * kHalf + 32u, v[1]);
+                tensor_loaded(v[0]);
+                tensor_loaded(v[1]);
+                if (valid < (uint32_t)kHalf) {               // behind the prefix's end: the score that weighs nothing
+#pragma unroll
+                    for (int k = 0; k < kHalf; ++k) if ((uint32_t)k >= valid) v[k / 32][k % 32] = __float_as_uint(scale < 0.0f ? INFINITY : -INFINITY);
+                }
+                float e[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) e[c] = __uint_as_float(v[c / 2][(c % 2) * 16]);
+                if (scale >= 0.0f) {
+#pragma unroll
+                    for (int k = 1; k < 15; k += 2)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) e[c] = max3_nan(e[c], __uint_as_float(v[c / 2][(c % 2) * 16 + k]), __uint_as_float(v[c / 2][(c % 2) * 16 + k + 1]));
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) e[c] = max3_nan(e[c], e[c], __uint_as_float(v[c / 2][(c % 2) * 16 + 15]));
+                    e[0] = max3_nan(e[0], e[1], max3_nan(e[2], e[2], e[3]));
+                } else {
+#pragma unroll
+                    for (int k = 1; k < 15; k += 2)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) e[c] = min3_nan(e[c], __uint_as_float(v[c / 2][(c % 2) * 16 + k]), __uint_as_float(v[c / 2][(c % 2) * 16 + k + 1]));
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) e[c] = min3_nan(e[c], e[c], __uint_as_float(v[c / 2][(c % 2) * 16 + 15]));
+                    e[0] = min3_nan(e[0], e[1], min3_nan(e[2], e[2], e[3]));
+                }
+                float best = valid ? e[0] * scale : -INFINITY;
+                // (the barrier also says that both halves' scores were read: the weights go over them)
+                sh.other[t][half][r] = best;
+                barrier_of(2u + t, 256u);
+                const float theirs = sh.other[t][half ^ 1u][r];
+                best = max3_nan(best, best, theirs);
+                if (!(best < INFINITY)) l = __int_as_float(0x7fc00000);       // a NaN or an infinity among the scores: the row has no weights
+                const bool grow = m != -INFINITY && best > m + kPfGrow;
+                if (__any_sync(0xffffffffu, grow)) {         // the sums so far, scaled to the new maximum: when the products before are done
+                    const float f = grow ? exp2_fast(m - best) : 1.0f;
+                    live = bar_wait(smem_addr(&sh.o_full[t]), (i - 1u) & 1u, live);
+                    __syncwarp();
+                    tensor_fence_after();
 #pragma unroll 1
-                for (int c = 0; c < D / 32; ++c) {
-                    uint32_t o[32];
-                    tensor_load(o_at + c * 32u, o);
-                    tensor_loaded(o);
+                    for (int c = 0; c < D / 32; ++c) {
+                        uint32_t o[16];
+                        tensor_load16(o_at + c * 16u, o);
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-                    tensor_store32(o_at + c * 32u, o);
-                }
-                l *= f;
-            }
-            if (grow || m == -INFINITY) m = best;
-            const float z = m == -INFINITY ? 0.0f : m - lift;
-            const uint64_t minus_z = two_of(-z, -z);
-            uint64_t sum[2] = {0ull, 0ull};
-            const bool whole = valid == (uint32_t)kPfTile;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t w[16];
-#pragma unroll
-                for (int k = 0; k < 32; k += 2) {
-                    const uint64_t x = fma_two(two_of(__uint_as_float(v[c][k]), __uint_as_float(v[c][k + 1])), scales, minus_z);
-                    float a, b;
-                    if ((k / 2) % 4 == 3) {
-                        exp2_two(x, a, b);
-                    } else {
-                        float x0, x1;
-                        of_two(x, x0, x1);
-                        a = exp2_fast(x0); b = exp2_fast(x1);
+                        for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                        tensor_store16(o_at + c * 16u, o);
                     }
-                    if (!whole) { if (c * 32u + k >= valid) a = 0.0f; if (c * 32u + k + 1u >= valid) b = 0.0f; }
-                    sum[(k / 2) & 1] = add_two(sum[(k / 2) & 1], two_of(a, b));
-                    w[k / 2] = Ty::pack(a, b);
+                    l *= f;
                 }
-                tensor_store16(s_at + c * 16u, w);
-            }
-            float s0, s1;
-            of_two(add_two(sum[0], sum[1]), s0, s1);
-            if (m != -INFINITY) l += s0 + s1;
-            tensor_stored();
-            tensor_fence_before();
-            bar_arrive(smem_addr(&sh.p_full[t]));
-        }
-        live = bar_wait(smem_addr(&sh.o_full[t]), (n_tiles - 1u) & 1u, live);
-        __syncwarp();
-        tensor_fence_after();
-        if (!live || *(volatile uint32_t *)&sh.bad) l = __int_as_float(0x7fc00000);
-        const uint32_t n = row0 + t * kPfTile + r;
-        const bool mine = n < all_rows;
-        const uint32_t b = n / p.G, h = head * p.G + (n - b * p.G);
-        const size_t rows = (size_t)p.B * p.Hq, at = (size_t)(p.own_pieces + piece) * rows + (size_t)b * p.Hq + h;
-        const float z = m - lift, inv = l == 0.0f ? 0.0f : 1.0f / l;
+                if (grow || m == -INFINITY) m = best;
+                const float z = m == -INFINITY ? 0.0f : m - lift;
+                const uint64_t minus_z = two_of(-z, -z);
+                uint64_t sum[2] = {0ull, 0ull};
+                const bool whole = valid == (uint32_t)kHalf;
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-            uint32_t v[32];
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int k = 0; k < 32; k += 2) {
+                        float a, b;
+                        of_two(fma_two(two_of(__uint_as_float(v[c][k]), __uint_as_float(v[c][k + 1])), scales, minus_z), a, b);
+                        a = exp2_fast(a); b = exp2_fast(b);
+                        if (!whole) { if (c * 32u + k >= valid) a = 0.0f; if (c * 32u + k + 1u >= valid) b = 0.0f; }
+                        sum[(k / 2) & 1] = add_two(sum[(k / 2) & 1], two_of(a, b));
+                        w[k / 2] = Ty::pack(a, b);
+                    }
+                    tensor_store16(s_at + half * 32u + c * 16u, w);
+                }
+                float s0, s1;
+                of_two(add_two(sum[0], sum[1]), s0, s1);
+                if (m != -INFINITY) l += s0 + s1;
+                tensor_stored();
+                tensor_fence_before();
+                bar_arrive(smem_addr(&sh.p_full[t]));
+            }
+            live = bar_wait(smem_addr(&sh.o_full[t]), (n_tiles - 1u) & 1u, live);
             __syncwarp();
-            tensor_load(o_at + c * 32u, v);
-            tensor_loaded(v);
-            if (mine && p.pieces == 1u) {
-                uint4 *to = reinterpret_cast<uint4 *>(p.out + (int64_t)b * p.out_row + (int64_t)h * p.out_head + c * 32);
+            tensor_fence_after();
+            if (!live || *(volatile uint32_t *)&sh.bad) l = __int_as_float(0x7fc00000);
+            barrier_of(2u + t, 256u);
+            sh.other[t][half][r] = l;
+            barrier_of(2u + t, 256u);
+            l += sh.other[t][half ^ 1u][r];
+            const uint32_t n = row0 + t * kPfTile + r;
+            const bool mine = n < all_rows;
+            const uint32_t b = n / p.G, h = head * p.G + (n - b * p.G);
+            const size_t rows = (size_t)p.B * p.Hq, at = (size_t)(p.own_pieces + piece) * rows + (size_t)b * p.Hq + h;
+            const float z = m - lift, inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
-                for (int k = 0; k < 32; k += 8) {
-                    uint32_t w[4];
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t v[16];
+                __syncwarp();
+                tensor_load16(o_at + c * 16u, v);
+                if (mine && p.pieces == 1u) {
+                    uint4 *to = reinterpret_cast<uint4 *>(p.out + (int64_t)b * p.out_row + (int64_t)h * p.out_head + half * (D / 2) + c * 16);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = l == 0.0f ? 0u : Ty::pack(__uint_as_float(v[k + 2 * e]) * inv, __uint_as_float(v[k + 2 * e + 1]) * inv);
-                    to[k / 8] = make_uint4(w[0], w[1], w[2], w[3]);
+                    for (int k = 0; k < 16; k += 8) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) w[e] = l == 0.0f ? 0u : Ty::pack(__uint_as_float(v[k + 2 * e]) * inv, __uint_as_float(v[k + 2 * e + 1]) * inv);
+                        to[k / 8] = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                } else if (mine) {
+                    uint4 *to = reinterpret_cast<uint4 *>(p.part_o + at * D + half * (D / 2) + c * 16);
+#pragma unroll
+                    for (int k = 0; k < 16; k += 4) to[k / 4] = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
                 }
-            } else if (mine) {
-                uint4 *to = reinterpret_cast<uint4 *>(p.part_o + at * D + c * 32);
-#pragma unroll
-                for (int k = 0; k < 32; k += 4) to[k / 4] = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
             }
-        }
-        if (mine) {
-            if (p.pieces > 1u) p.part_ml[at] = make_float2(z, l);
-            else if (p.lse) p.lse[(size_t)b * p.Hq + h] = l == 0.0f ? -INFINITY : (z + log2f(l)) * 0.69314718055994531f;
-        }
-        tensor_fence_before();
+            if (mine && half == 0u) {
+                if (p.pieces > 1u) p.part_ml[at] = make_float2(z, l);
+                else if (p.lse) p.lse[(size_t)b * p.Hq + h] = l == 0.0f ? -INFINITY : (z + log2f(l)) * 0.69314718055994531f;
+            }
+            tensor_fence_before();
         }
     }
     pdl_wait();                                              // a kernel behind this one counts on what came before it, too
     __syncthreads();
     __syncwarp();
-    if (warp == 12u) {
+    if (warp == 20u) {
         tensor_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
