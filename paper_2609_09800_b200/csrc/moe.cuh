@@ -1,0 +1,217 @@
+// What the kernels of the mixture-of-experts layer share: the parameters, and the choice of the experts.
+#pragma once
+#include "tensor_ops.cuh"
+
+namespace hbf {
+
+constexpr int kMoeWarps = 16, kMoeThreads = kMoeWarps * 32;
+
+struct MoeDev {
+    uint32_t T, D, I, E, K, renorm;
+    const uint16_t *x; int64_t x_stride;
+    const float *scores; int64_t scores_stride;
+    const uint16_t *experts; int64_t expert_stride;
+    uint16_t *out; int64_t out_stride;
+    int32_t *chosen; float *weights;
+    uint16_t *h_hi, *h_lo;                                   // [pairs by expert, then token][I]
+    uint32_t rows;                                           // of the down product that a block takes, at most 16
+    float *part; uint32_t groups;                            // moe_tiles.cu: [groups][T][D], the sums of a group's experts
+    Div32 div_slices, div_k;                                 // I / 8; K
+};
+
+// What the choice leaves in shared memory, the same in every block that makes it.  An entry is an expert in use with up to `chunk` of its
+// tokens; entries by expert, pairs (expert, token) by entry.
+template <int kTokens>
+struct Route {
+    static constexpr int kWords = (kTokens + 31) / 32, kPairs = kTokens * HBF_MOE_MAX_TOP_K, kEntries = HBF_MOE_MAX_EXPERTS + kPairs / 8;
+    uint32_t mask[HBF_MOE_MAX_EXPERTS][kWords];                      // tokens of each expert
+    uint16_t base[HBF_MOE_MAX_EXPERTS];                              // pairs of the experts before it
+    uint16_t active[HBF_MOE_MAX_EXPERTS];                            // experts in use, ascending
+    uint16_t expert[kEntries], pair0[kEntries];
+    uint8_t count[kEntries];
+    uint8_t token[kPairs];                                           // of each pair
+    float weight[kPairs];
+    uint32_t bad[kWords];                                            // tokens with a NaN among their scores
+    uint32_t n_active, n_entries, scan[kMoeWarps][3];
+};
+template <int kTokens>
+struct RouteTemp {                                                   // of the choice itself; the memory is used again behind it
+    uint16_t expert[kTokens * HBF_MOE_MAX_TOP_K];
+    float weight[kTokens * HBF_MOE_MAX_TOP_K];
+};
+template <int kTokens> constexpr uint32_t kRouteBytes = (sizeof(Route<kTokens>) + 127u) / 128u * 128u;
+
+__device__ __forceinline__ uint32_t ordered(float f) {              // larger scores, larger keys; -inf (never chosen): 0
+    const uint32_t u = __float_as_uint(f + 0.0f);           // (-0 and 0 tie)
+    const uint32_t k = u & 0x80000000u ? ~u : u | 0x80000000u;
+    return f == -INFINITY ? 0u : k;
+}
+__device__ __forceinline__ float from_ordered(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
+__device__ __forceinline__ float warp_sum_f(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// The choice of kTok tokens t0, t0 + step, ... by one warp, kKeys neighbouring scores a lane.  A turn finds the largest score left (the lowest lane
+// that has it, and the lowest of its experts, win a tie); the tokens' turns do not depend on one another, so several of them hide
+// each other's latency.  Left in `tmp`: the chosen experts (0xffff: none left), and their scores' keys as the bits of the weights.
+template <int kKeys, int kTok, int kTokens>
+__device__ __forceinline__ void choose(const MoeDev &m, Route<kTokens> &r, RouteTemp<kTokens> &tmp, uint32_t t0, uint32_t step, bool write) {
+    const uint32_t lane = lane_id();
+    uint32_t key[kTok][kKeys], first[kTok];
+    float all[kTok];
+    bool live[kTok];
+#pragma unroll
+    for (int t = 0; t < kTok; ++t) {
+        const uint32_t tok = t0 + t * step;
+        const float *s = m.scores + (int64_t)tok * m.scores_stride;
+#pragma unroll
+        for (int i = 0; i < kKeys; ++i) {
+            const uint32_t e = lane * kKeys + i;
+            key[t][i] = __float_as_uint(tok < m.T && e < m.E ? s[e] : -INFINITY);
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < kTok; ++t) {
+        bool nan = false;
+#pragma unroll
+        for (int i = 0; i < kKeys; ++i) { const float f = __uint_as_float(key[t][i]); nan |= f != f; key[t][i] = ordered(f); }
+        nan = __any_sync(0xffffffffu, nan);
+        const uint32_t tok = t0 + t * step;
+        live[t] = tok < m.T && !nan;
+        if (nan && lane == 0u) atomicOr(&r.bad[tok >> 5], 1u << (tok & 31u));
+        first[t] = 0u; all[t] = 0.0f;
+        if (tok < m.T && lane < m.K) tmp.expert[tok * m.K + lane] = 0xffffu;
+    }
+    __syncwarp();
+#pragma unroll 1
+    for (uint32_t j = 0; j < m.K; ++j) {
+        uint32_t best[kTok];
+#pragma unroll
+        for (int t = 0; t < kTok; ++t) {
+            best[t] = key[t][0];
+#pragma unroll
+            for (int i = 1; i < kKeys; ++i) best[t] = max(best[t], key[t][i]);
+        }
+#pragma unroll
+        for (int t = 0; t < kTok; ++t) best[t] = __reduce_max_sync(0xffffffffu, best[t]);
+#pragma unroll
+        for (int t = 0; t < kTok; ++t) {
+            if (j == 0u) {
+                first[t] = best[t];
+                if (!m.renorm)
+#pragma unroll
+                    for (int i = 0; i < kKeys; ++i) all[t] += key[t][i] ? expf(from_ordered(key[t][i]) - from_ordered(first[t])) : 0.0f;
+            }
+            uint32_t at = kKeys;
+#pragma unroll
+            for (int i = kKeys - 1; i >= 0; --i) if (key[t][i] == best[t]) at = i;
+            const unsigned has = __ballot_sync(0xffffffffu, at < kKeys);
+            if (live[t] && best[t] && lane == __ffs(has) - 1u) {
+                const uint32_t tok = t0 + t * step, e = lane * kKeys + at;
+                tmp.expert[tok * m.K + j] = (uint16_t)e; tmp.weight[tok * m.K + j] = __uint_as_float(best[t]);
+                atomicOr(&r.mask[e][tok >> 5], 1u << (tok & 31u));
+                if (m.renorm) all[t] += expf(from_ordered(best[t]) - from_ordered(first[t]));
+#pragma unroll
+                for (int i = 0; i < kKeys; ++i) if (i == (int)at) key[t][i] = 0u;
+            }
+        }
+    }
+    __syncwarp();
+#pragma unroll
+    for (int t = 0; t < kTok; ++t) {
+        const uint32_t tok = t0 + t * step, at = tok * m.K + lane;
+        const float sum = warp_sum_f(all[t]);
+        if (tok < m.T && lane < m.K) {
+            const uint32_t e = tmp.expert[at];
+            const float w = e == 0xffffu ? 0.0f : expf(from_ordered(__float_as_uint(tmp.weight[at])) - from_ordered(first[t])) / sum;
+            tmp.weight[at] = w;
+            if (write) {
+                if (m.chosen) m.chosen[at] = e == 0xffffu ? -1 : (int32_t)e;
+                if (m.weights) m.weights[at] = w;
+            }
+        }
+    }
+}
+
+// The whole batch's choice by a block.  Every block of both kernels makes it for itself, which costs less than a kernel of its
+// own in front would.
+template <int kKeys, int kTok, int kTokens>
+__device__ __forceinline__ void route_tokens(const MoeDev &m, Route<kTokens> &r, RouteTemp<kTokens> &tmp, bool write) {
+    constexpr uint32_t kWarps = kMoeWarps;
+#pragma unroll 1
+    for (uint32_t t = threadIdx.x >> 5; t < m.T; t += kWarps * kTok) choose<kKeys, kTok>(m, r, tmp, t, kWarps, write);
+}
+template <int kTokens>
+__device__ __forceinline__ void route(const MoeDev &m, Route<kTokens> &r, RouteTemp<kTokens> &tmp, uint32_t chunk, bool write) {
+    constexpr int kEach = HBF_MOE_MAX_EXPERTS / kMoeThreads, kWords = Route<kTokens>::kWords;  // experts a thread in the scan, side by side
+    const uint32_t tid = threadIdx.x, lane = lane_id(), warp = tid >> 5;
+    for (uint32_t i = tid; i < m.E * kWords; i += kMoeThreads) r.mask[0][i] = 0u;
+    if (tid < kWords) r.bad[tid] = 0u;
+    __syncthreads();
+    if (m.E > 128u) route_tokens<HBF_MOE_MAX_EXPERTS / 32, 1>(m, r, tmp, write);
+    else if (kTokens > kMoeWarps && m.T > kMoeWarps) route_tokens<4, kTokens / kMoeWarps < 4 ? 1 : 4>(m, r, tmp, write);
+    else route_tokens<4, 1>(m, r, tmp, write);
+    __syncthreads();
+    // places of the experts in the list of pairs, of those in use, and of the entries: one scan over the experts
+    uint32_t count[kEach], a0 = 0u, b0 = 0u, c0 = 0u;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const uint32_t e = tid * kEach + i;
+        count[i] = 0u;
+        if (e < m.E) {
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) count[i] += __popc(r.mask[e][w]);
+        }
+        a0 += count[i]; b0 += count[i] ? 1u : 0u; c0 += (count[i] + chunk - 1u) / chunk;
+    }
+    uint32_t a = a0, b = b0, c = c0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t pa = __shfl_up_sync(0xffffffffu, a, o), pb = __shfl_up_sync(0xffffffffu, b, o), pc = __shfl_up_sync(0xffffffffu, c, o);
+        if (lane >= (uint32_t)o) { a += pa; b += pb; c += pc; }
+    }
+    if (lane == 31u) { r.scan[warp][0] = a; r.scan[warp][1] = b; r.scan[warp][2] = c; }
+    __syncthreads();
+#pragma unroll 1
+    for (uint32_t w = 0; w < warp; ++w) { a += r.scan[w][0]; b += r.scan[w][1]; c += r.scan[w][2]; }
+    if (tid == kMoeThreads - 1) { r.n_active = b; r.n_entries = c; }
+    a -= a0; b -= b0; c -= c0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const uint32_t e = tid * kEach + i;
+        if (e >= m.E) break;
+        r.base[e] = (uint16_t)a;
+        if (count[i]) r.active[b++] = (uint16_t)e;
+#pragma unroll 1
+        for (uint32_t k = 0; k < count[i]; k += chunk, ++c) {
+            r.expert[c] = (uint16_t)e; r.pair0[c] = (uint16_t)(a + k); r.count[c] = (uint8_t)min(chunk, count[i] - k);
+        }
+        a += count[i];
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (uint32_t i = tid; i < m.T * m.K; i += kMoeThreads) {
+        const uint32_t e = tmp.expert[i], t = div32(i, m.div_k);
+        if (e == 0xffffu) continue;
+        uint32_t at = r.base[e];
+#pragma unroll
+        for (int w = 0; w < kWords; ++w)
+            at += __popc(r.mask[e][w] & ((uint32_t)w < (t >> 5) ? 0xffffffffu : (uint32_t)w == (t >> 5) ? (1u << (t & 31u)) - 1u : 0u));
+        r.token[at] = (uint8_t)t; r.weight[at] = tmp.weight[i];
+    }
+    __syncthreads();
+}
+static_assert(HBF_MOE_MAX_EXPERTS % kMoeThreads == 0 && HBF_MOE_MAX_TOKENS == 128, "the scan and the masks");
+
+// The layer for more than a few tokens, on tensor memory (moe_tiles.cu).
+cudaError_t launch_moe_tiles(const MoeDev &m, bool bf16, uint32_t n_sm, cudaStream_t st);
+// Blocks that share a tile of 128 rows of the output, each with a part of the experts.
+inline uint32_t moe_groups(uint32_t tokens, uint32_t hidden, uint32_t experts, uint32_t top_k, uint32_t n_sm) {
+    const uint32_t tiles = (hidden + 127u) / 128u, pairs = tokens * top_k, most = pairs < experts + pairs / 32u ? pairs : experts + pairs / 32u;
+    const uint32_t there = tiles < n_sm ? n_sm / tiles : 1u;
+    return there < most ? there : most ? most : 1u;
+}
+
+}  // namespace hbf

@@ -10,209 +10,11 @@
 // is free, so every lane takes 16 consecutive bytes of its row (two steps' worth) from weights and activations alike, and reads back only
 // what it copied itself: no transposition, no barrier in the stream.  (Bulk copies of a row's stretch by a warp of their own, which need fewer
 // instructions, were slower throughout: 64 tokens 556 us against 272, the copies of 0.5 to 1 KB leave the SM one after the other.)
-#include "tensor_ops.cuh"
+#include <type_traits>
+
+#include "moe.cuh"
 
 namespace hbf {
-
-constexpr int kMoeWarps = 16, kMoeThreads = kMoeWarps * 32;
-
-struct MoeDev {
-    uint32_t T, D, I, E, K, renorm;
-    const uint16_t *x; int64_t x_stride;
-    const float *scores; int64_t scores_stride;
-    const uint16_t *experts; int64_t expert_stride;
-    uint16_t *out; int64_t out_stride;
-    int32_t *chosen; float *weights;
-    uint16_t *h_hi, *h_lo;                                   // [pairs by expert, then token][I]
-    uint32_t rows;                                           // of the down product that a block takes, at most 16
-    Div32 div_slices, div_k;                                 // I / 8; K
-};
-
-// What the choice leaves in shared memory, the same in every block that makes it.  An entry is an expert in use with up to `chunk` of its
-// tokens; entries by expert, pairs (expert, token) by entry.
-template <int kTokens>
-struct Route {
-    static constexpr int kWords = (kTokens + 31) / 32, kPairs = kTokens * HBF_MOE_MAX_TOP_K, kEntries = HBF_MOE_MAX_EXPERTS + kPairs / 8;
-    uint32_t mask[HBF_MOE_MAX_EXPERTS][kWords];                      // tokens of each expert
-    uint16_t base[HBF_MOE_MAX_EXPERTS];                              // pairs of the experts before it
-    uint16_t active[HBF_MOE_MAX_EXPERTS];                            // experts in use, ascending
-    uint16_t expert[kEntries], pair0[kEntries];
-    uint8_t count[kEntries];
-    uint8_t token[kPairs];                                           // of each pair
-    float weight[kPairs];
-    uint32_t bad[kWords];                                            // tokens with a NaN among their scores
-    uint32_t n_active, n_entries, scan[kMoeWarps][3];
-};
-template <int kTokens>
-struct RouteTemp {                                                   // of the choice itself; the memory is used again behind it
-    uint16_t expert[kTokens * HBF_MOE_MAX_TOP_K];
-    float weight[kTokens * HBF_MOE_MAX_TOP_K];
-};
-template <int kTokens> constexpr uint32_t kRouteBytes = (sizeof(Route<kTokens>) + 127u) / 128u * 128u;
-
-__device__ __forceinline__ uint32_t ordered(float f) {              // larger scores, larger keys; -inf (never chosen): 0
-    const uint32_t u = __float_as_uint(f + 0.0f);           // (-0 and 0 tie)
-    const uint32_t k = u & 0x80000000u ? ~u : u | 0x80000000u;
-    return f == -INFINITY ? 0u : k;
-}
-__device__ __forceinline__ float from_ordered(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
-__device__ __forceinline__ float warp_sum_f(float v) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
-}
-
-// The choice of kTok tokens t0, t0 + step, ... by one warp, kKeys neighbouring scores a lane.  A turn finds the largest score left (the lowest lane
-// that has it, and the lowest of its experts, win a tie); the tokens' turns do not depend on one another, so several of them hide
-// each other's latency.  Left in `tmp`: the chosen experts (0xffff: none left), and their scores' keys as the bits of the weights.
-template <int kKeys, int kTok, int kTokens>
-__device__ __forceinline__ void choose(const MoeDev &m, Route<kTokens> &r, RouteTemp<kTokens> &tmp, uint32_t t0, uint32_t step, bool write) {
-    const uint32_t lane = lane_id();
-    uint32_t key[kTok][kKeys], first[kTok];
-    float all[kTok];
-    bool live[kTok];
-#pragma unroll
-    for (int t = 0; t < kTok; ++t) {
-        const uint32_t tok = t0 + t * step;
-        const float *s = m.scores + (int64_t)tok * m.scores_stride;
-#pragma unroll
-        for (int i = 0; i < kKeys; ++i) {
-            const uint32_t e = lane * kKeys + i;
-            key[t][i] = __float_as_uint(tok < m.T && e < m.E ? s[e] : -INFINITY);
-        }
-    }
-#pragma unroll
-    for (int t = 0; t < kTok; ++t) {
-        bool nan = false;
-#pragma unroll
-        for (int i = 0; i < kKeys; ++i) { const float f = __uint_as_float(key[t][i]); nan |= f != f; key[t][i] = ordered(f); }
-        nan = __any_sync(0xffffffffu, nan);
-        const uint32_t tok = t0 + t * step;
-        live[t] = tok < m.T && !nan;
-        if (nan && lane == 0u) atomicOr(&r.bad[tok >> 5], 1u << (tok & 31u));
-        first[t] = 0u; all[t] = 0.0f;
-        if (tok < m.T && lane < m.K) tmp.expert[tok * m.K + lane] = 0xffffu;
-    }
-    __syncwarp();
-#pragma unroll 1
-    for (uint32_t j = 0; j < m.K; ++j) {
-        uint32_t best[kTok];
-#pragma unroll
-        for (int t = 0; t < kTok; ++t) {
-            best[t] = key[t][0];
-#pragma unroll
-            for (int i = 1; i < kKeys; ++i) best[t] = max(best[t], key[t][i]);
-        }
-#pragma unroll
-        for (int t = 0; t < kTok; ++t) best[t] = __reduce_max_sync(0xffffffffu, best[t]);
-#pragma unroll
-        for (int t = 0; t < kTok; ++t) {
-            if (j == 0u) {
-                first[t] = best[t];
-                if (!m.renorm)
-#pragma unroll
-                    for (int i = 0; i < kKeys; ++i) all[t] += key[t][i] ? expf(from_ordered(key[t][i]) - from_ordered(first[t])) : 0.0f;
-            }
-            uint32_t at = kKeys;
-#pragma unroll
-            for (int i = kKeys - 1; i >= 0; --i) if (key[t][i] == best[t]) at = i;
-            const unsigned has = __ballot_sync(0xffffffffu, at < kKeys);
-            if (live[t] && best[t] && lane == __ffs(has) - 1u) {
-                const uint32_t tok = t0 + t * step, e = lane * kKeys + at;
-                tmp.expert[tok * m.K + j] = (uint16_t)e; tmp.weight[tok * m.K + j] = __uint_as_float(best[t]);
-                atomicOr(&r.mask[e][tok >> 5], 1u << (tok & 31u));
-                if (m.renorm) all[t] += expf(from_ordered(best[t]) - from_ordered(first[t]));
-#pragma unroll
-                for (int i = 0; i < kKeys; ++i) if (i == (int)at) key[t][i] = 0u;
-            }
-        }
-    }
-    __syncwarp();
-#pragma unroll
-    for (int t = 0; t < kTok; ++t) {
-        const uint32_t tok = t0 + t * step, at = tok * m.K + lane;
-        const float sum = warp_sum_f(all[t]);
-        if (tok < m.T && lane < m.K) {
-            const uint32_t e = tmp.expert[at];
-            const float w = e == 0xffffu ? 0.0f : expf(from_ordered(__float_as_uint(tmp.weight[at])) - from_ordered(first[t])) / sum;
-            tmp.weight[at] = w;
-            if (write) {
-                if (m.chosen) m.chosen[at] = e == 0xffffu ? -1 : (int32_t)e;
-                if (m.weights) m.weights[at] = w;
-            }
-        }
-    }
-}
-
-// The whole batch's choice by a block.  Every block of both kernels makes it for itself, which costs less than a kernel of its
-// own in front would.
-template <int kKeys, int kTok, int kTokens>
-__device__ __forceinline__ void route_tokens(const MoeDev &m, Route<kTokens> &r, RouteTemp<kTokens> &tmp, bool write) {
-    constexpr uint32_t kWarps = kMoeWarps;
-#pragma unroll 1
-    for (uint32_t t = threadIdx.x >> 5; t < m.T; t += kWarps * kTok) choose<kKeys, kTok>(m, r, tmp, t, kWarps, write);
-}
-template <int kTokens>
-__device__ __forceinline__ void route(const MoeDev &m, Route<kTokens> &r, RouteTemp<kTokens> &tmp, uint32_t chunk, bool write) {
-    constexpr int kEach = HBF_MOE_MAX_EXPERTS / kMoeThreads, kWords = Route<kTokens>::kWords;  // experts a thread in the scan, side by side
-    const uint32_t tid = threadIdx.x, lane = lane_id(), warp = tid >> 5;
-    for (uint32_t i = tid; i < m.E * kWords; i += kMoeThreads) r.mask[0][i] = 0u;
-    if (tid < kWords) r.bad[tid] = 0u;
-    __syncthreads();
-    if (m.E > 128u) route_tokens<HBF_MOE_MAX_EXPERTS / 32, 1>(m, r, tmp, write);
-    else if (kTokens > kMoeWarps && m.T > kMoeWarps) route_tokens<4, kTokens / kMoeWarps < 4 ? 1 : 4>(m, r, tmp, write);
-    else route_tokens<4, 1>(m, r, tmp, write);
-    __syncthreads();
-    // places of the experts in the list of pairs, of those in use, and of the entries: one scan over the experts
-    uint32_t count[kEach], a0 = 0u, b0 = 0u, c0 = 0u;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const uint32_t e = tid * kEach + i;
-        count[i] = 0u;
-        if (e < m.E) {
-#pragma unroll
-            for (int w = 0; w < kWords; ++w) count[i] += __popc(r.mask[e][w]);
-        }
-        a0 += count[i]; b0 += count[i] ? 1u : 0u; c0 += (count[i] + chunk - 1u) / chunk;
-    }
-    uint32_t a = a0, b = b0, c = c0;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t pa = __shfl_up_sync(0xffffffffu, a, o), pb = __shfl_up_sync(0xffffffffu, b, o), pc = __shfl_up_sync(0xffffffffu, c, o);
-        if (lane >= (uint32_t)o) { a += pa; b += pb; c += pc; }
-    }
-    if (lane == 31u) { r.scan[warp][0] = a; r.scan[warp][1] = b; r.scan[warp][2] = c; }
-    __syncthreads();
-#pragma unroll 1
-    for (uint32_t w = 0; w < warp; ++w) { a += r.scan[w][0]; b += r.scan[w][1]; c += r.scan[w][2]; }
-    if (tid == kMoeThreads - 1) { r.n_active = b; r.n_entries = c; }
-    a -= a0; b -= b0; c -= c0;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const uint32_t e = tid * kEach + i;
-        if (e >= m.E) break;
-        r.base[e] = (uint16_t)a;
-        if (count[i]) r.active[b++] = (uint16_t)e;
-#pragma unroll 1
-        for (uint32_t k = 0; k < count[i]; k += chunk, ++c) {
-            r.expert[c] = (uint16_t)e; r.pair0[c] = (uint16_t)(a + k); r.count[c] = (uint8_t)min(chunk, count[i] - k);
-        }
-        a += count[i];
-    }
-    __syncthreads();
-#pragma unroll 1
-    for (uint32_t i = tid; i < m.T * m.K; i += kMoeThreads) {
-        const uint32_t e = tmp.expert[i], t = div32(i, m.div_k);
-        if (e == 0xffffu) continue;
-        uint32_t at = r.base[e];
-#pragma unroll
-        for (int w = 0; w < kWords; ++w)
-            at += __popc(r.mask[e][w] & ((uint32_t)w < (t >> 5) ? 0xffffffffu : (uint32_t)w == (t >> 5) ? (1u << (t & 31u)) - 1u : 0u));
-        r.token[at] = (uint8_t)t; r.weight[at] = tmp.weight[i];
-    }
-    __syncthreads();
-}
-static_assert(HBF_MOE_MAX_EXPERTS % kMoeThreads == 0 && HBF_MOE_MAX_TOKENS == 128, "the scan and the masks");
 
 // Sixteen warps' sums of a 16 x 8 n product, left as they lie in the accumulators: eight lanes for a column of the pile, two warps' parts
 // each, always in the same order.  f(tile, lane of the accumulator, its four sums) is called once for every column.
@@ -520,6 +322,19 @@ static bool moe_pointers_ok(const hbf_moe_t *m) {
     if (!m->scores || !m->experts || (uintptr_t)m->experts % 16 || (uintptr_t)m->scores % 4 || m->scores_stride < (int64_t)m->n_experts) return false;
     return true;
 }
+// Tokens up to which the weights are read from registers' side (k_moe_up, k_moe_down).
+constexpr uint32_t kMoeFew = 8;
+// The activations between the products, and past a few tokens the parts' sums; 0: the device cannot be asked.
+static size_t moe_bytes(const hbf_moe_t *m, uint32_t *groups) {
+    const size_t h = ((size_t)m->tokens * m->top_k * m->inter * 4u + 255u) / 256u * 256u;
+    if (groups) *groups = 1u;
+    if (m->tokens <= kMoeFew) return h;
+    uint32_t n_sm = 0;
+    if (sm_count(&n_sm) != HBF_OK) return 0;
+    const uint32_t g = moe_groups(m->tokens, m->hidden, m->n_experts, m->top_k, n_sm);
+    if (groups) *groups = g;
+    return h + ((size_t)g * m->tokens * m->hidden * 4u + 255u) / 256u * 256u;
+}
 static MoeDev moe_dev(const hbf_moe_t *m) {
     MoeDev d = {};
     d.T = m->tokens; d.D = m->hidden; d.I = m->inter; d.E = m->n_experts; d.K = m->top_k; d.renorm = m->renormalise;
@@ -557,10 +372,8 @@ static cudaError_t launch_moe(MoeDev d, uint32_t n_sm, cudaStream_t st) {
     // an even share of the output's rows to every SM, 16 at most: 2,048 rows are 14 a block on 147 blocks
     const uint32_t rounds = (d.D + 16u * n_sm - 1u) / (16u * n_sm);
     d.rows = (d.D + rounds * n_sm - 1u) / (rounds * n_sm);
-    if (d.T <= 8u) return launch_moe_as<Ty, 1, 8, 5, 4, 1, 2>(d, n_sm, st);
-    if (d.T <= 64u && d.T * d.K <= 16u * d.E) return launch_moe_as<Ty, 2, 64, 8, 4, 2, 1>(d, n_sm, st);
-    if (d.T * d.K <= 16u * d.E) return launch_moe_as<Ty, 2, HBF_MOE_MAX_TOKENS, 8, 2, 2, 1>(d, n_sm, st);
-    return launch_moe_as<Ty, 4, HBF_MOE_MAX_TOKENS, 8, 4, 1, 1>(d, n_sm, st);
+    if (d.T <= kMoeFew) return launch_moe_as<Ty, 1, 8, 5, 4, 1, 2>(d, n_sm, st);
+    return launch_moe_tiles(d, std::is_same<Ty, Bf16>::value, n_sm, st);
 }
 
 }  // namespace hbf
@@ -569,7 +382,7 @@ using namespace hbf;
 
 extern "C" size_t hbf_moe_workspace_bytes(const hbf_moe_t *m) {
     if (!moe_ok(m)) return 0;
-    return ((size_t)m->tokens * m->top_k * m->inter * 4u + 255u) / 256u * 256u;
+    return moe_bytes(m, nullptr);
 }
 
 extern "C" int hbf_moe_layer(const hbf_moe_t *m, void *d_workspace, size_t workspace_bytes, void *cuda_stream) {
@@ -577,12 +390,17 @@ extern "C" int hbf_moe_layer(const hbf_moe_t *m, void *d_workspace, size_t works
     if (m->tokens == 0) return HBF_OK;
     if (!moe_pointers_ok(m) || !m->x || !m->out || (uintptr_t)m->x % 16 || (uintptr_t)m->out % 2 || m->x_stride % 8) return HBF_E_INVAL;
     if (m->x_stride < (int64_t)m->hidden || m->out_stride < (int64_t)m->hidden) return HBF_E_INVAL;
-    if (!d_workspace || (uintptr_t)d_workspace % 256 || workspace_bytes < hbf_moe_workspace_bytes(m)) return HBF_E_WORKSPACE;
+    if (!d_workspace || (uintptr_t)d_workspace % 256) return HBF_E_WORKSPACE;
     uint32_t n_sm = 0;
+    MoeDev d = moe_dev(m);
+    const size_t need = moe_bytes(m, &d.groups);
+    if (need == 0) return HBF_E_CUDA;
+    if (workspace_bytes < need) return HBF_E_WORKSPACE;
     const int rc = device_of(m->experts, &n_sm);
     if (rc != HBF_OK) return rc;
-    MoeDev d = moe_dev(m);
-    d.h_hi = static_cast<uint16_t *>(d_workspace); d.h_lo = d.h_hi + (size_t)m->tokens * m->top_k * m->inter;
+    const size_t pairs = (size_t)m->tokens * m->top_k;
+    d.h_hi = static_cast<uint16_t *>(d_workspace); d.h_lo = d.h_hi + pairs * m->inter;
+    d.part = reinterpret_cast<float *>(static_cast<unsigned char *>(d_workspace) + (pairs * m->inter * 4u + 255u) / 256u * 256u);
     const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     return (m->dtype == HBF_BF16 ? launch_moe<Bf16>(d, n_sm, st) : launch_moe<Fp16>(d, n_sm, st)) == cudaSuccess ? HBF_OK : HBF_E_CUDA;
 }

@@ -1,0 +1,333 @@
+// The mixture-of-experts layer for more than a few tokens.  With many experts in use the layer is bound by their bytes, and what counts is that
+// nothing but the copies stands between HBM and the products: weights go by tensor copies into the swizzled layout that the 5th-generation
+// tensor cores read, and 128 rows of them against 16 or 32 tokens are products into tensor memory that one thread issues.  (With m16n8k16
+// products fed from registers, as moe_kernels.cu does for a few tokens, instructions bound it: 64 tokens, 837 MB of weights, 257 us.)
+//
+//   k_moe_up_tiles    up to 64 gate rows and the same up rows of an expert in use, times its tokens: h = w silu(gate) up
+//   k_moe_down_tiles  128 rows of the output for all tokens, from a part of the experts: their sums, in the experts' order
+//   k_moe_sum         the parts' sums, in their order
+#include "moe.cuh"
+#include "tensor_memory.cuh"
+
+namespace hbf {
+
+constexpr int kMtTokens = HBF_MOE_MAX_TOKENS, kMtChunk = 32;             // tokens of an expert that an entry takes
+constexpr uint32_t kMtA = 128u * 128u, kMtB = kMtChunk * 128u;           // bytes of a stage, 64 of the sum's places: weights; activations
+constexpr int kUpStages = 8, kDownStages = 5, kMtLag = 3;
+constexpr uint32_t kUpStageBytes = kMtA + kMtB, kDownStageBytes = kMtA + 2u * kMtB;
+
+struct MtShared {
+    Route<kMtTokens> route;
+    uint64_t full[kUpStages], empty[kUpStages], acc_full[2], acc_empty[2];
+    uint32_t tmem;
+};
+constexpr uint32_t kUpTilesSmem = 1024u + kUpStages * kUpStageBytes + 2u * kMtChunk * 64u * 4u + sizeof(MtShared);
+constexpr uint32_t down_tiles_smem(uint32_t tokens) { return 1024u + kDownStages * kDownStageBytes + tokens * 512u + sizeof(MtShared); }
+static_assert(kUpTilesSmem <= 227 * 1024 && down_tiles_smem(kMtTokens) <= 227 * 1024 && sizeof(RouteTemp<kMtTokens>) <= kDownStages * kDownStageBytes, "shared memory");
+
+__device__ __forceinline__ void tensor_copy3(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, int32_t z, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+
+// Both kernels' blocks begin alike: barriers, tensor memory (two times 32 columns), the choice.  Warps 0 to 3: a lane of tensor memory a thread;
+// 4 to 7: the activations' 16-byte copies; 8: tensor copies; 9: products; all 16 make the choice.
+template <int kStages>
+__device__ __forceinline__ void begin_tiles(const MoeDev &m, MtShared &sh, unsigned char *tmp, bool write) {
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) { bar_init(smem_addr(&sh.full[i]), 129u); bar_init(smem_addr(&sh.empty[i]), 1u); }
+        for (int i = 0; i < 2; ++i) { bar_init(smem_addr(&sh.acc_full[i]), 1u); bar_init(smem_addr(&sh.acc_empty[i]), 128u); }
+        bar_init_done();
+    }
+    if ((threadIdx.x >> 5) == 9u) { tensor_alloc(smem_addr(&sh.tmem), 64u); tensor_fence_before(); }
+    route(m, sh.route, *reinterpret_cast<RouteTemp<kMtTokens> *>(tmp), kMtChunk, write);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");         // the choice's memory is the ring's now
+    __syncthreads();
+    tensor_fence_after();
+}
+__device__ __forceinline__ void end_tiles(const MtShared &sh) {
+    tensor_fence_before();
+    __syncthreads();
+    if ((threadIdx.x >> 5) == 9u) { __syncwarp(); tensor_fence_after(); tensor_free(sh.tmem, 64u); }
+}
+
+// The activations' side of a ring: stage g's copies are issued by `copy(stage address)`; they are said to be there kMtLag stages later, and before
+// a wait for a free stage.
+template <int kStages, uint32_t kBytes>
+struct Gather {
+    uint32_t ring, full, empty, g = 0u;
+    bool live = true;
+    __device__ __forceinline__ void tell(uint32_t n) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        bar_arrive(full + (n % kStages) * 8u);
+    }
+    template <class F> __device__ __forceinline__ void stage(F copy) {
+        if (g >= (uint32_t)kMtLag) { copy_wait<kMtLag - 1>(); tell(g - kMtLag); }
+        live = bar_wait(empty + (g % kStages) * 8u, ((g / kStages) & 1u) ^ 1u, live);
+        copy(ring + (g % kStages) * kBytes + kMtA);
+        copy_commit();
+        ++g;
+    }
+    __device__ __forceinline__ void finish() {
+        copy_wait<0>();
+        for (uint32_t n = g > (uint32_t)kMtLag ? g - kMtLag : 0u; n < g; ++n) tell(n);
+    }
+};
+
+template <class Ty, bool kBf16>
+__global__ void __launch_bounds__(kMoeThreads, 1)
+k_moe_up_tiles(const __grid_constant__ MoeDev m, const __grid_constant__ CUtensorMap w_map) {
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char *smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+    const uint32_t ring = smem_addr(smem);
+    float *ex = reinterpret_cast<float *>(smem + kUpStages * kUpStageBytes);                // [2][token][64]: the up rows' sums
+    MtShared &sh = *reinterpret_cast<MtShared *>(smem + kUpStages * kUpStageBytes + 2u * kMtChunk * 64u * 4u);
+    const Route<kMtTokens> &r = sh.route;
+    const uint32_t tid = threadIdx.x, lane = lane_id(), warp = tid >> 5;
+    pdl_trigger();
+    begin_tiles<kUpStages>(m, sh, smem, blockIdx.x == 0);
+    // rows of gate and up that an item takes: of 64, 48 and 32 those with which the blocks are done first
+    uint32_t rows = 64u, best = 0xffffffffu;
+#pragma unroll
+    for (uint32_t c = 64u; c >= 32u; c -= 16u) {
+        const uint32_t items = r.n_entries * ((m.I + c - 1u) / c), cost = (items + gridDim.x - 1u) / gridDim.x * c;
+        if (cost < best) { best = cost; rows = c; }
+    }
+    const uint32_t tiles = (m.I + rows - 1u) / rows, n_items = r.n_entries * tiles, chunks = (m.D + 63u) / 64u;
+    const uint32_t full = smem_addr(sh.full), empty = smem_addr(sh.empty), acc_full = smem_addr(sh.acc_full), acc_empty = smem_addr(sh.acc_empty);
+    bool live = true;
+    if (warp == 8u) {
+        if (lane == 0u) {
+            uint32_t g = 0u;
+            for (uint32_t item = blockIdx.x; item < n_items; item += gridDim.x) {
+                const uint32_t en = item / tiles, i0 = (item - en * tiles) * rows, e = r.expert[en];
+                for (uint32_t c = 0; c < chunks; ++c, ++g) {
+                    const uint32_t s = g % kUpStages, at = ring + s * kUpStageBytes, bar = full + s * 8u;
+                    live = bar_wait(empty + s * 8u, ((g / kUpStages) & 1u) ^ 1u, live);
+                    bar_arrive_bytes(bar, live ? rows * 256u : 0u);
+                    if (live)
+                        for (uint32_t b = 0; b < rows; b += 16u) {
+                            tensor_copy3(at + b * 128u, &w_map, (int32_t)(c * 64u), (int32_t)(i0 + b), (int32_t)e, bar);
+                            tensor_copy3(at + 8192u + b * 128u, &w_map, (int32_t)(c * 64u), (int32_t)(m.I + i0 + b), (int32_t)e, bar);
+                        }
+                }
+            }
+        }
+    } else if (warp >= 4u && warp < 8u) {
+        const uint32_t t = tid - 128u, col = t & 7u, row = t >> 3, to = row * 128u + ((col ^ (row & 7u)) * 16u);
+        Gather<kUpStages, kUpStageBytes> in{ring, full, empty};
+        for (uint32_t item = blockIdx.x; item < n_items; item += gridDim.x) {
+            const uint32_t en = item / tiles, n = r.count[en], pair0 = r.pair0[en];
+            const uint16_t *x0 = row < n ? m.x + (int64_t)r.token[pair0 + row] * m.x_stride : nullptr;
+            const uint16_t *x1 = row + 16u < n ? m.x + (int64_t)r.token[pair0 + row + 16u] * m.x_stride : nullptr;
+            for (uint32_t c = 0; c < chunks; ++c)
+                in.stage([&](uint32_t at) {
+                    const uint32_t k = c * 64u + col * 8u;
+                    const bool is = k < m.D;
+                    if (x0) copy_async16_shared(at + to, is ? x0 + k : m.x, is);
+                    if (x1) copy_async16_shared(at + 2048u + to, is ? x1 + k : m.x, is);
+                });
+        }
+        in.finish();
+    } else if (warp == 9u) {
+        if (lane == 0u) {
+            uint32_t g = 0u, it = 0u;
+            const TileDesc a0(ring, 16u, 1024u), b0(ring + kMtA, 16u, 1024u);
+            for (uint32_t item = blockIdx.x; item < n_items; item += gridDim.x, ++it) {
+                const uint32_t n = r.count[item / tiles], buf = it & 1u, id = product_desc(kBf16, false, 128u, n <= 16u ? 16u : 32u);
+                live = bar_wait(acc_empty + buf * 8u, ((it >> 1) & 1u) ^ 1u, live);
+                tensor_fence_after();
+                for (uint32_t c = 0; c < chunks; ++c, ++g) {
+                    const uint32_t s = g % kUpStages;
+                    live = bar_wait(full + s * 8u, (g / kUpStages) & 1u, live);
+                    tensor_fence_after();
+                    TileDesc a = a0, b = b0;
+                    a.lo += s * (kUpStageBytes >> 4); b.lo += s * (kUpStageBytes >> 4);
+#pragma unroll
+                    for (uint32_t k = 0; k < 4u; ++k) product_ss(sh.tmem + buf * 32u, a.at(k * 32u), b.at(k * 32u), id, c || k ? 1u : 0u);
+                    products_arrive(empty + s * 8u);
+                }
+                products_arrive(acc_full + buf * 8u);
+            }
+        }
+        __syncwarp();
+    } else if (warp < 4u) {
+        uint32_t it = 0u;
+        for (uint32_t item = blockIdx.x; item < n_items; item += gridDim.x, ++it) {
+            const uint32_t en = item / tiles, i0 = (item - en * tiles) * rows, n = r.count[en], pair0 = r.pair0[en], buf = it & 1u;
+            live = bar_wait(acc_full + buf * 8u, (it >> 1) & 1u, live);
+            __syncwarp();
+            tensor_fence_after();
+            uint32_t v[32];
+            tensor_load(sh.tmem + buf * 32u + ((warp * 32u) << 16), v);   // (columns past the tokens hold anything)
+            tensor_loaded(v);
+            tensor_fence_before();
+            bar_arrive(acc_empty + buf * 8u);
+            float *up = ex + buf * (kMtChunk * 64u);
+            const uint32_t row = (warp & 1u) * 32u + lane;
+            if (warp >= 2u) {
+#pragma unroll
+                for (int c = 0; c < kMtChunk; ++c) if ((uint32_t)c < n) up[c * 64 + row] = __uint_as_float(v[c]);
+            }
+            barrier_of(1, 128);                              // (the buffer after next is written behind the next one's barrier)
+            if (warp < 2u && row < rows && i0 + row < m.I) {
+#pragma unroll
+                for (int c = 0; c < kMtChunk; ++c)
+                    if ((uint32_t)c < n) {
+                        const float g = __uint_as_float(v[c]), u = up[c * 64 + row];
+                        const float h = live ? r.weight[pair0 + c] * (g / (1.0f + expf(-g)) * u) : __int_as_float(0x7fc00000);
+                        // (held as the sum of two numbers: see k_moe_up)
+                        const typename Ty::type hi = Ty::from(h), lo = Ty::from(isfinite(h) ? h - Ty::to(hi) : 0.0f);
+                        const size_t at = (size_t)(pair0 + c) * m.I + i0 + row;
+                        reinterpret_cast<typename Ty::type *>(m.h_hi)[at] = hi;
+                        reinterpret_cast<typename Ty::type *>(m.h_lo)[at] = isfinite(Ty::to(hi)) ? lo : Ty::from(0.0f);
+                    }
+            }
+        }
+    }
+    end_tiles(sh);
+}
+
+template <class Ty, bool kBf16>
+__global__ void __launch_bounds__(kMoeThreads, 1)
+k_moe_down_tiles(const __grid_constant__ MoeDev m, const __grid_constant__ CUtensorMap w_map) {
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char *smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+    const uint32_t ring = smem_addr(smem);
+    float *sums = reinterpret_cast<float *>(smem + kDownStages * kDownStageBytes);          // [token][128]
+    MtShared &sh = *reinterpret_cast<MtShared *>(smem + kDownStages * kDownStageBytes + m.T * 512u);
+    const Route<kMtTokens> &r = sh.route;
+    const uint32_t tid = threadIdx.x, lane = lane_id(), warp = tid >> 5;
+    pdl_trigger();
+    begin_tiles<kDownStages>(m, sh, smem, false);
+    const uint32_t d_tiles = (m.D + 127u) / 128u, group = blockIdx.x / d_tiles, d0 = (blockIdx.x - group * d_tiles) * 128u, chunks = (m.I + 63u) / 64u;
+    const uint32_t en0 = r.n_entries * group / m.groups, en1 = r.n_entries * (group + 1u) / m.groups;
+    const uint32_t full = smem_addr(sh.full), empty = smem_addr(sh.empty), acc_full = smem_addr(sh.acc_full), acc_empty = smem_addr(sh.acc_empty);
+    bool live = true;
+    if (warp == 8u) {                                        // weights: as far ahead as the ring goes while the kernel before still runs
+        if (lane == 0u) {
+            uint32_t g = 0u;
+            for (uint32_t en = en0; en < en1; ++en)
+                for (uint32_t c = 0; c < chunks; ++c, ++g) {
+                    const uint32_t s = g % kDownStages, bar = full + s * 8u;
+                    live = bar_wait(empty + s * 8u, ((g / kDownStages) & 1u) ^ 1u, live);
+                    bar_arrive_bytes(bar, live ? kMtA : 0u);
+                    if (live) tensor_copy3(ring + s * kDownStageBytes, &w_map, (int32_t)(c * 64u), (int32_t)d0, (int32_t)r.expert[en], bar);
+                }
+        }
+    } else if (warp >= 4u && warp < 8u) {
+        const uint32_t t = tid - 128u, col = t & 7u, row = t >> 3, to = row * 128u + ((col ^ (row & 7u)) * 16u);
+        Gather<kDownStages, kDownStageBytes> in{ring, full, empty};
+        pdl_wait();
+        for (uint32_t en = en0; en < en1; ++en) {
+            const uint32_t n = r.count[en], pair0 = r.pair0[en];
+            const size_t h0 = (size_t)(pair0 + row) * m.I, h1 = (size_t)(pair0 + row + 16u) * m.I;
+            const bool is0 = row < n, is1 = row + 16u < n;
+            for (uint32_t c = 0; c < chunks; ++c)
+                in.stage([&](uint32_t at) {
+                    const uint32_t k = c * 64u + col * 8u;
+                    const bool is = k < m.I;
+                    const size_t a = is ? h0 + k : 0u, b = is ? h1 + k : 0u;
+                    if (is0) { copy_async16(at + to, m.h_hi + a, is); copy_async16(at + kMtB + to, m.h_lo + a, is); }
+                    if (is1) { copy_async16(at + 2048u + to, m.h_hi + b, is); copy_async16(at + kMtB + 2048u + to, m.h_lo + b, is); }
+                });
+        }
+        in.finish();
+    } else if (warp == 9u) {
+        if (lane == 0u) {
+            uint32_t g = 0u, it = 0u;
+            const TileDesc a0(ring, 16u, 1024u), b0(ring + kMtA, 16u, 1024u);
+            for (uint32_t en = en0; en < en1; ++en, ++it) {
+                const uint32_t buf = it & 1u, id = product_desc(kBf16, false, 128u, r.count[en] <= 16u ? 16u : 32u);
+                live = bar_wait(acc_empty + buf * 8u, ((it >> 1) & 1u) ^ 1u, live);
+                tensor_fence_after();
+                for (uint32_t c = 0; c < chunks; ++c, ++g) {
+                    const uint32_t s = g % kDownStages;
+                    live = bar_wait(full + s * 8u, (g / kDownStages) & 1u, live);
+                    tensor_fence_after();
+                    TileDesc a = a0, b = b0;
+                    a.lo += s * (kDownStageBytes >> 4); b.lo += s * (kDownStageBytes >> 4);
+#pragma unroll
+                    for (uint32_t k = 0; k < 4u; ++k) {
+                        product_ss(sh.tmem + buf * 32u, a.at(k * 32u), b.at(k * 32u), id, c || k ? 1u : 0u);
+                        product_ss(sh.tmem + buf * 32u, a.at(k * 32u), b.at(kMtB + k * 32u), id, 1u);
+                    }
+                    products_arrive(empty + s * 8u);
+                }
+                products_arrive(acc_full + buf * 8u);
+            }
+        }
+        __syncwarp();
+    } else if (warp < 4u) {
+        const uint32_t row = tid;                            // a row of the output a thread: its sums are nobody else's
+        for (uint32_t t = 0; t < m.T; ++t) sums[t * 128u + row] = 0.0f;
+        uint32_t it = 0u;
+        for (uint32_t en = en0; en < en1; ++en, ++it) {
+            const uint32_t n = r.count[en], pair0 = r.pair0[en], buf = it & 1u;
+            live = bar_wait(acc_full + buf * 8u, (it >> 1) & 1u, live);
+            __syncwarp();
+            tensor_fence_after();
+            uint32_t v[32];
+            tensor_load(sh.tmem + buf * 32u + ((warp * 32u) << 16), v);
+            tensor_loaded(v);
+            tensor_fence_before();
+            bar_arrive(acc_empty + buf * 8u);
+#pragma unroll
+            for (int c = 0; c < kMtChunk; ++c) if ((uint32_t)c < n) sums[r.token[pair0 + c] * 128u + row] += __uint_as_float(v[c]);
+        }
+        if (d0 + row < m.D)
+            for (uint32_t t = 0; t < m.T; ++t) {
+                const bool bad = !live || (r.bad[t >> 5] >> (t & 31u)) & 1u;
+                m.part[((size_t)group * m.T + t) * m.D + d0 + row] = bad ? __int_as_float(0x7fc00000) : sums[t * 128u + row];
+            }
+    }
+    end_tiles(sh);
+}
+
+template <class Ty>
+__global__ void __launch_bounds__(256)
+k_moe_sum(const __grid_constant__ MoeDev m) {
+    const uint64_t pairs = (uint64_t)m.T * (m.D / 2u), i = (uint64_t)blockIdx.x * 256u + threadIdx.x;
+    pdl_wait();
+    if (i >= pairs) return;
+    const uint32_t t = (uint32_t)(i / (m.D / 2u)), d = (uint32_t)(i - (uint64_t)t * (m.D / 2u)) * 2u;
+    float a = 0.0f, b = 0.0f;
+    const float *from = m.part + (size_t)t * m.D + d;
+#pragma unroll 8
+    for (uint32_t g = 0; g < m.groups; ++g) {
+        const float2 v = __ldcg(reinterpret_cast<const float2 *>(from + (size_t)g * m.T * m.D));
+        a += v.x; b += v.y;
+    }
+    typename Ty::type *to = reinterpret_cast<typename Ty::type *>(m.out) + (int64_t)t * m.out_stride + d;
+    to[0] = Ty::from(a); to[1] = Ty::from(b);
+}
+
+static bool weights_map(CUtensorMap *map, const void *base, uint64_t k, uint64_t rows, const MoeDev &m, bool bf16, uint32_t box) {
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    const cuuint64_t dims[3] = {k, rows, m.E}, strides[2] = {k * 2u, (cuuint64_t)m.expert_stride * 2u};
+    const cuuint32_t boxes[3] = {64u, box, 1u}, steps[3] = {1u, 1u, 1u};
+    return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(base), dims, strides, boxes, steps,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <class Ty, bool kBf16>
+static cudaError_t launch_tiles(const MoeDev &m, uint32_t n_sm, cudaStream_t st) {
+    CUtensorMap up_map, down_map;
+    if (!weights_map(&up_map, m.experts, m.D, 2ull * m.I, m, kBf16, 16u) || !weights_map(&down_map, m.experts + 2ull * m.I * m.D, m.I, m.D, m, kBf16, 128u)) return cudaErrorInvalidValue;
+    const auto up = k_moe_up_tiles<Ty, kBf16>;
+    const auto down = k_moe_down_tiles<Ty, kBf16>;
+    cudaError_t e = ensure_dyn_smem((const void *)up, kUpTilesSmem);
+    if (e == cudaSuccess) e = ensure_dyn_smem((const void *)down, down_tiles_smem(kMtTokens));
+    if (e != cudaSuccess) return e;
+    up<<<n_sm, kMoeThreads, kUpTilesSmem, st>>>(m, up_map);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    g_kernel_launches += 3;
+    if ((e = launch_pdl(down, (m.D + 127u) / 128u * m.groups, kMoeThreads, down_tiles_smem(m.T), st, m, down_map)) != cudaSuccess) return e;
+    return launch_pdl(k_moe_sum<Ty>, (unsigned)(((uint64_t)m.T * (m.D / 2u) + 255u) / 256u), 256, 0, st, m);
+}
+cudaError_t launch_moe_tiles(const MoeDev &m, bool bf16, uint32_t n_sm, cudaStream_t st) {
+    return bf16 ? launch_tiles<Bf16, true>(m, n_sm, st) : launch_tiles<Fp16, false>(m, n_sm, st);
+}
+
+}  // namespace hbf
