@@ -85,6 +85,7 @@ __device__ __forceinline__ void choose(const MoeDev &m, Route<kTokens> &r, Route
         if (tok < m.T && lane < m.K) tmp.expert[tok * m.K + lane] = 0xffffu;
     }
     __syncwarp();
+    // (what the winner does is a store or two without a branch; all else is done for all places at once, below)
 #pragma unroll 1
     for (uint32_t j = 0; j < m.K; ++j) {
         uint32_t best[kTok];
@@ -98,37 +99,42 @@ __device__ __forceinline__ void choose(const MoeDev &m, Route<kTokens> &r, Route
         for (int t = 0; t < kTok; ++t) best[t] = __reduce_max_sync(0xffffffffu, best[t]);
 #pragma unroll
         for (int t = 0; t < kTok; ++t) {
-            if (j == 0u) {
-                first[t] = best[t];
-                if (!m.renorm)
-#pragma unroll
-                    for (int i = 0; i < kKeys; ++i) all[t] += key[t][i] ? expf(from_ordered(key[t][i]) - from_ordered(first[t])) : 0.0f;
-            }
+            if (j == 0u) first[t] = best[t];
             uint32_t at = kKeys;
 #pragma unroll
             for (int i = kKeys - 1; i >= 0; --i) if (key[t][i] == best[t]) at = i;
             const unsigned has = __ballot_sync(0xffffffffu, at < kKeys);
-            if (live[t] && best[t] && lane == __ffs(has) - 1u) {
-                const uint32_t tok = t0 + t * step, e = lane * kKeys + at;
-                tmp.expert[tok * m.K + j] = (uint16_t)e; tmp.weight[tok * m.K + j] = __uint_as_float(best[t]);
-                atomicOr(&r.mask[e][tok >> 5], 1u << (tok & 31u));
-                if (m.renorm) all[t] += expf(from_ordered(best[t]) - from_ordered(first[t]));
+            const bool won = live[t] && best[t] && (has & lanemask_lt()) == 0u && at < kKeys;
+            const uint32_t place = (t0 + t * step) * m.K + j;
+            if (won) { tmp.expert[place] = (uint16_t)(lane * kKeys + at); tmp.weight[place] = __uint_as_float(best[t]); }
+            if (!m.renorm && j == 0u)
 #pragma unroll
-                for (int i = 0; i < kKeys; ++i) if (i == (int)at) key[t][i] = 0u;
-            }
+                for (int i = 0; i < kKeys; ++i) all[t] += key[t][i] ? expf(from_ordered(key[t][i]) - from_ordered(first[t])) : 0.0f;
+#pragma unroll
+            for (int i = 0; i < kKeys; ++i) if (won && i == (int)at) key[t][i] = 0u;
         }
     }
     __syncwarp();
+    float p[kTok];
+    uint32_t mine[kTok];
 #pragma unroll
     for (int t = 0; t < kTok; ++t) {
         const uint32_t tok = t0 + t * step, at = tok * m.K + lane;
-        const float sum = warp_sum_f(all[t]);
+        mine[t] = tok < m.T && lane < m.K ? tmp.expert[at] : 0xffffu;
+        p[t] = mine[t] != 0xffffu ? expf(from_ordered(__float_as_uint(tmp.weight[at])) - from_ordered(first[t])) : 0.0f;
+        if (mine[t] != 0xffffu) atomicOr(&r.mask[mine[t]][tok >> 5], 1u << (tok & 31u));
+        if (m.renorm) all[t] = p[t];
+    }
+#pragma unroll
+    for (int t = 0; t < kTok; ++t) all[t] = warp_sum_f(all[t]);
+#pragma unroll
+    for (int t = 0; t < kTok; ++t) {
+        const uint32_t tok = t0 + t * step, at = tok * m.K + lane;
         if (tok < m.T && lane < m.K) {
-            const uint32_t e = tmp.expert[at];
-            const float w = e == 0xffffu ? 0.0f : expf(from_ordered(__float_as_uint(tmp.weight[at])) - from_ordered(first[t])) / sum;
+            const float w = mine[t] != 0xffffu ? p[t] / all[t] : 0.0f;
             tmp.weight[at] = w;
             if (write) {
-                if (m.chosen) m.chosen[at] = e == 0xffffu ? -1 : (int32_t)e;
+                if (m.chosen) m.chosen[at] = mine[t] != 0xffffu ? (int32_t)mine[t] : -1;
                 if (m.weights) m.weights[at] = w;
             }
         }

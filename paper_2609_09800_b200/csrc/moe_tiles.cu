@@ -12,7 +12,8 @@
 namespace hbf {
 
 constexpr int kMtTokens = HBF_MOE_MAX_TOKENS, kMtChunk = 32;             // tokens of an expert that an entry takes
-constexpr uint32_t kMtA = 128u * 128u, kMtB = kMtChunk * 128u;           // bytes of a stage, 64 of the sum's places: weights; activations
+constexpr uint32_t kMtA = 128u * 128u, kMtB = kMtChunk * 128u;           // bytes of a stage, 64 of the sum's places: weights; activations (the down product: twice)
+struct UpMaps { CUtensorMap rows[3]; };                                  // boxes of 64, 48 and 32 rows: a copy takes its thread 85 cycles, whatever its size
 constexpr int kUpStages = 8, kDownStages = 5, kMtLag = 3;
 constexpr uint32_t kUpStageBytes = kMtA + kMtB, kDownStageBytes = kMtA + 2u * kMtB;
 
@@ -30,7 +31,7 @@ __device__ __forceinline__ void tensor_copy3(uint32_t dst, const CUtensorMap *ma
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
 
-// Both kernels' blocks begin alike: barriers, tensor memory (two times 32 columns), the choice.  Warps 0 to 3: a lane of tensor memory a thread;
+// Both kernels' blocks begin alike: barriers, tensor memory (two times 64 columns), the choice.  Warps 0 to 3: a lane of tensor memory a thread;
 // 4 to 7: the activations' 16-byte copies; 8: tensor copies; 9: products; all 16 make the choice.
 template <int kStages>
 __device__ __forceinline__ void begin_tiles(const MoeDev &m, MtShared &sh, unsigned char *tmp, bool write) {
@@ -39,7 +40,7 @@ __device__ __forceinline__ void begin_tiles(const MoeDev &m, MtShared &sh, unsig
         for (int i = 0; i < 2; ++i) { bar_init(smem_addr(&sh.acc_full[i]), 1u); bar_init(smem_addr(&sh.acc_empty[i]), 128u); }
         bar_init_done();
     }
-    if ((threadIdx.x >> 5) == 9u) { tensor_alloc(smem_addr(&sh.tmem), 64u); tensor_fence_before(); }
+    if ((threadIdx.x >> 5) == 9u) { tensor_alloc(smem_addr(&sh.tmem), 128u); tensor_fence_before(); }
     route(m, sh.route, *reinterpret_cast<RouteTemp<kMtTokens> *>(tmp), kMtChunk, write);
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");         // the choice's memory is the ring's now
     __syncthreads();
@@ -48,7 +49,7 @@ __device__ __forceinline__ void begin_tiles(const MoeDev &m, MtShared &sh, unsig
 __device__ __forceinline__ void end_tiles(const MtShared &sh) {
     tensor_fence_before();
     __syncthreads();
-    if ((threadIdx.x >> 5) == 9u) { __syncwarp(); tensor_fence_after(); tensor_free(sh.tmem, 64u); }
+    if ((threadIdx.x >> 5) == 9u) { __syncwarp(); tensor_fence_after(); tensor_free(sh.tmem, 128u); }
 }
 
 // The activations' side of a ring: stage g's copies are issued by `copy(stage address)`; they are said to be there kMtLag stages later, and before
@@ -76,7 +77,7 @@ struct Gather {
 
 template <class Ty, bool kBf16>
 __global__ void __launch_bounds__(kMoeThreads, 1)
-k_moe_up_tiles(const __grid_constant__ MoeDev m, const __grid_constant__ CUtensorMap w_map) {
+k_moe_up_tiles(const __grid_constant__ MoeDev m, const __grid_constant__ UpMaps maps) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
     const uint32_t ring = smem_addr(smem);
@@ -99,17 +100,17 @@ k_moe_up_tiles(const __grid_constant__ MoeDev m, const __grid_constant__ CUtenso
     if (warp == 8u) {
         if (lane == 0u) {
             uint32_t g = 0u;
+            const CUtensorMap *map = &maps.rows[(64u - rows) / 16u];
             for (uint32_t item = blockIdx.x; item < n_items; item += gridDim.x) {
                 const uint32_t en = item / tiles, i0 = (item - en * tiles) * rows, e = r.expert[en];
                 for (uint32_t c = 0; c < chunks; ++c, ++g) {
                     const uint32_t s = g % kUpStages, at = ring + s * kUpStageBytes, bar = full + s * 8u;
                     live = bar_wait(empty + s * 8u, ((g / kUpStages) & 1u) ^ 1u, live);
                     bar_arrive_bytes(bar, live ? rows * 256u : 0u);
-                    if (live)
-                        for (uint32_t b = 0; b < rows; b += 16u) {
-                            tensor_copy3(at + b * 128u, &w_map, (int32_t)(c * 64u), (int32_t)(i0 + b), (int32_t)e, bar);
-                            tensor_copy3(at + 8192u + b * 128u, &w_map, (int32_t)(c * 64u), (int32_t)(m.I + i0 + b), (int32_t)e, bar);
-                        }
+                    if (live) {
+                        tensor_copy3(at, map, (int32_t)(c * 64u), (int32_t)i0, (int32_t)e, bar);
+                        tensor_copy3(at + 8192u, map, (int32_t)(c * 64u), (int32_t)(m.I + i0), (int32_t)e, bar);
+                    }
                 }
             }
         }
@@ -223,13 +224,14 @@ k_moe_down_tiles(const __grid_constant__ MoeDev m, const __grid_constant__ CUten
             const uint32_t n = r.count[en], pair0 = r.pair0[en];
             const size_t h0 = (size_t)(pair0 + row) * m.I, h1 = (size_t)(pair0 + row + 16u) * m.I;
             const bool is0 = row < n, is1 = row + 16u < n;
+            const uint32_t second = n <= 16u ? 2048u : kMtB; // rows 16 or 32 and on: the second numbers
             for (uint32_t c = 0; c < chunks; ++c)
                 in.stage([&](uint32_t at) {
                     const uint32_t k = c * 64u + col * 8u;
                     const bool is = k < m.I;
                     const size_t a = is ? h0 + k : 0u, b = is ? h1 + k : 0u;
-                    if (is0) { copy_async16(at + to, m.h_hi + a, is); copy_async16(at + kMtB + to, m.h_lo + a, is); }
-                    if (is1) { copy_async16(at + 2048u + to, m.h_hi + b, is); copy_async16(at + kMtB + 2048u + to, m.h_lo + b, is); }
+                    if (is0) { copy_async16(at + to, m.h_hi + a, is); copy_async16(at + second + to, m.h_lo + a, is); }
+                    if (is1) { copy_async16(at + 2048u + to, m.h_hi + b, is); copy_async16(at + second + 2048u + to, m.h_lo + b, is); }
                 });
         }
         in.finish();
@@ -238,7 +240,8 @@ k_moe_down_tiles(const __grid_constant__ MoeDev m, const __grid_constant__ CUten
             uint32_t g = 0u, it = 0u;
             const TileDesc a0(ring, 16u, 1024u), b0(ring + kMtA, 16u, 1024u);
             for (uint32_t en = en0; en < en1; ++en, ++it) {
-                const uint32_t buf = it & 1u, id = product_desc(kBf16, false, 128u, r.count[en] <= 16u ? 16u : 32u);
+                // first and second numbers are columns of one product (a product of 128 rows takes 60 cycles up to 64 columns)
+                const uint32_t buf = it & 1u, id = product_desc(kBf16, false, 128u, r.count[en] <= 16u ? 32u : 64u);
                 live = bar_wait(acc_empty + buf * 8u, ((it >> 1) & 1u) ^ 1u, live);
                 tensor_fence_after();
                 for (uint32_t c = 0; c < chunks; ++c, ++g) {
@@ -248,10 +251,7 @@ k_moe_down_tiles(const __grid_constant__ MoeDev m, const __grid_constant__ CUten
                     TileDesc a = a0, b = b0;
                     a.lo += s * (kDownStageBytes >> 4); b.lo += s * (kDownStageBytes >> 4);
 #pragma unroll
-                    for (uint32_t k = 0; k < 4u; ++k) {
-                        product_ss(sh.tmem + buf * 32u, a.at(k * 32u), b.at(k * 32u), id, c || k ? 1u : 0u);
-                        product_ss(sh.tmem + buf * 32u, a.at(k * 32u), b.at(kMtB + k * 32u), id, 1u);
-                    }
+                    for (uint32_t k = 0; k < 4u; ++k) product_ss(sh.tmem + buf * 64u, a.at(k * 32u), b.at(k * 32u), id, c || k ? 1u : 0u);
                     products_arrive(empty + s * 8u);
                 }
                 products_arrive(acc_full + buf * 8u);
@@ -267,13 +267,16 @@ k_moe_down_tiles(const __grid_constant__ MoeDev m, const __grid_constant__ CUten
             live = bar_wait(acc_full + buf * 8u, (it >> 1) & 1u, live);
             __syncwarp();
             tensor_fence_after();
-            uint32_t v[32];
-            tensor_load(sh.tmem + buf * 32u + ((warp * 32u) << 16), v);
-            tensor_loaded(v);
+            const uint32_t from = sh.tmem + buf * 64u + ((warp * 32u) << 16);
+            for (uint32_t c0 = 0; c0 < n; c0 += 16u) {
+                uint32_t v[16], w[16];
+                tensor_load16(from + c0, v);
+                tensor_load16(from + (n <= 16u ? 16u : 32u) + c0, w);
+#pragma unroll
+                for (int c = 0; c < 16; ++c) if (c0 + c < n) sums[r.token[pair0 + c0 + c] * 128u + row] += __uint_as_float(v[c]) + __uint_as_float(w[c]);
+            }
             tensor_fence_before();
             bar_arrive(acc_empty + buf * 8u);
-#pragma unroll
-            for (int c = 0; c < kMtChunk; ++c) if ((uint32_t)c < n) sums[r.token[pair0 + c] * 128u + row] += __uint_as_float(v[c]);
         }
         if (d0 + row < m.D)
             for (uint32_t t = 0; t < m.T; ++t) {
@@ -313,14 +316,16 @@ static bool weights_map(CUtensorMap *map, const void *base, uint64_t k, uint64_t
 
 template <class Ty, bool kBf16>
 static cudaError_t launch_tiles(const MoeDev &m, uint32_t n_sm, cudaStream_t st) {
-    CUtensorMap up_map, down_map;
-    if (!weights_map(&up_map, m.experts, m.D, 2ull * m.I, m, kBf16, 16u) || !weights_map(&down_map, m.experts + 2ull * m.I * m.D, m.I, m.D, m, kBf16, 128u)) return cudaErrorInvalidValue;
+    UpMaps up_maps;
+    CUtensorMap down_map;
+    for (uint32_t i = 0; i < 3u; ++i) if (!weights_map(&up_maps.rows[i], m.experts, m.D, 2ull * m.I, m, kBf16, 64u - 16u * i)) return cudaErrorInvalidValue;
+    if (!weights_map(&down_map, m.experts + 2ull * m.I * m.D, m.I, m.D, m, kBf16, 128u)) return cudaErrorInvalidValue;
     const auto up = k_moe_up_tiles<Ty, kBf16>;
     const auto down = k_moe_down_tiles<Ty, kBf16>;
     cudaError_t e = ensure_dyn_smem((const void *)up, kUpTilesSmem);
     if (e == cudaSuccess) e = ensure_dyn_smem((const void *)down, down_tiles_smem(kMtTokens));
     if (e != cudaSuccess) return e;
-    up<<<n_sm, kMoeThreads, kUpTilesSmem, st>>>(m, up_map);
+    up<<<n_sm, kMoeThreads, kUpTilesSmem, st>>>(m, up_maps);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     g_kernel_launches += 3;
     if ((e = launch_pdl(down, (m.D + 127u) / 128u * m.groups, kMoeThreads, down_tiles_smem(m.T), st, m, down_map)) != cudaSuccess) return e;
