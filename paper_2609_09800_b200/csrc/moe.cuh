@@ -16,6 +16,7 @@ struct MoeDev {
     uint16_t *h_hi, *h_lo;                                   // [pairs by expert, then token][I]
     uint32_t rows;                                           // of the down product that a block takes, at most 16
     float *part; uint32_t groups;                            // moe_tiles.cu: [groups][T][D], the sums of a group's experts
+    uint16_t *route_e; float *route_w;                       // and [T][K]: the choice, made by a kernel of its own (0xfffe: the token has none)
     Div32 div_slices, div_k;                                 // I / 8; K
 };
 
@@ -53,10 +54,11 @@ __device__ __forceinline__ float warp_sum_f(float v) {
     return v;
 }
 
-// The choice of kTok tokens t0, t0 + step, ... by one warp, kKeys neighbouring scores a lane.  A turn finds the largest score left (the lowest lane
-// that has it, and the lowest of its experts, win a tie); the tokens' turns do not depend on one another, so several of them hide
-// each other's latency.  Left in `tmp`: the chosen experts (0xffff: none left), and their scores' keys as the bits of the weights.
-template <int kKeys, int kTok, int kTokens>
+// The choice of kTok tokens t0, t0 + step, ... by one warp, kKeys neighbouring scores a lane.  A lane puts its own scores in order, once; a turn
+// takes the largest of the lanes' first ones (the lowest lane that has it wins a tie, and in a lane the lowest expert comes first), and lane j
+// keeps what turn j took.  Instructions bound it where a warp has several tokens (searching every lane's scores in every turn: 64 tokens of
+// 128 experts 6.5 us; turns of several tokens at once hide each other's latency).
+template <int kKeys, int kTok, bool kOwn, int kTokens>
 __device__ __forceinline__ void choose(const MoeDev &m, Route<kTokens> &r, RouteTemp<kTokens> &tmp, uint32_t t0, uint32_t step, bool write) {
     const uint32_t lane = lane_id();
     uint32_t key[kTok][kKeys], first[kTok];
@@ -80,83 +82,101 @@ __device__ __forceinline__ void choose(const MoeDev &m, Route<kTokens> &r, Route
         nan = __any_sync(0xffffffffu, nan);
         const uint32_t tok = t0 + t * step;
         live[t] = tok < m.T && !nan;
-        if (nan && lane == 0u) atomicOr(&r.bad[tok >> 5], 1u << (tok & 31u));
+        if (!kOwn && nan && lane == 0u) atomicOr(&r.bad[tok >> 5], 1u << (tok & 31u));
         first[t] = 0u; all[t] = 0.0f;
-        if (tok < m.T && lane < m.K) tmp.expert[tok * m.K + lane] = 0xffffu;
     }
-    __syncwarp();
-    // (what the winner does is a store or two without a branch; all else is done for all places at once, below)
+    uint32_t at[kTok][kKeys], mine[kTok], took[kTok];        // the scores' experts; of turn `lane`: expert and score
+#pragma unroll
+    for (int t = 0; t < kTok; ++t) {
+#pragma unroll
+        for (int i = 0; i < kKeys; ++i) at[t][i] = lane * kKeys + i;
+#pragma unroll
+        for (int k = 0; k < kKeys; ++k)
+#pragma unroll
+            for (int i = k & 1; i + 1 < kKeys; i += 2) {
+                const bool swap = key[t][i] < key[t][i + 1];
+                const uint32_t u = key[t][i], v = key[t][i + 1], x = at[t][i], y = at[t][i + 1];
+                key[t][i] = swap ? v : u; key[t][i + 1] = swap ? u : v; at[t][i] = swap ? y : x; at[t][i + 1] = swap ? x : y;
+            }
+        if (!m.renorm) {
+            first[t] = __reduce_max_sync(0xffffffffu, key[t][0]);
+#pragma unroll
+            for (int i = 0; i < kKeys; ++i) all[t] += key[t][i] ? expf(from_ordered(key[t][i]) - from_ordered(first[t])) : 0.0f;
+        }
+        mine[t] = 0xffffu; took[t] = 0u;
+        if (!live[t])
+#pragma unroll
+            for (int i = 0; i < kKeys; ++i) key[t][i] = 0u;
+    }
 #pragma unroll 1
     for (uint32_t j = 0; j < m.K; ++j) {
         uint32_t best[kTok];
 #pragma unroll
-        for (int t = 0; t < kTok; ++t) {
-            best[t] = key[t][0];
-#pragma unroll
-            for (int i = 1; i < kKeys; ++i) best[t] = max(best[t], key[t][i]);
-        }
-#pragma unroll
-        for (int t = 0; t < kTok; ++t) best[t] = __reduce_max_sync(0xffffffffu, best[t]);
+        for (int t = 0; t < kTok; ++t) best[t] = __reduce_max_sync(0xffffffffu, key[t][0]);
 #pragma unroll
         for (int t = 0; t < kTok; ++t) {
+            const unsigned has = __ballot_sync(0xffffffffu, key[t][0] == best[t]);
+            const uint32_t e = __shfl_sync(0xffffffffu, at[t][0], __ffs(has) - 1);
             if (j == 0u) first[t] = best[t];
-            uint32_t at = kKeys;
+            if (lane == j && best[t]) { mine[t] = e; took[t] = best[t]; }
+            const bool won = e == at[t][0];                  // (of a lane whose scores are used up nothing is left to lose)
 #pragma unroll
-            for (int i = kKeys - 1; i >= 0; --i) if (key[t][i] == best[t]) at = i;
-            const unsigned has = __ballot_sync(0xffffffffu, at < kKeys);
-            const bool won = live[t] && best[t] && (has & lanemask_lt()) == 0u && at < kKeys;
-            const uint32_t place = (t0 + t * step) * m.K + j;
-            if (won) { tmp.expert[place] = (uint16_t)(lane * kKeys + at); tmp.weight[place] = __uint_as_float(best[t]); }
-            if (!m.renorm && j == 0u)
-#pragma unroll
-                for (int i = 0; i < kKeys; ++i) all[t] += key[t][i] ? expf(from_ordered(key[t][i]) - from_ordered(first[t])) : 0.0f;
-#pragma unroll
-            for (int i = 0; i < kKeys; ++i) if (won && i == (int)at) key[t][i] = 0u;
+            for (int i = 0; i + 1 < kKeys; ++i) { key[t][i] = won ? key[t][i + 1] : key[t][i]; at[t][i] = won ? at[t][i + 1] : at[t][i]; }
+            key[t][kKeys - 1] = won ? 0u : key[t][kKeys - 1];
         }
     }
-    __syncwarp();
     float p[kTok];
-    uint32_t mine[kTok];
 #pragma unroll
     for (int t = 0; t < kTok; ++t) {
-        const uint32_t tok = t0 + t * step, at = tok * m.K + lane;
-        mine[t] = tok < m.T && lane < m.K ? tmp.expert[at] : 0xffffu;
-        p[t] = mine[t] != 0xffffu ? expf(from_ordered(__float_as_uint(tmp.weight[at])) - from_ordered(first[t])) : 0.0f;
-        if (mine[t] != 0xffffu) atomicOr(&r.mask[mine[t]][tok >> 5], 1u << (tok & 31u));
+        const uint32_t tok = t0 + t * step;
+        p[t] = mine[t] != 0xffffu ? expf(from_ordered(took[t]) - from_ordered(first[t])) : 0.0f;
+        if (!kOwn && mine[t] != 0xffffu) atomicOr(&r.mask[mine[t]][tok >> 5], 1u << (tok & 31u));
         if (m.renorm) all[t] = p[t];
     }
 #pragma unroll
     for (int t = 0; t < kTok; ++t) all[t] = warp_sum_f(all[t]);
 #pragma unroll
     for (int t = 0; t < kTok; ++t) {
-        const uint32_t tok = t0 + t * step, at = tok * m.K + lane;
+        const uint32_t tok = t0 + t * step, place = tok * m.K + lane;
         if (tok < m.T && lane < m.K) {
             const float w = mine[t] != 0xffffu ? p[t] / all[t] : 0.0f;
-            tmp.weight[at] = w;
+            if (kOwn) { m.route_e[place] = (uint16_t)(live[t] ? mine[t] : 0xfffeu); m.route_w[place] = w; }
+            else { tmp.expert[place] = (uint16_t)mine[t]; tmp.weight[place] = w; }
             if (write) {
-                if (m.chosen) m.chosen[at] = mine[t] != 0xffffu ? (int32_t)mine[t] : -1;
-                if (m.weights) m.weights[at] = w;
+                if (m.chosen) m.chosen[place] = mine[t] != 0xffffu ? (int32_t)mine[t] : -1;
+                if (m.weights) m.weights[place] = w;
             }
         }
     }
 }
 
-// The whole batch's choice by a block.  Every block of both kernels makes it for itself, which costs less than a kernel of its
-// own in front would.
+// The whole batch's choice by a block.  For a few tokens (one a warp) every block of both kernels makes it for itself, which costs less than a
+// kernel of its own in front would; else that has made it (kLoad), a token a warp on as many SMs (64 tokens by every block's sixteen warps
+// took 6.5 us in each of the two kernels), and the block only takes it over.
 template <int kKeys, int kTok, int kTokens>
 __device__ __forceinline__ void route_tokens(const MoeDev &m, Route<kTokens> &r, RouteTemp<kTokens> &tmp, bool write) {
     constexpr uint32_t kWarps = kMoeWarps;
 #pragma unroll 1
-    for (uint32_t t = threadIdx.x >> 5; t < m.T; t += kWarps * kTok) choose<kKeys, kTok>(m, r, tmp, t, kWarps, write);
+    for (uint32_t t = threadIdx.x >> 5; t < m.T; t += kWarps * kTok) choose<kKeys, kTok, false>(m, r, tmp, t, kWarps, write);
 }
-template <int kTokens>
+template <bool kLoad, int kTokens>
 __device__ __forceinline__ void route(const MoeDev &m, Route<kTokens> &r, RouteTemp<kTokens> &tmp, uint32_t chunk, bool write) {
     constexpr int kEach = HBF_MOE_MAX_EXPERTS / kMoeThreads, kWords = Route<kTokens>::kWords;  // experts a thread in the scan, side by side
     const uint32_t tid = threadIdx.x, lane = lane_id(), warp = tid >> 5;
     for (uint32_t i = tid; i < m.E * kWords; i += kMoeThreads) r.mask[0][i] = 0u;
     if (tid < kWords) r.bad[tid] = 0u;
     __syncthreads();
-    if (m.E > 128u) route_tokens<HBF_MOE_MAX_EXPERTS / 32, 1>(m, r, tmp, write);
+    if (kLoad) {
+#pragma unroll 1
+        for (uint32_t i = tid; i < m.T * m.K; i += kMoeThreads) {
+            uint32_t e = m.route_e[i];
+            const float w = m.route_w[i];
+            const uint32_t t = div32(i, m.div_k);
+            if (e == 0xfffeu) { atomicOr(&r.bad[t >> 5], 1u << (t & 31u)); e = 0xffffu; }
+            if (e != 0xffffu) atomicOr(&r.mask[e][t >> 5], 1u << (t & 31u));
+            tmp.expert[i] = (uint16_t)e; tmp.weight[i] = w;
+        }
+    } else if (m.E > 128u) route_tokens<HBF_MOE_MAX_EXPERTS / 32, 1>(m, r, tmp, write);
     else if (kTokens > kMoeWarps && m.T > kMoeWarps) route_tokens<4, kTokens / kMoeWarps < 4 ? 1 : 4>(m, r, tmp, write);
     else route_tokens<4, 1>(m, r, tmp, write);
     __syncthreads();

@@ -57,7 +57,7 @@ k_moe_up(const __grid_constant__ MoeDev m) {
     Route<kTokens> &r = *reinterpret_cast<Route<kTokens> *>(smem);
     const uint32_t lane = lane_id(), warp = threadIdx.x >> 5, row = lane >> 2, quad = lane & 3u;
     pdl_trigger();
-    route(m, r, *reinterpret_cast<RouteTemp<kTokens> *>(smem + kRouteBytes<kTokens>), kTiles * 8u, blockIdx.x == 0);
+    route<false>(m, r, *reinterpret_cast<RouteTemp<kTokens> *>(smem + kRouteBytes<kTokens>), kTiles * 8u, blockIdx.x == 0);
     const uint32_t slices = m.I / 8u, n_items = r.n_entries * slices;
     const uint32_t steps = ((m.D + 31u) / 32u + kMoeWarps - 1u) / kMoeWarps;               // of a warp, an item
     const uint32_t ring = smem_addr(smem) + kUpRingAt<kTiles, kTokens> + warp * (kRing * 1024u) + lane * 16u, k0 = warp * 32u + quad * 8u;
@@ -162,7 +162,7 @@ k_moe_down(const __grid_constant__ MoeDev m) {
     extern __shared__ __align__(128) unsigned char smem[];
     Route<kTokens> &r = *reinterpret_cast<Route<kTokens> *>(smem);
     const uint32_t tid = threadIdx.x, lane = lane_id(), warp = tid >> 5, row = lane >> 2, quad = lane & 3u;
-    route(m, r, *reinterpret_cast<RouteTemp<kTokens> *>(smem + kRouteBytes<kTokens>), kTiles * 8u, false);
+    route<false>(m, r, *reinterpret_cast<RouteTemp<kTokens> *>(smem + kRouteBytes<kTokens>), kTiles * 8u, false);
     float *sums = reinterpret_cast<float *>(smem + kRouteBytes<kTokens>);                   // [warp][token][16]
     float *mine = sums + (size_t)warp * m.T * 16u;
     constexpr uint32_t kStep = kWide * 32u, kSlot = kWide * 1024u;
@@ -298,7 +298,7 @@ k_moe_accesses(const __grid_constant__ MoeDev m, uint64_t expert_bytes, uint32_t
     extern __shared__ __align__(128) unsigned char smem[];
     constexpr int kTokens = HBF_MOE_MAX_TOKENS;
     Route<kTokens> &r = *reinterpret_cast<Route<kTokens> *>(smem);
-    route(m, r, *reinterpret_cast<RouteTemp<kTokens> *>(smem + kRouteBytes<kTokens>), 8u, false);
+    route<false>(m, r, *reinterpret_cast<RouteTemp<kTokens> *>(smem + kRouteBytes<kTokens>), 8u, false);
     for (uint64_t i = (uint64_t)blockIdx.x * kMoeThreads + threadIdx.x; i < n; i += (uint64_t)gridDim.x * kMoeThreads) {
         const uint32_t a = (uint32_t)(i / tiles), t = (uint32_t)(i - (uint64_t)a * tiles);
         hbf_access_t v = {0, issue_ns + (int64_t)i * gap_ns, 1, 0};
@@ -324,16 +324,16 @@ static bool moe_pointers_ok(const hbf_moe_t *m) {
 }
 // Tokens up to which the weights are read from registers' side (k_moe_up, k_moe_down).
 constexpr uint32_t kMoeFew = 8;
-// The activations between the products, and past a few tokens the parts' sums; 0: the device cannot be asked.
+// The activations between the products, and past a few tokens the parts' sums and the choice; 0: the device cannot be asked.
 static size_t moe_bytes(const hbf_moe_t *m, uint32_t *groups) {
-    const size_t h = ((size_t)m->tokens * m->top_k * m->inter * 4u + 255u) / 256u * 256u;
+    const size_t pairs = (size_t)m->tokens * m->top_k, h = (pairs * m->inter * 4u + 255u) / 256u * 256u;
     if (groups) *groups = 1u;
     if (m->tokens <= kMoeFew) return h;
     uint32_t n_sm = 0;
     if (sm_count(&n_sm) != HBF_OK) return 0;
     const uint32_t g = moe_groups(m->tokens, m->hidden, m->n_experts, m->top_k, n_sm);
     if (groups) *groups = g;
-    return h + ((size_t)g * m->tokens * m->hidden * 4u + 255u) / 256u * 256u;
+    return h + ((size_t)g * m->tokens * m->hidden * 4u + 255u) / 256u * 256u + (pairs * 6u + 255u) / 256u * 256u;
 }
 static MoeDev moe_dev(const hbf_moe_t *m) {
     MoeDev d = {};
@@ -400,7 +400,10 @@ extern "C" int hbf_moe_layer(const hbf_moe_t *m, void *d_workspace, size_t works
     if (rc != HBF_OK) return rc;
     const size_t pairs = (size_t)m->tokens * m->top_k;
     d.h_hi = static_cast<uint16_t *>(d_workspace); d.h_lo = d.h_hi + pairs * m->inter;
-    d.part = reinterpret_cast<float *>(static_cast<unsigned char *>(d_workspace) + (pairs * m->inter * 4u + 255u) / 256u * 256u);
+    unsigned char *more = static_cast<unsigned char *>(d_workspace) + (pairs * m->inter * 4u + 255u) / 256u * 256u;
+    d.part = reinterpret_cast<float *>(more);
+    d.route_w = reinterpret_cast<float *>(more + ((size_t)d.groups * m->tokens * m->hidden * 4u + 255u) / 256u * 256u);
+    d.route_e = reinterpret_cast<uint16_t *>(d.route_w + pairs);
     const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     return (m->dtype == HBF_BF16 ? launch_moe<Bf16>(d, n_sm, st) : launch_moe<Fp16>(d, n_sm, st)) == cudaSuccess ? HBF_OK : HBF_E_CUDA;
 }

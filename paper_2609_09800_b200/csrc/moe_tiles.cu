@@ -3,6 +3,7 @@
 // tensor cores read, and 128 rows of them against 16 or 32 tokens are products into tensor memory that one thread issues.  (With m16n8k16
 // products fed from registers, as moe_kernels.cu does for a few tokens, instructions bound it: 64 tokens, 837 MB of weights, 257 us.)
 //
+//   k_moe_choose      the tokens' experts, a token a warp
 //   k_moe_up_tiles    up to 64 gate rows and the same up rows of an expert in use, times its tokens: h = w silu(gate) up
 //   k_moe_down_tiles  128 rows of the output for all tokens, from a part of the experts: their sums, in the experts' order
 //   k_moe_sum         the parts' sums, in their order
@@ -32,16 +33,16 @@ __device__ __forceinline__ void tensor_copy3(uint32_t dst, const CUtensorMap *ma
 }
 
 // Both kernels' blocks begin alike: barriers, tensor memory (two times 64 columns), the choice.  Warps 0 to 3: a lane of tensor memory a thread;
-// 4 to 7: the activations' 16-byte copies; 8: tensor copies; 9: products; all 16 make the choice.
+// 4 to 7: the activations' 16-byte copies; 8: tensor copies; 9: products; all 16 take the choice over.
 template <int kStages>
-__device__ __forceinline__ void begin_tiles(const MoeDev &m, MtShared &sh, unsigned char *tmp, bool write) {
+__device__ __forceinline__ void begin_tiles(const MoeDev &m, MtShared &sh, unsigned char *tmp) {
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) { bar_init(smem_addr(&sh.full[i]), 129u); bar_init(smem_addr(&sh.empty[i]), 1u); }
         for (int i = 0; i < 2; ++i) { bar_init(smem_addr(&sh.acc_full[i]), 1u); bar_init(smem_addr(&sh.acc_empty[i]), 128u); }
         bar_init_done();
     }
     if ((threadIdx.x >> 5) == 9u) { tensor_alloc(smem_addr(&sh.tmem), 128u); tensor_fence_before(); }
-    route(m, sh.route, *reinterpret_cast<RouteTemp<kMtTokens> *>(tmp), kMtChunk, write);
+    route<true>(m, sh.route, *reinterpret_cast<RouteTemp<kMtTokens> *>(tmp), kMtChunk, false);
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");         // the choice's memory is the ring's now
     __syncthreads();
     tensor_fence_after();
@@ -75,6 +76,15 @@ struct Gather {
     }
 };
 
+__global__ void __launch_bounds__(32)
+k_moe_choose(const __grid_constant__ MoeDev m) {
+    pdl_trigger();
+    Route<32> *none = nullptr;
+    RouteTemp<32> *none_too = nullptr;
+    if (m.E <= 128u) choose<4, 1, true>(m, *none, *none_too, blockIdx.x, 1u, true);
+    else choose<HBF_MOE_MAX_EXPERTS / 32, 1, true>(m, *none, *none_too, blockIdx.x, 1u, true);
+}
+
 template <class Ty, bool kBf16>
 __global__ void __launch_bounds__(kMoeThreads, 1)
 k_moe_up_tiles(const __grid_constant__ MoeDev m, const __grid_constant__ UpMaps maps) {
@@ -85,8 +95,9 @@ k_moe_up_tiles(const __grid_constant__ MoeDev m, const __grid_constant__ UpMaps 
     MtShared &sh = *reinterpret_cast<MtShared *>(smem + kUpStages * kUpStageBytes + 2u * kMtChunk * 64u * 4u);
     const Route<kMtTokens> &r = sh.route;
     const uint32_t tid = threadIdx.x, lane = lane_id(), warp = tid >> 5;
+    pdl_wait();                                              // the choice is made; it is for the kernel behind this one, too
     pdl_trigger();
-    begin_tiles<kUpStages>(m, sh, smem, blockIdx.x == 0);
+    begin_tiles<kUpStages>(m, sh, smem);
     // rows of gate and up that an item takes: of 64, 48 and 32 those with which the blocks are done first
     uint32_t rows = 64u, best = 0xffffffffu;
 #pragma unroll
@@ -200,7 +211,7 @@ k_moe_down_tiles(const __grid_constant__ MoeDev m, const __grid_constant__ CUten
     const Route<kMtTokens> &r = sh.route;
     const uint32_t tid = threadIdx.x, lane = lane_id(), warp = tid >> 5;
     pdl_trigger();
-    begin_tiles<kDownStages>(m, sh, smem, false);
+    begin_tiles<kDownStages>(m, sh, smem);
     const uint32_t d_tiles = (m.D + 127u) / 128u, group = blockIdx.x / d_tiles, d0 = (blockIdx.x - group * d_tiles) * 128u, chunks = (m.I + 63u) / 64u;
     const uint32_t en0 = r.n_entries * group / m.groups, en1 = r.n_entries * (group + 1u) / m.groups;
     const uint32_t full = smem_addr(sh.full), empty = smem_addr(sh.empty), acc_full = smem_addr(sh.acc_full), acc_empty = smem_addr(sh.acc_empty);
@@ -325,9 +336,10 @@ static cudaError_t launch_tiles(const MoeDev &m, uint32_t n_sm, cudaStream_t st)
     cudaError_t e = ensure_dyn_smem((const void *)up, kUpTilesSmem);
     if (e == cudaSuccess) e = ensure_dyn_smem((const void *)down, down_tiles_smem(kMtTokens));
     if (e != cudaSuccess) return e;
-    up<<<n_sm, kMoeThreads, kUpTilesSmem, st>>>(m, up_maps);
+    k_moe_choose<<<m.T, 32, 0, st>>>(m);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    g_kernel_launches += 3;
+    g_kernel_launches += 4;
+    if ((e = launch_pdl(up, n_sm, kMoeThreads, kUpTilesSmem, st, m, up_maps)) != cudaSuccess) return e;
     if ((e = launch_pdl(down, (m.D + 127u) / 128u * m.groups, kMoeThreads, down_tiles_smem(m.T), st, m, down_map)) != cudaSuccess) return e;
     return launch_pdl(k_moe_sum<Ty>, (unsigned)(((uint64_t)m.T * (m.D / 2u) + 255u) / 256u), 256, 0, st, m);
 }
