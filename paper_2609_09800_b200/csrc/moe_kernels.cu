@@ -322,13 +322,18 @@ static bool moe_pointers_ok(const hbf_moe_t *m) {
     if (!m->scores || !m->experts || (uintptr_t)m->experts % 16 || (uintptr_t)m->scores % 4 || m->scores_stride < (int64_t)m->n_experts) return false;
     return true;
 }
-// Tokens up to which the weights are read from registers' side (k_moe_up, k_moe_down).
-constexpr uint32_t kMoeFew = 8;
+// Whether the layer goes through k_moe_up and k_moe_down: two launches instead of four, some 8 us less, but 4.0 to 5.3 TB/s where moe_tiles.cu
+// reaches 5.7; the sides are even at about 220 MB of weights (2048 x 768, top 8 of 128: 2 tokens 40 us against 45, 3 tokens 53 against 52, 6 tokens
+// 86 against 68).  The number of experts in use is the router's; the most that there can be are counted.
+static bool moe_few(const hbf_moe_t *m) {
+    const uint64_t pairs = (uint64_t)m->tokens * m->top_k, used = pairs < m->n_experts ? pairs : m->n_experts;
+    return m->tokens <= 8u && used * m->hidden * m->inter * 6u <= (220ull << 20);
+}
 // The activations between the products, and past a few tokens the parts' sums and the choice; 0: the device cannot be asked.
 static size_t moe_bytes(const hbf_moe_t *m, uint32_t *groups) {
     const size_t pairs = (size_t)m->tokens * m->top_k, h = (pairs * m->inter * 4u + 255u) / 256u * 256u;
     if (groups) *groups = 1u;
-    if (m->tokens <= kMoeFew) return h;
+    if (moe_few(m)) return h;
     uint32_t n_sm = 0;
     if (sm_count(&n_sm) != HBF_OK) return 0;
     const uint32_t g = moe_groups(m->tokens, m->hidden, m->n_experts, m->top_k, n_sm);
@@ -367,12 +372,12 @@ static cudaError_t launch_moe_as(const MoeDev &d, uint32_t n_sm, cudaStream_t st
     return launch_pdl(down_k, blocks < n_sm ? blocks : n_sm, kMoeThreads, down_smem<kTokens, kDownRing, kWide>(d.T), st, d);
 }
 template <class Ty>
-static cudaError_t launch_moe(MoeDev d, uint32_t n_sm, cudaStream_t st) {
+static cudaError_t launch_moe(MoeDev d, bool few, uint32_t n_sm, cudaStream_t st) {
     d.div_slices = make_div32(d.I / 8u);
     // an even share of the output's rows to every SM, 16 at most: 2,048 rows are 14 a block on 147 blocks
     const uint32_t rounds = (d.D + 16u * n_sm - 1u) / (16u * n_sm);
     d.rows = (d.D + rounds * n_sm - 1u) / (rounds * n_sm);
-    if (d.T <= kMoeFew) return launch_moe_as<Ty, 1, 8, 5, 4, 1, 2>(d, n_sm, st);
+    if (few) return launch_moe_as<Ty, 1, 8, 5, 4, 1, 2>(d, n_sm, st);
     return launch_moe_tiles(d, std::is_same<Ty, Bf16>::value, n_sm, st);
 }
 
@@ -405,7 +410,7 @@ extern "C" int hbf_moe_layer(const hbf_moe_t *m, void *d_workspace, size_t works
     d.route_w = reinterpret_cast<float *>(more + ((size_t)d.groups * m->tokens * m->hidden * 4u + 255u) / 256u * 256u);
     d.route_e = reinterpret_cast<uint16_t *>(d.route_w + pairs);
     const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    return (m->dtype == HBF_BF16 ? launch_moe<Bf16>(d, n_sm, st) : launch_moe<Fp16>(d, n_sm, st)) == cudaSuccess ? HBF_OK : HBF_E_CUDA;
+    return (m->dtype == HBF_BF16 ? launch_moe<Bf16>(d, moe_few(m), n_sm, st) : launch_moe<Fp16>(d, moe_few(m), n_sm, st)) == cudaSuccess ? HBF_OK : HBF_E_CUDA;
 }
 
 extern "C" uint64_t hbf_moe_access_count(const hbf_moe_t *m, uint32_t tile_bytes) {
