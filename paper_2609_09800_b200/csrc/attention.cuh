@@ -22,6 +22,7 @@ struct AttnDev {
     // what a piece leaves: sums not yet divided, [piece][row][d], and (largest score, sum of weights), [piece][row]
     float *part_o; float2 *part_ml;
     uint32_t pieces;                                         // own_pieces + prefix_pieces of every row; 1: written straight to `out`
+    uint32_t behind;                                         // k_attend was launched to overlap k_prefix_tiles
 };
 
 // The place of key `i` of a table's sequence; false: its page is none of the cache's.
@@ -30,7 +31,6 @@ __device__ __forceinline__ bool key_place(const AttnDev &p, int32_t page, uint32
     return (uint32_t)page < p.n_pages;
 }
 
-// `behind`: launched so that it may begin while the kernel before it, of the same call, still runs.
-cudaError_t launch_prefix_tiles(const AttnDev &p, uint32_t dim, bool bf16, bool behind, cudaStream_t st);
+cudaError_t launch_prefix_tiles(const AttnDev &p, uint32_t dim, bool bf16, cudaStream_t st);
 
 }  // namespace hbf

@@ -230,12 +230,14 @@ k_attend(const __grid_constant__ AttnDev p) {
             if (col == 0u) p.part_ml[slot_out * rows + n] = make_float2(M, L);
         }
     }
+    // What joins the pieces waits for this kernel only: its last block ends after the prefix's.  (Not every block: they would keep their SMs.)
+    if (p.behind && blockIdx.x == gridDim.x - 1u) pdl_wait();
 }
 
 // Joins the rows' pieces: kPer warps a row.  First the pieces' shares of the whole, exp2(m - M), by a thread each; then their sums, four of a
 // warp's pieces on their way at a time.
 constexpr int kJoinWarps = 8;
-constexpr uint32_t kMostPieces = 1024;
+constexpr uint32_t kMostPieces = 1024;                      // of a row (attention_pieces makes fewer)
 template <class Ty, int D, int kPer>
 __global__ void __launch_bounds__(kJoinWarps * 32)
 k_attend_join(const __grid_constant__ AttnDev p) {
@@ -351,8 +353,14 @@ static bool attention_pointers_ok(const hbf_attention_t *a) {
     return true;
 }
 
-// Rows (of all requests, for one key head) up to which the prefix goes through k_attend, which reads it again, from L2, for every 16 rows.
-constexpr uint32_t kPrefixRowsSmall = 32u;
+// Whether the prefix goes through k_attend, which reads it again, from L2, for every 16 rows: while that is no more than kPrefixAgain bytes
+// in all, it costs less than the further launch and the longer start of k_prefix_tiles (8 MB: 12.1 to 14.1 us against 14.5 to 21.2; 32 MB 16.5
+// and 18.5 against 16.5 and 20.8; 64 MB 20.6, 21.4 and 20.6 against 18.5, 20.6 and 22.6; 192 MB 36.8 against 28.8).
+constexpr uint64_t kPrefixAgain = 48ull << 20;
+static bool prefix_small(const hbf_attention_t *a) {
+    const uint64_t rows = (uint64_t)a->batch * (a->q_heads / a->kv.kv_heads);
+    return rows <= 16u || (rows + 15u) / 16u * a->kv.kv_heads * a->prefix_len * a->kv.head_dim * 4u <= kPrefixAgain;
+}
 
 static uint32_t up_to(uint32_t v, uint32_t m) { return (v + m - 1u) / m * m; }
 
@@ -361,7 +369,7 @@ static uint32_t up_to(uint32_t v, uint32_t m) { return (v + m - 1u) / m * m; }
 // multiple of 64, at most 1,024 of a request's own (whose lengths differ).
 static void attention_pieces(const hbf_attention_t *a, uint32_t n_sm, AttnDev &p) {
     const uint32_t G = p.G, blocks = 2u * n_sm;
-    p.prefix_rows = p.B * G > kPrefixRowsSmall ? 256u : 16u;
+    p.prefix_rows = prefix_small(a) ? 16u : 256u;
     p.row_tiles = (p.B * G + p.prefix_rows - 1u) / p.prefix_rows;
     p.group_tiles = (G + 15u) / 16u;
     p.prefix_pieces = 0u; p.prefix_chunk = 64u;
@@ -411,21 +419,24 @@ template <class Ty, int D>
 static cudaError_t launch_attention(AttnDev p, bool bf16, cudaStream_t st) {
     const bool tiles = p.prefix_rows == 256u && p.n_prefix_items;
     AttnDev own = p;
-    if (tiles) own.n_prefix_items = 0u;
+    if (tiles) { own.n_prefix_items = 0u; own.behind = 1u; }
     const uint64_t items = own.n_prefix_items + (uint64_t)p.B * p.Hk * p.group_tiles * p.own_pieces;
     cudaError_t e = cudaSuccess;
+    // the requests' own keys go to the SMs that the prefix's blocks leave free, and to the others as those end
+    if (tiles && (e = launch_prefix_tiles(p, D, bf16, st)) != cudaSuccess) return e;
     if (items) {
         if ((e = ensure_dyn_smem((const void *)k_attend<Ty, D>, att_smem<D>())) != cudaSuccess) return e;
-        k_attend<Ty, D><<<(unsigned)items, kAttThreads, att_smem<D>(), st>>>(own);
+        if (tiles) e = launch_pdl(k_attend<Ty, D>, (unsigned)items, kAttThreads, att_smem<D>(), st, own);
+        else { k_attend<Ty, D><<<(unsigned)items, kAttThreads, att_smem<D>(), st>>>(own); e = cudaGetLastError(); }
         g_kernel_launches += 1;
-        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        if (e != cudaSuccess) return e;
     }
-    if (tiles && (e = launch_prefix_tiles(p, D, bf16, items != 0u, st)) != cudaSuccess) return e;
     if (p.pieces == 1u) return e;
     g_kernel_launches += 1;
-    const bool few = p.pieces <= 32u;                        // 64 requests, 18 pieces each: two warps a row 5.3 us, eight 10.1
-    const auto join = few ? k_attend_join<Ty, D, 2> : k_attend_join<Ty, D, kJoinWarps>;
-    const uint32_t blocks = few ? (p.B * p.Hq + kJoinWarps / 2 - 1u) / (kJoinWarps / 2) : p.B * p.Hq;
+    // many rows: two warps each (64 requests, 17 pieces a row: 43.1 us, with eight 45.1), else eight
+    const uint32_t per = p.B * p.Hq >= 1024u && p.pieces <= kMostPieces / 4u ? 2u : kJoinWarps, rows = kJoinWarps / per;
+    const auto join = per == 2u ? k_attend_join<Ty, D, 2> : k_attend_join<Ty, D, kJoinWarps>;
+    const uint32_t blocks = (p.B * p.Hq + rows - 1u) / rows;
     if (p.pieces == 0u) { join<<<blocks, kJoinWarps * 32, 0, st>>>(p); return cudaGetLastError(); }
     return launch_pdl(join, blocks, kJoinWarps * 32, 0, st, p);
 }

@@ -104,7 +104,6 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
         // boxes of `box` slots (0: none): whole tiles; warp w takes the boxes w, w + 4, ...
         const uint32_t whole = box ? (end - begin) / kPfTile : 0u, boxes = box ? kPfTile / box : 0u, my_boxes = boxes > w4 ? (boxes - w4 + 3u) / 4u : 0u;
         if (whole) {
-            copy_wait<0>(); arrive(smem_addr(&sh.q_full));
             int32_t page = 0;                                // lane l: that of this warp's box l
             uint32_t slot0 = 0u;
             auto look = [&](uint32_t i) {
@@ -134,6 +133,7 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
                             for (int x = 0; x < D / 64; ++x) tensor_copy(dst + x * 16384u, kv ? &v_map : &k_map, x * 64, sl, (int32_t)head, pg, full);
                         }
                     }
+                    if (n == 0u) { copy_wait<0>(); arrive(smem_addr(&sh.q_full)); }
                 }
             }
         }
@@ -344,7 +344,6 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
             tensor_fence_before();
         }
     }
-    pdl_wait();                                              // a kernel behind this one counts on what came before it, too
     __syncthreads();
     __syncwarp();
     if (warp == 20u) {
@@ -366,7 +365,7 @@ static bool cache_map(CUtensorMap *map, const AttnDev &p, const uint16_t *base, 
 }
 
 template <class Ty, int D, bool kBf16>
-static cudaError_t launch_tiles(const AttnDev &p, bool behind, cudaStream_t st) {
+static cudaError_t launch_tiles(const AttnDev &p, cudaStream_t st) {
     const auto k = k_prefix_tiles<Ty, D, kBf16>;
     cudaError_t e = ensure_dyn_smem((const void *)k, pf_smem<D>());
     if (e != cudaSuccess) return e;
@@ -375,13 +374,12 @@ static cudaError_t launch_tiles(const AttnDev &p, bool behind, cudaStream_t st) 
     uint32_t box = p.page_tokens & (0u - p.page_tokens);     // the largest power of two that a page is a multiple of
     if (box > (uint32_t)kPfTile) box = kPfTile;
     if (box < 8u || !cache_map(&k_map, p, p.k, D, kBf16, box) || !cache_map(&v_map, p, p.v, D, kBf16, box)) box = 0u;
-    if (behind) return launch_pdl(k, p.n_prefix_items, kPfThreads, pf_smem<D>(), st, p, k_map, v_map, box);
     k<<<p.n_prefix_items, kPfThreads, pf_smem<D>(), st>>>(p, k_map, v_map, box);
     return cudaGetLastError();
 }
-cudaError_t launch_prefix_tiles(const AttnDev &p, uint32_t dim, bool bf16, bool behind, cudaStream_t st) {
-    if (bf16) return dim == 128u ? launch_tiles<Bf16, 128, true>(p, behind, st) : launch_tiles<Bf16, 64, true>(p, behind, st);
-    return dim == 128u ? launch_tiles<Fp16, 128, false>(p, behind, st) : launch_tiles<Fp16, 64, false>(p, behind, st);
+cudaError_t launch_prefix_tiles(const AttnDev &p, uint32_t dim, bool bf16, cudaStream_t st) {
+    if (bf16) return dim == 128u ? launch_tiles<Bf16, 128, true>(p, st) : launch_tiles<Bf16, 64, true>(p, st);
+    return dim == 128u ? launch_tiles<Fp16, 128, false>(p, st) : launch_tiles<Fp16, 64, false>(p, st);
 }
 
 }  // namespace hbf

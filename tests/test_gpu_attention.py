@@ -3,7 +3,8 @@
 Tolerance, from the arithmetic.  With eps the type's spacing at 1: the output is rounded once, eps / 2 of its magnitude.  A weight p is
 exp2 of a score in 32 bits: the score's sum of d products is off by at most (d + 8) * 2^-23 of the sum S of their magnitudes (times the
 scale), which is the weight's relative error up to second order, and exp2, the running rescales and the sums add some 2^-18.  Weights enter the
-second product as two numbers of the type, leaving (eps / 2)^2, or, where a tile of 128 rows goes through tensor memory, as one, leaving eps / 2.
+second product as two numbers of the type, leaving 2 (eps / 2)^2 (the first is rounded down, so up to eps is left for the second), or, where a tile of 128 rows goes through
+tensor memory, as one, leaving eps / 2.
 All of these multiply A = sum p |v|, for the numerator and once more for the denominator."""
 import math
 
@@ -97,7 +98,7 @@ class Case:
         torch = self.torch
         want, want_lse, A, S = self.expect(scale, q)
         half = torch.finfo(self.dt).eps / 2
-        weight = half if self.B * (self.Hq // self.Hk) > 32 else half * half
+        weight = half if self.B * (self.Hq // self.Hk) > 16 else 2 * half * half
         rel = weight + 2 * (self.d + 8) * 2.0 ** -23 * S + 2.0 ** -18
         tol = half * want.abs() + (1 + half) * A * rel[..., None] + torch.finfo(self.dt).tiny
         err = (out.double() - want).abs()
@@ -126,6 +127,95 @@ def test_against_64_bits(torch, serving, shape, dtype):
     c = Case(torch, *shape, dtype=dtype, seed=sum(shape))
     lse = torch.empty(c.B, c.Hq, device="cuda")
     c.check(c.plan(serving)(c.q, lse=lse), lse)
+
+
+# enough rows and keys for the prefix to go through tensor memory: pages that copies fetch whole, pages that they cannot, one tile of rows in the
+# last pair, the prefix's end in a tile and on its border, a single piece
+WIDE = [(128, 32, 4, 128, 16, 512, 20), (128, 32, 4, 128, 64, 700, 0), (101, 32, 4, 128, 12, 640, 9), (128, 32, 4, 64, 8, 1000, 30), (128, 64, 4, 64, 1, 513, 3),
+        (120, 40, 8, 64, 100, 640, 11), (128, 16, 1, 128, 24, 1500, 5), (16, 128, 8, 128, 256, 999, 33), (128, 128, 8, 64, 16, 385, 2), (67, 32, 1, 128, 16, 3000, 0)]
+
+
+@pytest.mark.parametrize("shape", WIDE, ids=["x".join(map(str, s)) for s in WIDE])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_wide_against_64_bits(torch, serving, shape, dtype):
+    c = Case(torch, *shape, dtype=dtype, seed=sum(shape))
+    lse = torch.empty(c.B, c.Hq, device="cuda")
+    c.check(c.plan(serving)(c.q, lse=lse), lse)
+
+
+@pytest.mark.parametrize("layout", ["heads", "gaps"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_wide_page_layouts(torch, serving, layout, d):
+    c = Case(torch, 128, 32, 4, d, 16, 900, 12, seed=5, layout=layout)
+    x = c.q.clone()
+    c.plan(serving)(x, x)                                    # in place, too
+    c.check(x)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_wide_scales_and_rising_scores(torch, serving, d):
+    c = Case(torch, 128, 16, 2, d, 16, 1601, 30, k_scale=4.0)
+    for scale in (0.5, -0.25, 0.0):
+        c.check(c.plan(serving, scale=scale)(c.q), scale=scale)
+    c = Case(torch, 128, 16, 2, d, 16, 1600, 10, lens=[10] * 128)
+    ramp = torch.linspace(0.01, 6.0, 1600, device="cuda").view(100, 16, 1, 1)
+    c.k[c.pp.long()] = (c.q[0, 0].sign() * ramp).to(c.dt)
+    c.check(c.plan(serving)(c.q))
+
+
+@pytest.mark.parametrize("page", [16, 12])
+def test_wide_nan_infinity_and_pages_that_are_none(torch, serving, page):
+    mk = lambda: Case(torch, 128, 32, 4, 128, page, 640, 12, lens=[12] * 128, poison=False)
+    c = mk()
+    clean = c.plan(serving)(c.q)
+    c.v[c.pp[2].long(), 3, 1, 5] = math.inf
+    out = c.plan(serving)(c.q)
+    assert torch.isinf(out[:, 8:16, 5]).all() and torch.equal(out[:, :8], clean[:, :8]) and torch.equal(out[:, 16:], clean[:, 16:])
+    c = mk()
+    c.k[c.pp[30].long(), 0, 2] = math.nan
+    out = c.plan(serving)(c.q)
+    assert torch.isnan(out[:, 16:24]).all() and torch.equal(out[:, :16], clean[:, :16])
+    c = mk()
+    c.q[7, 9, 3] = math.inf
+    out = c.plan(serving)(c.q)
+    assert torch.isnan(out[7, 9]).all() and torch.equal(out[8:], clean[8:])
+    for bad in (-1, 1 << 30):
+        c = mk()
+        c.pp[20] = bad
+        assert torch.isnan(c.plan(serving)(c.q)).all()
+    c = mk()
+    c.lens[3] = 13
+    out = c.plan(serving)(c.q)
+    assert torch.isnan(out[3]).all() and torch.equal(out[4:], clean[4:])
+
+
+def test_wide_captured_and_on_two_streams(torch, serving):
+    cases = [Case(torch, 128, 16, 2, 128, 16, 1700, 64, seed=s, poison=False) for s in range(2)]
+    streams = [torch.cuda.Stream() for _ in cases]
+    plans = [c.plan(serving, stream=s) for c, s in zip(cases, streams)]
+    outs = [torch.empty_like(c.q) for c in cases]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c, p, o in zip(cases, plans, outs):
+            p(c.q, o)
+    torch.cuda.synchronize()
+    for c, o in zip(cases, outs):
+        c.check(o)
+    c, plan, out, st = cases[0], plans[0], outs[0], streams[0]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        plan(c.q, out)
+    for turn in range(2):
+        c.lens.copy_(torch.randint(0, 65, c.lens.shape, device="cuda")); c.q.mul_(-1.0); out.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(st):
+            graph.replay()
+        torch.cuda.synchronize()
+        c.check(out)
+        first = out.clone()
+        plan(c.q, out)
+        torch.cuda.synchronize()
+        assert torch.equal(first, out)
 
 
 @pytest.mark.parametrize("layout", ["heads", "gaps"])

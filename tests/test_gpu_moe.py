@@ -92,7 +92,7 @@ SHAPES = [
     # T, D, I, E, K
     (1, 8, 8, 1, 1), (1, 2048, 768, 16, 8), (2, 64, 32, 2, 2), (3, 1000, 520, 12, 3), (5, 72, 200, 40, 16), (8, 512, 1024, 8, 2), (9, 256, 128, 3, 1),
     (17, 4096, 64, 9, 4), (33, 128, 40, 2, 2), (40, 136, 264, 4, 4), (64, 2048, 768, 16, 8), (65, 264, 72, 512, 16), (100, 512, 24, 5, 1), (128, 384, 96, 3, 3),
-    (128, 2400, 64, 6, 2), (7, 8, 2048, 33, 5), (128, 64, 64, 1, 1),
+    (128, 2400, 64, 6, 2), (7, 8, 2048, 33, 5), (128, 64, 64, 1, 1), (8, 2048, 1024, 24, 8), (3, 4096, 2048, 6, 2), (16, 20000, 16, 3, 2),
 ]
 
 
