@@ -73,12 +73,13 @@ def parse_args():
     ap.add_argument("--no-configs", action="store_true", help="skip the per-configuration block (other streams, coupled run)")
     ap.add_argument("--shuffle", action="store_true", help="submit the records in a random order: the sort path has to serve the batch")
     ap.add_argument("--profile", default="nominal", choices=["nominal", "aggressive"], help="timing profile of the coupled_thermal run")
-    ap.add_argument("--workload", default="capacity_mode", choices=["capacity_mode", "coupled_thermal", "capacity_paged", "rom", "capacity_retention"],
+    ap.add_argument("--workload", default="capacity_mode", choices=["capacity_mode", "coupled_thermal", "capacity_paged", "rom", "capacity_retention", "served_layer"],
                     help="coupled_thermal: the prefix-KV stream in 1 ms batches, each followed by a thermal step; "
                          "capacity_paged: the capacity-mode batch through the page-granular submit; rom: fit the reduced-order "
                          "thermal model of the package floorplan and time its step against the full grid; capacity_retention: the "
                          "capacity-mode batch with retention on: a batch without debt, an epoch (damage, eligibility, plan), the "
-                         "same batch paying refresh claims (none is the headline)")
+                         "same batch paying refresh claims; served_layer: one layer of the shared-prefix decode executed on memory "
+                         "in registered ranges, its own accesses served (none is the headline)")
     ap.add_argument("--horizon-ms", type=int, default=1000, help="simulated time of the coupled_thermal run")
     ap.add_argument("--channel-bus", action="store_true",
                     help="capacity_mode: also run the channel-bus stage (reads' transfers queue per channel); not the headline")
@@ -582,6 +583,47 @@ def run_rom(args):
                       "full_grid_us_per_step": grid_us, "rom_us_per_step": rom_us, "model_vs_grid": errs}), flush=True)
 
 
+def run_served(args):
+    """One layer of the shared-prefix decode at batch 64, executed (attention over the 8K-token prefix and the requests' own keys, top-8 of 128
+    experts), and the accesses that it makes served by the model: microseconds of each part, accesses a step, stalls."""
+    import torch
+    from paper_2609_09800_b200 import build as hbf_build, hbf, serving
+    hbf_build.build()
+    ctx = hbf.Context(wl.load_profile("nominal", **wl.GEOMETRY["serving"]))
+    batch = 64
+    layer = serving.ServedLayer(ctx, batch=batch, prefix_tokens=wl.KV_TOKENS, own_tokens=512, hidden=wl.HIDDEN, inter=wl.EXPERT_INTER, n_experts=wl.N_EXPERTS, top_k=wl.TOP_K)
+    g = torch.Generator(device="cuda"); g.manual_seed(1)
+    rnd = lambda *s: torch.randn(*s, device="cuda", generator=g)
+    q, x, scores = rnd(batch, 32, 128).bfloat16(), rnd(batch, wl.HIDDEN).bfloat16(), rnd(wl.N_EXPERTS) * 0.7 + rnd(batch, wl.N_EXPERTS)
+    for _ in range(448):
+        layer.append(rnd(batch, 4, 128).bfloat16(), rnd(batch, 4, 128).bfloat16())
+    ev = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+
+    def timed(f):
+        for _ in range(args.warmup):
+            f()
+        torch.cuda.synchronize(); ev[0].record()
+        for _ in range(args.steps):
+            f()
+        ev[1].record(); torch.cuda.synchronize()
+        return ev[0].elapsed_time(ev[1]) * 1e3 / args.steps
+
+    gap = 20                                                  # ns between the accesses of a step
+    o, y = torch.empty_like(q), torch.empty_like(x)
+    attention_us, moe_us = timed(lambda: layer.attention(q, o)), timed(lambda: layer.moe(x, scores, y))
+    step_us = timed(lambda: (ctx.reset(), layer.step(q, x, scores, 0, gap)))
+    ctx.reset()
+    _, _, served = layer.step(q, x, scores, 0, gap)
+    res = ctx.last_result()
+    n = sum(int(s[0].shape[0]) for s in served)
+    modeled = sum(int((s[0][:, 0] != 0).sum()) for s in served)
+    print(json.dumps({"metric": "executed layer steps/s, accesses served", "value": 1e6 / step_us, "unit": "steps/s", "n_gpus": 1, "steps": args.steps,
+                      "warmup": args.warmup, "ms_per_step": step_us * 1e-3, "higher_is_better": True, "dtype": "bf16", "data": "synthetic",
+                      "config": {"workload": "served_layer", "batch": batch, "prefix_tokens": wl.KV_TOKENS, "own_tokens": 448, "experts": wl.N_EXPERTS,
+                                 "attention_us": round(attention_us, 2), "experts_us": round(moe_us, 2), "records": n, "accesses": modeled,
+                                 "mean_stall_ns": round(sum(float(s[2].sum()) for s in served) / max(1, modeled), 1), "code": res["code"]}}))
+
+
 def main():
     args = parse_args()
     rank = int(os.environ.get("RANK", "0"))
@@ -605,6 +647,10 @@ def main():
     if args.workload == "coupled_thermal":
         if rank == 0:
             run_coupled(args)
+        return
+    if args.workload == "served_layer":
+        if rank == 0:
+            run_served(args)
         return
 
     import torch

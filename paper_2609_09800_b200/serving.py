@@ -260,3 +260,72 @@ class CachePages(_Operator):
         out = self._records(n) if out is None else out
         self._raise(self._lib.hbf_pages_accesses(self._ref, self._ws_ptr, issue_ns, gap_ns, out.data_ptr(), n, self._st) if n else 0, "hbf_pages_accesses")
         return out
+
+
+class ServedLayer:
+    """One layer of the model that the streams ``decode_weights`` and ``prefix_kv`` stand for (``workloads``), executed: its experts and its
+    key/value cache lie in ranges registered with a context, and every step serves the accesses that its operators make.
+
+    Row 0 of the cache holds the shared prefix; the requests, rows 1 to batch, are forked from it, so that they share its full pages and
+    begin with a copy of a page that it had begun; each then has room for own_tokens more.  Values are random (seed)."""
+
+    def __init__(self, ctx, batch=64, prefix_tokens=8192, own_tokens=64, page_tokens=16, hidden=2048, inter=768, n_experts=128, top_k=8, q_heads=32,
+                 kv_heads=4, head_dim=128, seed=0):
+        import torch
+        self.ctx, self.batch, self.page = ctx, batch, page_tokens
+        with torch.cuda.stream(ctx.stream):
+            dev = torch.device("cuda", torch.cuda.current_device())
+            g = torch.Generator(device=dev)
+            g.manual_seed(seed)
+            rnd = lambda *s: torch.randn(*s, device=dev, dtype=torch.bfloat16, generator=g)
+            self.experts = rnd(n_experts, 3 * inter * hidden) * hidden ** -0.5
+            full, started = divmod(prefix_tokens, page_tokens)
+            mine = -(-(started + own_tokens) // page_tokens)      # pages of a request behind the full ones that it shares
+            held = full + (1 if started else 0)
+            pages = held + batch * mine + 1
+            self.kv = rnd(2, pages, page_tokens, kv_heads, head_dim)
+            i32 = lambda *s: torch.full(s, -1, dtype=torch.int32, device=dev)
+            self.refs, self.lens, self.tables = i32(pages).fill_(0), i32(batch + 1).fill_(0), i32(batch + 1, full + mine + 1)
+            self.tables[0, :held] = torch.arange(held, device=dev, dtype=torch.int32)
+            self.refs[:held] = 1
+            self.lens[0] = prefix_tokens
+            self.own_len = torch.zeros(batch, dtype=torch.int32, device=dev)
+            self._rows = torch.arange(1, batch + 1, device=dev, dtype=torch.int32)
+        self.cache = CachePages(self.kv, self.refs, self.tables, self.lens, page_tokens, stream=ctx.stream)
+        self.cache.fork(torch.zeros_like(self._rows), self._rows)
+        self.cache.result()
+        with torch.cuda.stream(ctx.stream):                       # the pages that the requests will grow into, the lowest free ones
+            free = torch.nonzero(self.refs == 0).flatten().to(torch.int32)
+            more = mine - (1 if started else 0)
+            grow = free[:batch * more].view(batch, more)
+            self.tables[1:, full + (1 if started else 0):full + mine] = grow
+            self.refs[grow.flatten().long()] = 1
+            self.base_tokens = full * page_tokens
+        self.attention = PrefixAttention(self.kv[0], self.kv[1], batch, q_heads, self.tables[0, :full].contiguous() if full else None, self.base_tokens,
+                                         self.tables[1:, full:], self.own_len, mine * page_tokens, stream=ctx.stream)
+        self.moe = MoeLayer(self.experts, hidden, inter, top_k, batch, stream=ctx.stream)
+        offset = 0
+        for t in (self.experts, self.kv):                         # one range each, side by side on the media
+            ctx.register_range(t.data_ptr(), t.numel() * t.element_size(), 3, 0, 0, offset)
+            offset += -(-t.numel() * t.element_size() // (1 << 20)) << 20
+
+    def append(self, k, v):
+        """Every request's next token: k, v [batch, kv_heads, head_dim] go into its cache."""
+        import torch
+        with torch.cuda.stream(self.ctx.stream):
+            at = self.lens[1:].long()
+            page = self.tables[1:].gather(1, (at // self.page)[:, None])[:, 0].long()
+            self.kv[0, page, at % self.page], self.kv[1, page, at % self.page] = k, v
+            self.lens[1:] += 1
+
+    def step(self, q, x, scores, issue_ns=0, gap_ns=0):
+        """Attention of the requests' queries q [batch, q_heads, head_dim], then the experts on x [batch, hidden] by the router's scores [batch,
+        n_experts].  Returns (attention's output, experts' output, [what ``Context.serve`` returns for each])."""
+        import torch
+        with torch.cuda.stream(self.ctx.stream):
+            torch.sub(self.lens[1:], self.base_tokens, out=self.own_len)
+        o = self.attention(q)
+        a = self.ctx.serve(self.attention, issue_ns, gap_ns)
+        y = self.moe(x, scores)
+        b = self.ctx.serve(self.moe, issue_ns + gap_ns * a[0].shape[0], gap_ns)
+        return o, y, [a, b]
