@@ -234,14 +234,14 @@ k_attend(const __grid_constant__ AttnDev p) {
     if (p.behind && blockIdx.x == gridDim.x - 1u) pdl_wait();
 }
 
-// Joins the rows' pieces: kPer warps a row.  First the pieces' shares of the whole, exp2(m - M), by a thread each; then their sums, four of a
-// warp's pieces on their way at a time.
+// Joins the rows' pieces: kPer warps a row.  First the pieces' shares of the whole, exp2(m - M), by a thread each; then their sums, four or eight
+// of a warp's pieces on their way at a time.
 constexpr int kJoinWarps = 8;
 constexpr uint32_t kMostPieces = 1024;                      // of a row (attention_pieces makes fewer)
 template <class Ty, int D, int kPer>
 __global__ void __launch_bounds__(kJoinWarps * 32)
 k_attend_join(const __grid_constant__ AttnDev p) {
-    constexpr int kRows = kJoinWarps / kPer, kEach = D / 32;
+    constexpr int kRows = kJoinWarps / kPer, kEach = D / 32, kOn = kPer == kJoinWarps ? 8 : 4;
     __shared__ float share[kRows][kMostPieces / kRows], red[kJoinWarps][2], so[kJoinWarps][D];
     const uint32_t lane = lane_id(), warp = threadIdx.x >> 5, group = warp / kPer, part = warp % kPer;
     const size_t rows = (size_t)p.B * p.Hq;
@@ -277,10 +277,10 @@ k_attend_join(const __grid_constant__ AttnDev p) {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) v[i] = 0.0f;
     if (there)
-        for (uint32_t s0 = part; s0 < p.pieces; s0 += kPer * 4u) {
-            float x[4][kEach], g[4];
+        for (uint32_t s0 = part; s0 < p.pieces; s0 += kPer * kOn) {
+            float x[kOn][kEach], g[kOn];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < kOn; ++k) {
                 const uint32_t s = s0 + k * kPer;
                 g[k] = s < p.pieces ? exp2_fast(f[s] - z) : 0.0f;
                 const float *from = p.part_o + (s * rows + n) * D + lane * kEach;
@@ -292,7 +292,7 @@ k_attend_join(const __grid_constant__ AttnDev p) {
                 }
             }
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
+            for (int k = 0; k < kOn; ++k)
 #pragma unroll
                 for (int i = 0; i < kEach; ++i) v[i] += g[k] * x[k][i];
         }

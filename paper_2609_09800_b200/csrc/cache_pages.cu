@@ -107,6 +107,17 @@ __device__ __forceinline__ void apply_plan(const PagesDev &p, const int32_t *a, 
         }
         for (uint64_t k = first; k < moves; k += step) { p.refs[p.dst[k]] = p.refs[p.src[k]]; p.refs[p.src[k]] = 0; }
     }
+    if (kThreads == (uint32_t)kPlanThreads) {                // the plan's block by itself: 16 bytes a thread of all that moves
+        const uint32_t n16 = (uint32_t)(p.page_bytes / 16u), all = moves * p.n_slabs * n16;
+#pragma unroll 4
+        for (uint32_t i = threadIdx.x; i < all; i += kThreads) {
+            const uint32_t u = i / n16, k = div32(u, p.div_slabs);
+            const uint64_t at = (uint64_t)(u - k * p.n_slabs) * p.slab_stride + (uint64_t)(i - u * n16) * 16u;
+            const uint4 v = *reinterpret_cast<const uint4 *>(p.base + at + (uint64_t)p.src[k] * p.page_stride);
+            *reinterpret_cast<uint4 *>(p.base + at + (uint64_t)p.dst[k] * p.page_stride) = v;
+        }
+        return;
+    }
     const uint32_t units = moves * p.n_slabs;
     for (uint32_t u = blockIdx.x; u < units; u += gridDim.x) {
         const uint32_t k = div32(u, p.div_slabs), s = u - k * p.n_slabs;
@@ -359,9 +370,8 @@ static int pages_call(const hbf_pages_t *p, const int32_t *a, const int32_t *b, 
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const size_t smem = ((size_t)mark_bits + 31u) / 32u * 4u;
     if (ensure_dyn_smem((const void *)plan, smem) != cudaSuccess) return HBF_E_CUDA;
-    // without pages to move, and with up to 32 entries a thread, one block is done before a second kernel would have begun (with pages it is
-    // not: three forks of 4 KB pages in four slabs took 14 us, with two kernels 10)
-    const int alone = most_moves == 0u && entries <= 32u * kPlanThreads;
+    // up to 128 KB to move and 32 entries a thread, one block is done about when a second kernel would begin
+    const int alone = most_moves * p->n_slabs * p->page_bytes <= 128u * 1024u && entries <= 32u * kPlanThreads;
     plan<<<1, kPlanThreads, smem, st>>>(d, args..., alone);
     if (cudaGetLastError() != cudaSuccess) return HBF_E_CUDA;
     if (alone) { g_kernel_launches += 1; return HBF_OK; }

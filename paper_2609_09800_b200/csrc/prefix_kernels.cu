@@ -317,24 +317,48 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
             const uint32_t b = n / p.G, h = head * p.G + (n - b * p.G);
             const size_t rows = (size_t)p.B * p.Hq, at = (size_t)(p.own_pieces + piece) * rows + (size_t)b * p.Hq + h;
             const float z = m - lift, inv = l == 0.0f ? 0.0f : 1.0f / l;
+            if (p.pieces == 1u) {
 #pragma unroll
-            for (int c = 0; c < D / 32; ++c) {
-                uint32_t v[16];
-                __syncwarp();
-                tensor_load16(o_at + c * 16u, v);
-                if (mine && p.pieces == 1u) {
-                    uint4 *to = reinterpret_cast<uint4 *>(p.out + (int64_t)b * p.out_row + (int64_t)h * p.out_head + half * (D / 2) + c * 16);
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t v[16];
+                    __syncwarp();
+                    tensor_load16(o_at + c * 16u, v);
+                    if (mine) {
+                        uint4 *to = reinterpret_cast<uint4 *>(p.out + (int64_t)b * p.out_row + (int64_t)h * p.out_head + half * (D / 2) + c * 16);
 #pragma unroll
-                    for (int k = 0; k < 16; k += 8) {
-                        uint32_t w[4];
+                        for (int k = 0; k < 16; k += 8) {
+                            uint32_t w[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) w[e] = l == 0.0f ? 0u : Ty::pack(__uint_as_float(v[k + 2 * e]) * inv, __uint_as_float(v[k + 2 * e + 1]) * inv);
-                        to[k / 8] = make_uint4(w[0], w[1], w[2], w[3]);
+                            for (int e = 0; e < 4; ++e) w[e] = l == 0.0f ? 0u : Ty::pack(__uint_as_float(v[k + 2 * e]) * inv, __uint_as_float(v[k + 2 * e + 1]) * inv);
+                            to[k / 8] = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
                     }
-                } else if (mine) {
-                    uint4 *to = reinterpret_cast<uint4 *>(p.part_o + at * D + half * (D / 2) + c * 16);
+                }
+            } else {
+                // Through shared memory, the queries' now that the products are done: a warp's rows by itself, so that whole lines are written.
+                constexpr uint32_t kCols = D / 4, kChunks = D / 16, kAtOnce = 32u / kChunks;      // columns a turn; 16 bytes each; rows a store
+                const uint32_t own = q_at + t * kBytes + (warp & 7u) * (32u * D), chunk = lane % kChunks;
 #pragma unroll
-                    for (int k = 0; k < 16; k += 4) to[k / 4] = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+                for (uint32_t c = 0; c < (D / 2) / kCols; ++c) {
+                    __syncwarp();
+#pragma unroll
+                    for (uint32_t k = 0; k < kCols; k += 16u) {
+                        uint32_t v[16];
+                        tensor_load16(o_at + c * kCols + k, v);
+#pragma unroll
+                        for (uint32_t e = 0; e < 4u; ++e)
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(own + lane * D + (((k / 4u + e) ^ (lane % kChunks)) * 16u)),
+                                         "r"(v[4 * e]), "r"(v[4 * e + 1]), "r"(v[4 * e + 2]), "r"(v[4 * e + 3]) : "memory");
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (uint32_t k = 0; k < 32u; k += kAtOnce) {
+                        const uint32_t from = k + lane / kChunks;
+                        const bool there = __shfl_sync(0xffffffffu, mine ? 1 : 0, from) != 0;
+                        const uint64_t row = __shfl_sync(0xffffffffu, (unsigned long long)at, from);
+                        const uint4 v = ld_shared16(own + from * D + ((chunk ^ (from % kChunks)) * 16u));
+                        if (there) *reinterpret_cast<uint4 *>(p.part_o + row * D + half * (D / 2) + c * kCols + chunk * 4u) = v;
+                    }
                 }
             }
             if (mine && half == 0u) {

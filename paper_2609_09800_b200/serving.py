@@ -30,6 +30,7 @@ class _Operator:
         self.stream = stream if stream is not None else torch.cuda.current_stream()
         _check(self.stream.device == self.device, "the stream belongs to another device")
         self._st = self.stream.cuda_stream
+        self._dev, self._i32, self._f32 = self.device.index, torch.int32, torch.float32
 
     def _int32(self, t, what, dims):
         _check(t.dtype == self._torch.int32 and t.dim() == dims and t.device == self.device and (t.numel() == 0 or t.stride(-1) == 1),
@@ -97,15 +98,15 @@ class PrefixAttention(_Operator):
         if out is None:
             with self._torch.cuda.stream(self.stream):
                 out = self._torch.empty(self._shape, dtype=self._dtype, device=self.device)
-        for t in (q, out):
-            if t.shape != self._shape or t.dtype != self._dtype or t.device != self.device or t.stride(2) != 1:
-                raise ValueError("q and out have to be [batch, q_heads, head_dim] of the cache's type, dense in the last dimension")
+        qs, os = q.stride(), out.stride()
+        if q.shape != self._shape or out.shape != self._shape or q.dtype is not self._dtype or out.dtype is not self._dtype or qs[2] != 1 or os[2] != 1 or \
+                q.get_device() != self._dev or out.get_device() != self._dev:
+            raise ValueError("q and out have to be [batch, q_heads, head_dim] of the cache's type, dense in the last dimension")
         if lse is not None:
             _check(lse.shape == self._shape[:2] and lse.dtype == self._torch.float32 and lse.device == self.device and lse.is_contiguous(), "lse has to be float32 [batch, q_heads]")
         a = self._a
         a.q, a.out, a.lse = q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr()
-        a.q_row_stride, a.q_head_stride, _ = q.stride()
-        a.out_row_stride, a.out_head_stride, _ = out.stride()
+        a.q_row_stride, a.q_head_stride, a.out_row_stride, a.out_head_stride = qs[0], qs[1], os[0], os[1]
         rc = self._lib.hbf_prefix_attention(self._ref, self._ws_ptr, self._ws_bytes, self._st)
         if rc:
             self._raise(rc, "hbf_prefix_attention")
@@ -150,19 +151,20 @@ class MoeLayer(_Operator):
         if out is None:
             with torch.cuda.stream(self.stream):
                 out = torch.empty(x.shape, dtype=self._dtype, device=self.device)
-        n = x.shape[0]
-        for t in (x, out):
-            if t.dim() != 2 or t.shape[0] != n or t.shape[1] != m.hidden or n > self.max_tokens or t.dtype != self._dtype or t.device != self.device or t.stride(1) != 1:
-                raise ValueError("x and out have to be [tokens <= max_tokens, hidden] of the experts' type, rows dense")
-        if scores.shape != (n, m.n_experts) or scores.dtype != torch.float32 or scores.device != self.device or scores.stride(1) != 1:
+        n, want, dev = x.shape[0], (x.shape[0], m.hidden), self._dev
+        xs, os, ss = x.stride(), out.stride(), scores.stride()
+        if n > self.max_tokens or x.shape != want or out.shape != want or x.dtype is not self._dtype or out.dtype is not self._dtype or xs[1] != 1 or os[1] != 1 or \
+                x.get_device() != dev or out.get_device() != dev:
+            raise ValueError("x and out have to be [tokens <= max_tokens, hidden] of the experts' type, rows dense")
+        if scores.shape != (n, m.n_experts) or scores.dtype is not self._f32 or scores.get_device() != dev or ss[1] != 1:
             raise ValueError("scores has to be float32 [tokens, n_experts], rows dense")
-        for t, dt in ((chosen, torch.int32), (weights, torch.float32)):
-            if t is not None and (t.shape != (n, m.top_k) or t.dtype != dt or t.device != self.device or not t.is_contiguous()):
+        for t, dt in ((chosen, self._i32), (weights, self._f32)):
+            if t is not None and (t.shape != (n, m.top_k) or t.dtype is not dt or t.get_device() != dev or not t.is_contiguous()):
                 raise ValueError("chosen (int32) and weights (float32) have to be [tokens, top_k], contiguous")
         m.tokens = n
-        m.x, m.x_stride = x.data_ptr(), x.stride(0) if n > 1 else m.hidden
-        m.scores, m.scores_stride = scores.data_ptr(), scores.stride(0) if n > 1 else m.n_experts
-        m.out, m.out_stride = out.data_ptr(), out.stride(0) if n > 1 else m.hidden
+        m.x, m.x_stride = x.data_ptr(), xs[0] if n > 1 else m.hidden
+        m.scores, m.scores_stride = scores.data_ptr(), ss[0] if n > 1 else m.n_experts
+        m.out, m.out_stride = out.data_ptr(), os[0] if n > 1 else m.hidden
         m.chosen, m.weights = None if chosen is None else chosen.data_ptr(), None if weights is None else weights.data_ptr()
         rc = self._lib.hbf_moe_layer(self._ref, self._ws_ptr, self._ws_bytes, self._st)
         if rc:
@@ -212,7 +214,7 @@ class CachePages(_Operator):
         self._what, self._moves = "", 0
 
     def _list(self, t, what):
-        if t.dtype != self._torch.int32 or t.dim() != 1 or t.device != self.device or not t.is_contiguous():
+        if t.dtype is not self._i32 or t.dim() != 1 or t.get_device() != self._dev or not t.is_contiguous():
             raise ValueError("%s has to be a contiguous int32 tensor of one dimension on %s" % (what, self.device))
         return t.data_ptr()
 
