@@ -8,7 +8,7 @@ struct AttnDev {
     const uint16_t *k, *v;
     int64_t page_stride, slot_stride, head_stride;
     uint32_t n_pages, Hk, G, Hq, B;
-    Div32 div_page;
+    Div32 div_page, div_g;
     uint32_t page_tokens;
     const uint16_t *q; int64_t q_row, q_head;
     uint16_t *out; int64_t out_row, out_head;

@@ -52,7 +52,7 @@ k_attend(const __grid_constant__ AttnDev p) {
     }
     // row r of the tile: request and query head
     auto place = [&](uint32_t r, uint32_t &rb, uint32_t &rh) {
-        if (shared) { const uint32_t n = tile * 16u + r; rb = n / p.G; rh = head * p.G + n % p.G; }
+        if (shared) { const uint32_t n = tile * 16u + r; rb = div32(n, p.div_g); rh = head * p.G + n - rb * p.G; }
         else { rb = b; rh = head * p.G + tile * 16u + r; }
     };
 
@@ -401,7 +401,7 @@ static AttnDev attention_dev(const hbf_attention_t *a, uint32_t n_sm) {
     p.k = static_cast<const uint16_t *>(a->kv.k); p.v = static_cast<const uint16_t *>(a->kv.v);
     p.page_stride = a->kv.page_stride; p.slot_stride = a->kv.slot_stride; p.head_stride = a->kv.head_stride;
     p.n_pages = a->kv.n_pages; p.Hk = a->kv.kv_heads; p.Hq = a->q_heads; p.G = p.Hq / p.Hk; p.B = a->batch;
-    p.page_tokens = a->kv.page_tokens; p.div_page = make_div32(p.page_tokens);
+    p.page_tokens = a->kv.page_tokens; p.div_page = make_div32(p.page_tokens); p.div_g = make_div32(p.G);
     p.q = static_cast<const uint16_t *>(a->q); p.q_row = a->q_row_stride; p.q_head = a->q_head_stride;
     p.out = static_cast<uint16_t *>(a->out); p.out_row = a->out_row_stride; p.out_head = a->out_head_stride;
     p.lse = a->lse; p.scale_log2 = a->scale * 1.4426950408889634f;

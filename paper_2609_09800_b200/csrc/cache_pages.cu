@@ -369,7 +369,7 @@ static int pages_call(const hbf_pages_t *p, const int32_t *a, const int32_t *b, 
     const PagesDev d = pages_dev(p, ws, result);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const size_t smem = ((size_t)mark_bits + 31u) / 32u * 4u;
-    if (ensure_dyn_smem((const void *)plan, smem) != cudaSuccess) return HBF_E_CUDA;
+    if (ensure_dyn_smem((const void *)plan, smem + 1024u) != cudaSuccess) return HBF_E_CUDA;          // (with what the plans hold besides)
     // up to 128 KB to move and 32 entries a thread, one block is done about when a second kernel would begin
     const int alone = most_moves * p->n_slabs * p->page_bytes <= 128u * 1024u && entries <= 32u * kPlanThreads;
     plan<<<1, kPlanThreads, smem, st>>>(d, args..., alone);

@@ -50,6 +50,10 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
     const uint32_t q_at = base, kv_at = base + 2u * kBytes;
     const uint32_t tid = threadIdx.x, lane = lane_id(), warp = tid >> 5;
     pdl_trigger();
+    if (tid == (uint32_t)kPfRowThreads && box) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
+    }
     // the piece: `row_tiles` counts pairs of tiles here
     uint32_t item = blockIdx.x;
     const uint32_t piece = item % p.prefix_pieces; item /= p.prefix_pieces;
@@ -79,17 +83,6 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
         // ---- keys and values: eight lanes a row of 128 bytes
         const uint32_t t = tid - (uint32_t)kPfRowThreads, w4 = warp - 16u, col = t & 7u, row = t >> 3;
         auto swizzled = [&](uint32_t r) { return r * 128u + ((col ^ (r & 7u)) * 16u); };
-        for (uint32_t h = 0; h < (two ? 2u : 1u); ++h)
-#pragma unroll 1
-            for (uint32_t r = row; r < kPfTile; r += 16u) {
-                const uint32_t n = row0 + h * kPfTile + r;
-                const bool ok = n < all_rows;
-                const uint32_t b = n / p.G, g = n - b * p.G;
-                const uint16_t *src = ok ? p.q + (int64_t)b * p.q_row + (int64_t)(head * p.G + g) * p.q_head + col * 8u : p.q;
-#pragma unroll
-                for (int x = 0; x < D / 64; ++x) copy_async16(q_at + h * kBytes + x * 16384u + swizzled(r), ok ? src + x * 64 : src, ok);
-            }
-        copy_commit();
         auto find = [&](uint32_t i) {                        // thread t: key t of tile i
             const uint32_t k = begin + i * kPfTile + t;
             int64_t at = -1;
@@ -103,17 +96,28 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
         auto arrive = [&](uint32_t bar) { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); bar_arrive(bar); };
         // boxes of `box` slots (0: none): whole tiles; warp w takes the boxes w, w + 4, ...
         const uint32_t whole = box ? (end - begin) / kPfTile : 0u, boxes = box ? kPfTile / box : 0u, my_boxes = boxes > w4 ? (boxes - w4 + 3u) / 4u : 0u;
+        int32_t page = 0;                                    // lane l: that of this warp's box l
+        uint32_t slot0 = 0u;
+        auto look = [&](uint32_t i) {
+            if (lane >= my_boxes || i >= whole) return;
+            const uint32_t k = begin + i * kPfTile + (w4 + lane * 4u) * box, n = div32(k, p.div_page);
+            page = p.prefix_pages[n]; slot0 = k - n * p.page_tokens;
+        };
+        look(0);
+        for (uint32_t h = 0; h < (two ? 2u : 1u); ++h)
+#pragma unroll
+            for (uint32_t r = row; r < kPfTile; r += 16u) {
+                const uint32_t n = row0 + h * kPfTile + r;
+                const bool ok = n < all_rows;
+                const uint32_t b = div32(n, p.div_g), g = n - b * p.G;
+                const uint16_t *src = ok ? p.q + (int64_t)b * p.q_row + (int64_t)(head * p.G + g) * p.q_head + col * 8u : p.q;
+#pragma unroll
+                for (int x = 0; x < D / 64; ++x) copy_async16(q_at + h * kBytes + x * 16384u + swizzled(r), ok ? src + x * 64 : src, ok);
+            }
+        copy_commit();
         if (whole) {
-            int32_t page = 0;                                // lane l: that of this warp's box l
-            uint32_t slot0 = 0u;
-            auto look = [&](uint32_t i) {
-                if (lane >= my_boxes || i >= whole) return;
-                const uint32_t k = begin + i * kPfTile + (w4 + lane * 4u) * box, n = div32(k, p.div_page);
-                page = p.prefix_pages[n]; slot0 = k - n * p.page_tokens;
-                if ((uint32_t)page >= p.n_pages) { sh.bad = 1u; page = -1; }              // (such a box is zeros)
-            };
-            look(0);
             for (uint32_t i = 0; i < whole; ++i) {
+                if (lane < my_boxes && (uint32_t)page >= p.n_pages) { sh.bad = 1u; page = -1; }        // (such a box is zeros)
                 const int32_t page_now = page;
                 const uint32_t slot_now = slot0;
                 look(i + 1u);
@@ -314,7 +318,7 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
             l += sh.other[t][half ^ 1u][r];
             const uint32_t n = row0 + t * kPfTile + r;
             const bool mine = n < all_rows;
-            const uint32_t b = n / p.G, h = head * p.G + (n - b * p.G);
+            const uint32_t b = div32(n, p.div_g), h = head * p.G + (n - b * p.G);
             const size_t rows = (size_t)p.B * p.Hq, at = (size_t)(p.own_pieces + piece) * rows + (size_t)b * p.Hq + h;
             const float z = m - lift, inv = l == 0.0f ? 0.0f : 1.0f / l;
             if (p.pieces == 1u) {
