@@ -18,7 +18,7 @@ struct AttnDev {
     const int32_t *prefix_pages, *own_pages, *own_len;
     // the pieces: `row_tiles` * Hk * prefix_pieces of the prefix, then B * Hk * group_tiles * own_pieces of the requests' own keys
     uint32_t row_tiles, prefix_pieces, prefix_chunk, group_tiles, own_pieces, own_chunk, n_prefix_items;
-    uint32_t prefix_rows;                                    // rows of a tile of the prefix's queries: 16, or 256 (two tiles) with k_prefix_tiles
+    uint32_t rows, prefix_rows;                              // rows of a tile; of the prefix's: the same, or 256 (two tiles) with k_prefix_tiles
     // what a piece leaves: sums not yet divided, [piece][row][d], and (largest score, sum of weights), [piece][row]
     float *part_o; float2 *part_ml;
     uint32_t pieces;                                         // own_pieces + prefix_pieces of every row; 1: written straight to `out`

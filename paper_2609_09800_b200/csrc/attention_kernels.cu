@@ -12,18 +12,21 @@ namespace hbf {
 
 constexpr int kAttWarps = 4, kAttThreads = kAttWarps * 32;
 constexpr int kStageKeys = 16;
-template <int D> constexpr int kAttRing = D == 128 ? 3 : 6;  // stages on their way, a warp: 24 KB, 192 KB an SM
-template <int D> constexpr size_t att_smem() { return (size_t)kAttWarps * kAttRing<D> * kStageKeys * D * 4; }
+template <int D> constexpr int kAttRing = D == 128 ? 2 : 4;  // stages on their way, a warp: 16 KB, 192 KB an SM
+template <int D> constexpr size_t kAttSmem = (size_t)kAttWarps * kAttRing<D> * kStageKeys * D * 4;
 
-// One piece by four warps: 16 rows (a group's heads of one request, or rows of several requests before the prefix), stages of 16 keys
+// One piece by four warps: 8 kN rows (a group's heads of one request, or rows of several requests before the prefix), stages of 16 keys
 // that go to the warps in turn, each with sums of its own, joined at the end.  Keys and values stream through a ring of each
-// warp's own.  The sum over a head's dimensions may take its 16-wide steps in any order, so a lane takes 16 consecutive
-// bytes of a key, copied by itself; values need the transpose, and lie in rows whose 16-byte columns are permuted by the row's number.
-template <class Ty, int D>
-__global__ void __launch_bounds__(kAttThreads)
+// warp's own.  The products are S^T = K Q^T and O^T = V^T P^T, so that eight rows are a whole product and the 16 of its other side are keys
+// or dimensions (with rows on that side half of the work was for rows that a group of eight heads does not have).  The sum over a head's
+// dimensions may take its 16-wide steps in any order, so a lane takes 16 consecutive bytes of a key, copied by itself; values need the
+// transpose, and lie in rows whose 16-byte columns are permuted by the row's number.  Latencies bound it (two to three warps a scheduler,
+// 0.3 instructions a cycle), before the copies' 28 bytes a cycle and SM.
+template <class Ty, int D, int kN>
+__global__ void __launch_bounds__(kAttThreads, 3)
 k_attend(const __grid_constant__ AttnDev p) {
     extern __shared__ __align__(128) unsigned char smem[];
-    constexpr int kRing = kAttRing<D>, kBlocks = D / 32, kHalf = kStageKeys * D * 2, kStage = 2 * kHalf;
+    constexpr int kRing = kAttRing<D>, kBlocks = D / 32, kRows = 8 * kN, kHalf = kStageKeys * D * 2, kStage = 2 * kHalf;
     const uint32_t lane = lane_id(), warp = threadIdx.x >> 5, row = lane >> 2, quad = lane & 3u;
     pdl_trigger();
     uint32_t item = blockIdx.x, head, tile, piece, b = 0u, begin, end, slot_out;
@@ -36,7 +39,7 @@ k_attend(const __grid_constant__ AttnDev p) {
         tile = item % p.row_tiles; head = item / p.row_tiles;
         begin = piece * p.prefix_chunk; end = min(p.prefix_len, begin + p.prefix_chunk);
         table = p.prefix_pages;
-        n_rows = min(16u, p.B * p.G - tile * 16u);
+        n_rows = min((uint32_t)kRows, p.B * p.G - tile * kRows);
         slot_out = p.own_pieces + piece;
     } else {
         item -= p.n_prefix_items;
@@ -47,13 +50,13 @@ k_attend(const __grid_constant__ AttnDev p) {
         bad = len < 0 || (uint32_t)len > p.max_own;
         begin = piece * p.own_chunk; end = bad ? 0u : min((uint32_t)len, begin + p.own_chunk);
         table = p.own_pages + (size_t)b * p.own_stride;
-        n_rows = min(16u, p.G - tile * 16u);
+        n_rows = min((uint32_t)kRows, p.G - tile * kRows);
         slot_out = piece;
     }
     // row r of the tile: request and query head
     auto place = [&](uint32_t r, uint32_t &rb, uint32_t &rh) {
-        if (shared) { const uint32_t n = tile * 16u + r; rb = div32(n, p.div_g); rh = head * p.G + n - rb * p.G; }
-        else { rb = b; rh = head * p.G + tile * 16u + r; }
+        if (shared) { const uint32_t n = tile * kRows + r; rb = div32(n, p.div_g); rh = head * p.G + n - rb * p.G; }
+        else { rb = b; rh = head * p.G + tile * kRows + r; }
     };
 
     const uint32_t base = smem_addr(smem) + warp * (kRing * kStage);
@@ -100,107 +103,128 @@ k_attend(const __grid_constant__ AttnDev p) {
 #pragma unroll
     for (int i = 0; i < kRing; ++i) issue();
 
-    uint4 q0[kBlocks], q1[kBlocks];                          // this lane's parts of rows `row` and `row + 8`
-    {
+    uint4 q[kN][kBlocks];                                    // this lane's parts of rows `row` and, with kN 2, `row + 8`
+#pragma unroll
+    for (int r = 0; r < kN; ++r) {
         uint32_t rb, rh;
-        place(row, rb, rh);
-        const uint16_t *s0 = p.q + (int64_t)rb * p.q_row + (int64_t)rh * p.q_head + quad * 8u;
-        place(row + 8u, rb, rh);
-        const uint16_t *s1 = p.q + (int64_t)rb * p.q_row + (int64_t)rh * p.q_head + quad * 8u;
+        place(row + r * 8u, rb, rh);
+        const uint16_t *from = p.q + (int64_t)rb * p.q_row + (int64_t)rh * p.q_head + quad * 8u;
 #pragma unroll
-        for (int i = 0; i < kBlocks; ++i) {
-            q0[i] = row < n_rows ? __ldg(reinterpret_cast<const uint4 *>(s0 + i * 32)) : make_uint4(0u, 0u, 0u, 0u);
-            q1[i] = row + 8u < n_rows ? __ldg(reinterpret_cast<const uint4 *>(s1 + i * 32)) : make_uint4(0u, 0u, 0u, 0u);
-        }
+        for (int i = 0; i < kBlocks; ++i) q[r][i] = row + r * 8u < n_rows ? __ldg(reinterpret_cast<const uint4 *>(from + i * 32)) : make_uint4(0u, 0u, 0u, 0u);
     }
-    const bool both = n_rows > 8u;
-    float o[D / 8][4], m0 = -INFINITY, m1 = -INFINITY, l0 = 0.0f, l1 = 0.0f;
+    // of the rows 8 r + 2 quad + c: the largest score so far, this lane's share of the weights; their sums, dimensions 16 j + row and + 8
+    float o[kN][D / 16][4], m[kN][2], l[kN][2];
 #pragma unroll
-    for (int j = 0; j < D / 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.0f;
+    for (int r = 0; r < kN; ++r) {
+        m[r][0] = m[r][1] = -INFINITY; l[r][0] = l[r][1] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) o[r][j][0] = o[r][j][1] = o[r][j][2] = o[r][j][3] = 0.0f;
+    }
     uint32_t slot = 0u;
     for (uint32_t st = warp; st < stages; st += kAttWarps) {
         copy_wait<kRing - 1>();
         __syncwarp();
         const uint32_t src = base + slot * kStage;
         slot = slot + 1u == kRing ? 0u : slot + 1u;
-        float s[2][4] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+        float s[kN][4];                                      // keys `row` (0, 1) and `row + 8` (2, 3) for two rows
+#pragma unroll
+        for (int r = 0; r < kN; ++r) s[r][0] = s[r][1] = s[r][2] = s[r][3] = 0.0f;
 #pragma unroll
         for (int i = 0; i < kBlocks; ++i) {
             const uint4 ka = ld_shared16(src + (i * 2) * 512u + lane * 16u), kb = ld_shared16(src + (i * 2 + 1) * 512u + lane * 16u);
-            Ty::mma(s[0], q0[i].x, q1[i].x, q0[i].y, q1[i].y, ka.x, ka.y);
-            Ty::mma(s[1], q0[i].x, q1[i].x, q0[i].y, q1[i].y, kb.x, kb.y);
-            Ty::mma(s[0], q0[i].z, q1[i].z, q0[i].w, q1[i].w, ka.z, ka.w);
-            Ty::mma(s[1], q0[i].z, q1[i].z, q0[i].w, q1[i].w, kb.z, kb.w);
-        }
-        const uint32_t key = begin + st * kStageKeys + quad * 2u;
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                s[t][c] *= p.scale_log2;
-                if (key + t * 8u + (c & 1) >= end) s[t][c] = -INFINITY;
+            for (int r = 0; r < kN; ++r) {
+                Ty::mma(s[r], ka.x, kb.x, ka.y, kb.y, q[r][i].x, q[r][i].y);
+                Ty::mma(s[r], ka.z, kb.z, ka.w, kb.w, q[r][i].z, q[r][i].w);
             }
-        // the running maximum of both rows; while it is -inf there is nothing to scale and every weight is 0
-        float a0 = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1])), a1 = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
-        a0 = fmaxf(a0, __shfl_xor_sync(0xffffffffu, a0, 1)); a1 = fmaxf(a1, __shfl_xor_sync(0xffffffffu, a1, 1));
-        a0 = fmaxf(a0, __shfl_xor_sync(0xffffffffu, a0, 2)); a1 = fmaxf(a1, __shfl_xor_sync(0xffffffffu, a1, 2));
-        if (__any_sync(0xffffffffu, a0 > m0 || (both && a1 > m1))) {
-            const float n0 = fmaxf(m0, a0), n1 = fmaxf(m1, a1);
-            const float f0 = n0 == -INFINITY ? 1.0f : exp2_fast(m0 - n0), f1 = n1 == -INFINITY ? 1.0f : exp2_fast(m1 - n1);
-            m0 = n0; m1 = n1; l0 *= f0; l1 *= f1;
-#pragma unroll
-            for (int j = 0; j < D / 8; ++j) { o[j][0] *= f0; o[j][1] *= f0; o[j][2] *= f1; o[j][3] *= f1; }
         }
-        const float z0 = m0 == -INFINITY ? 0.0f : m0 - Ty::kLift, z1 = m1 == -INFINITY ? 0.0f : m1 - Ty::kLift;
-        // The weights as an A operand (rows, then keys 8 to 15), each as the sum of two numbers of the values' type: rounding them once would
-        // cost as much again as rounding the output does.  The first is rounded down and the second is positive where the weight
-        // is, so that both take an infinite value the same way.
-        uint32_t hi[4], lo[4];
-        auto split = [&](int k, float pa, float pb) {
-            hi[k] = Ty::pack_down(pa, pb);
-            const float2 r = Ty::unpack(hi[k]);
-            lo[k] = Ty::pack(fmaxf(pa - r.x, fminf(pa, Ty::kTiny)), fmaxf(pb - r.y, fminf(pb, Ty::kTiny)));
-        };
+        const uint32_t key = begin + st * kStageKeys + row;
+        const bool in0 = key < end, in1 = key + 8u < end;
+        // the running maximum of each row; while it is -inf there is nothing to scale and every weight is 0
+        float top[kN][2];
+        bool more = false;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const float p0 = exp2_fast(s[t][0] - z0), p1 = exp2_fast(s[t][1] - z0);
-            l0 += p0 + p1;
-            split(t * 2, p0, p1);
-            hi[t * 2 + 1] = lo[t * 2 + 1] = 0u;
-            if (both) {
-                const float p2 = exp2_fast(s[t][2] - z1), p3 = exp2_fast(s[t][3] - z1);
-                l1 += p2 + p3;
-                split(t * 2 + 1, p2, p3);
+        for (int r = 0; r < kN; ++r)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                s[r][c] = in0 ? s[r][c] * p.scale_log2 : -INFINITY;
+                s[r][c + 2] = in1 ? s[r][c + 2] * p.scale_log2 : -INFINITY;
+                top[r][c] = fmaxf(s[r][c], s[r][c + 2]);
+            }
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1)
+#pragma unroll
+            for (int r = 0; r < kN; ++r)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) top[r][c] = fmaxf(top[r][c], __shfl_xor_sync(0xffffffffu, top[r][c], x));
+#pragma unroll
+        for (int r = 0; r < kN; ++r) more |= top[r][0] > m[r][0] || top[r][1] > m[r][1];
+        if (__any_sync(0xffffffffu, more)) {
+#pragma unroll
+            for (int r = 0; r < kN; ++r) {
+                float f[2];
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const float n = fmaxf(m[r][c], top[r][c]);
+                    f[c] = n == -INFINITY ? 1.0f : exp2_fast(m[r][c] - n);
+                    m[r][c] = n; l[r][c] *= f[c];
+                }
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) { o[r][j][0] *= f[0]; o[r][j][1] *= f[1]; o[r][j][2] *= f[0]; o[r][j][3] *= f[1]; }
+            }
+        }
+        // The weights as a B operand (keys, then rows), each as the sum of two numbers of the values' type: rounding them once would cost as
+        // much again as rounding the output does.  The first is rounded down and the second is positive where the weight is, so that
+        // both take an infinite value the same way.
+        uint32_t hi[kN][2], lo[kN][2];
+#pragma unroll
+        for (int r = 0; r < kN; ++r) {
+            const float z0 = m[r][0] == -INFINITY ? 0.0f : m[r][0] - Ty::kLift, z1 = m[r][1] == -INFINITY ? 0.0f : m[r][1] - Ty::kLift;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float a = exp2_fast(s[r][2 * k] - z0), b = exp2_fast(s[r][2 * k + 1] - z1);
+                l[r][0] += a; l[r][1] += b;
+                const uint32_t h = Ty::pack_down(a, b);
+                const float2 back = Ty::unpack(h);
+                hi[r][k] = transpose_tile(h);
+                lo[r][k] = transpose_tile(Ty::pack(fmaxf(a - back.x, fminf(a, Ty::kTiny)), fmaxf(b - back.y, fminf(b, Ty::kTiny))));
             }
         }
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) {
-            uint32_t b0, b1, b2, b3;
-            const uint32_t r = (lane & 7u) + ((lane >> 3) & 1u) * 8u, c = j * 2u + (lane >> 4);
-            load_tiles_t(src + kHalf + r * (D * 2) + ((c ^ (r & 7u)) * 16u), b0, b1, b2, b3);
-            Ty::mma(o[j * 2], hi[0], hi[1], hi[2], hi[3], b0, b1);
-            Ty::mma(o[j * 2 + 1], hi[0], hi[1], hi[2], hi[3], b2, b3);
-            Ty::mma(o[j * 2], lo[0], lo[1], lo[2], lo[3], b0, b1);
-            Ty::mma(o[j * 2 + 1], lo[0], lo[1], lo[2], lo[3], b2, b3);
+            uint32_t v0, v1, v2, v3;
+            const uint32_t kr = (lane & 7u) + (lane >> 4) * 8u, c = j * 2u + ((lane >> 3) & 1u);
+            load_tiles_t(src + kHalf + kr * (D * 2) + ((c ^ (kr & 7u)) * 16u), v0, v1, v2, v3);
+#pragma unroll
+            for (int r = 0; r < kN; ++r) {
+                Ty::mma(o[r][j], v0, v1, v2, v3, hi[r][0], hi[r][1]);
+                Ty::mma(o[r][j], v0, v1, v2, v3, lo[r][0], lo[r][1]);
+            }
         }
         __syncwarp();                                        // every lane has read the values that the next copies replace
         issue();
     }
-    l0 += __shfl_xor_sync(0xffffffffu, l0, 1); l1 += __shfl_xor_sync(0xffffffffu, l1, 1);
-    l0 += __shfl_xor_sync(0xffffffffu, l0, 2); l1 += __shfl_xor_sync(0xffffffffu, l1, 2);
+#pragma unroll
+    for (int x = 4; x < 32; x <<= 1)
+#pragma unroll
+        for (int r = 0; r < kN; ++r)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) l[r][c] += __shfl_xor_sync(0xffffffffu, l[r][c], x);
     copy_wait<0>();
-    if (__any_sync(0xffffffffu, bad)) l0 = l1 = __int_as_float(0x7fc00000);         // a page that is none: the row has no answer
+    const bool none = __any_sync(0xffffffffu, bad);          // a page that is none: the rows have no answer
     __syncthreads();                                         // the rings are empty: their memory holds the warps' sums
     float *os = reinterpret_cast<float *>(smem);
-    __shared__ float2 ml[kAttWarps][16];
+    __shared__ float2 ml[kAttWarps][kRows];
     constexpr int kPitch = D + 4;
+    static_assert((size_t)kAttWarps * kRows * kPitch * 4 <= kAttSmem<D>, "the warps' sums");
 #pragma unroll
-    for (int j = 0; j < D / 8; ++j) {
-        float *d0 = os + ((size_t)warp * 16 + row) * kPitch + j * 8 + quad * 2;
-        *reinterpret_cast<float2 *>(d0) = make_float2(o[j][0], o[j][1]);
-        if (both) *reinterpret_cast<float2 *>(d0 + 8 * kPitch) = make_float2(o[j][2], o[j][3]);
+    for (int r = 0; r < kN; ++r) {
+        float *to = os + ((size_t)warp * kRows + r * 8 + quad * 2) * kPitch + row;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) { to[j * 16] = o[r][j][0]; to[kPitch + j * 16] = o[r][j][1]; to[j * 16 + 8] = o[r][j][2]; to[kPitch + j * 16 + 8] = o[r][j][3]; }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) if (row == 0u) ml[warp][r * 8 + quad * 2 + c] = make_float2(m[r][c] - Ty::kLift, none ? __int_as_float(0x7fc00000) : l[r][c]);
     }
-    if (quad == 0u) { ml[warp][row] = make_float2(m0 - Ty::kLift, l0); ml[warp][row + 8u] = make_float2(m1 - Ty::kLift, l1); }
     __syncthreads();
     constexpr int kLanes = D / 4;                            // threads a row, four dimensions each
     const uint32_t col = threadIdx.x % kLanes;
@@ -213,7 +237,7 @@ k_attend(const __grid_constant__ AttnDev p) {
 #pragma unroll
         for (int w = 0; w < kAttWarps; ++w) {
             const float f = exp2_fast(ml[w][r].x - z);
-            const float4 x = *reinterpret_cast<const float4 *>(os + ((size_t)w * 16 + r) * kPitch + col * 4u);
+            const float4 x = *reinterpret_cast<const float4 *>(os + ((size_t)w * kRows + r) * kPitch + col * 4u);
             L += f * ml[w][r].y; v.x += f * x.x; v.y += f * x.y; v.z += f * x.z; v.w += f * x.w;
         }
         uint32_t rb, rh;
@@ -369,9 +393,12 @@ static uint32_t up_to(uint32_t v, uint32_t m) { return (v + m - 1u) / m * m; }
 // multiple of 64, at most 1,024 of a request's own (whose lengths differ).
 static void attention_pieces(const hbf_attention_t *a, uint32_t n_sm, AttnDev &p) {
     const uint32_t G = p.G, blocks = 2u * n_sm;
-    p.prefix_rows = prefix_small(a) ? 16u : 256u;
+    // rows of a tile of k_attend: eight, or sixteen where more come together
+    const bool small = prefix_small(a);
+    p.rows = G > 8u || (small && a->prefix_len && p.B * G > 8u) ? 16u : 8u;
+    p.prefix_rows = small ? p.rows : 256u;
     p.row_tiles = (p.B * G + p.prefix_rows - 1u) / p.prefix_rows;
-    p.group_tiles = (G + 15u) / 16u;
+    p.group_tiles = (G + p.rows - 1u) / p.rows;
     p.prefix_pieces = 0u; p.prefix_chunk = 64u;
     if (a->prefix_len) {
         // (k_prefix_tiles: a block an SM, tiles of 128 keys)
@@ -425,9 +452,10 @@ static cudaError_t launch_attention(AttnDev p, bool bf16, cudaStream_t st) {
     // the requests' own keys go to the SMs that the prefix's blocks leave free, and to the others as those end
     if (tiles && (e = launch_prefix_tiles(p, D, bf16, st)) != cudaSuccess) return e;
     if (items) {
-        if ((e = ensure_dyn_smem((const void *)k_attend<Ty, D>, att_smem<D>())) != cudaSuccess) return e;
-        if (tiles) e = launch_pdl(k_attend<Ty, D>, (unsigned)items, kAttThreads, att_smem<D>(), st, own);
-        else { k_attend<Ty, D><<<(unsigned)items, kAttThreads, att_smem<D>(), st>>>(own); e = cudaGetLastError(); }
+        const auto attend = p.rows == 8u ? k_attend<Ty, D, 1> : k_attend<Ty, D, 2>;
+        if ((e = ensure_dyn_smem((const void *)attend, kAttSmem<D>)) != cudaSuccess) return e;
+        if (tiles) e = launch_pdl(attend, (unsigned)items, kAttThreads, kAttSmem<D>, st, own);
+        else { attend<<<(unsigned)items, kAttThreads, kAttSmem<D>, st>>>(own); e = cudaGetLastError(); }
         g_kernel_launches += 1;
         if (e != cudaSuccess) return e;
     }

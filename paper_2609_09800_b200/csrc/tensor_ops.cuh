@@ -87,6 +87,8 @@ __device__ __forceinline__ uint4 ld_shared16(uint32_t a) {
 __device__ __forceinline__ void load_tiles_t(uint32_t a, uint32_t &r0, uint32_t &r1, uint32_t &r2, uint32_t &r3) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3) : "r"(a) : "memory");
 }
+// an 8x8 tile of 16-bit values that lies in registers as a product's sums do (row lane / 4, columns 2 (lane % 4) and the next), transposed
+__device__ __forceinline__ uint32_t transpose_tile(uint32_t a) { uint32_t d; asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a)); return d; }
 __device__ __forceinline__ float exp2_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
 // n / d for n, d < 2^31: with l = ceil(log2 d) and m = floor(2^(31+l) / d) + 1 < 2^32, n / d = (n * m) >> (31 + l), exact since
