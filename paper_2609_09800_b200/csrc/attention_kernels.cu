@@ -388,9 +388,10 @@ static bool prefix_small(const hbf_attention_t *a) {
 
 static uint32_t up_to(uint32_t v, uint32_t m) { return (v + m - 1u) / m * m; }
 
-// How the keys are cut.  A piece costs its start-up (about 2 us to the first values) and d * 4 bytes a row to join, so pieces are as long as
-// leaves about two blocks an SM, which are resident at once (one request behind 8K tokens 12.3 us, with four 14.5): at least 64 keys, a
-// multiple of 64, at most 1,024 of a request's own (whose lengths differ).
+// How the keys are cut.  A piece costs its start-up (about 2 us to the first values) and d * 4 bytes a row to join.  The prefix: as long as
+// leaves about two blocks an SM, which are resident at once (one request behind 8K tokens 12.0 us, with four 14.5).  The requests' own, whose
+// lengths differ: shorter ones, so that the blocks that are done take others' (128 requests with up to 2,048 130 us with pieces of 512 at
+// most, with 1,024 132, with 256 133).  At least 64 keys, a multiple of 64.
 static void attention_pieces(const hbf_attention_t *a, uint32_t n_sm, AttnDev &p) {
     const uint32_t G = p.G, blocks = 2u * n_sm;
     // rows of a tile of k_attend: eight, or sixteen where more come together
@@ -411,9 +412,9 @@ static void attention_pieces(const hbf_attention_t *a, uint32_t n_sm, AttnDev &p
     p.own_pieces = 0u; p.own_chunk = 64u;
     if (a->max_own_len) {
         const uint64_t lists = (uint64_t)p.B * p.Hk * p.group_tiles;
-        const uint64_t want = lists < blocks ? blocks / lists : 1u;
+        const uint64_t want = lists < 2u * blocks ? 2u * blocks / lists : 1u;
         uint64_t chunk = (a->max_own_len + want - 1u) / want;
-        chunk = chunk < 64u ? 64u : chunk > 1024u ? 1024u : chunk;
+        chunk = chunk < 64u ? 64u : chunk > 512u ? 512u : chunk;
         const uint64_t least = ((uint64_t)a->max_own_len + kMostPieces / 4u - 1u) / (kMostPieces / 4u);
         if (chunk < least) chunk = least;
         p.own_chunk = up_to((uint32_t)chunk, 64u);
