@@ -177,7 +177,7 @@ __device__ __forceinline__ void route(const MoeDev &m, Route<kTokens> &r, RouteT
             tmp.expert[i] = (uint16_t)e; tmp.weight[i] = w;
         }
     } else if (m.E > 128u) route_tokens<HBF_MOE_MAX_EXPERTS / 32, 1>(m, r, tmp, write);
-    else if (kTokens > kMoeWarps && m.T > kMoeWarps) route_tokens<4, kTokens / kMoeWarps < 4 ? 1 : 4>(m, r, tmp, write);
+    else if (kTokens > kMoeWarps && m.T > kMoeWarps) route_tokens<4, kTokens < 4 * kMoeWarps ? 1 : 4>(m, r, tmp, write);
     else route_tokens<4, 1>(m, r, tmp, write);
     __syncthreads();
     // places of the experts in the list of pairs, of those in use, and of the entries: one scan over the experts

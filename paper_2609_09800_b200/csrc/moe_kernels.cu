@@ -1,4 +1,4 @@
-// A mixture-of-experts layer for a few tokens in two kernels.
+// A mixture-of-experts layer for up to eight tokens in two kernels (moe_tiles.cu has the form for more, or for many bytes of weights).
 //
 //   choice      the top_k largest of a token's scores, ties to the lowest expert; weights w = softmax over the chosen (or over all)
 //   k_moe_up    h[pair] = w * silu(gate x) * (up x)             for every (expert, token that chose it) pair
@@ -16,24 +16,28 @@
 
 namespace hbf {
 
-// Sixteen warps' sums of a 16 x 8 n product, left as they lie in the accumulators: eight lanes for a column of the pile, two warps' parts
-// each, always in the same order.  f(tile, lane of the accumulator, its four sums) is called once for every column.
+// Rings of five and three steps, 80 and 96 KB of weights an SM on their way; longer ones were no faster, and neither was room for both kernels on
+// an SM (a token 26.8 us against 24.7: half of the registers each, and the weights of the second take their share of the bandwidth early).
+constexpr int kFewTokens = 8, kUpRing = 5, kDownRing = 3, kDownWide = 2;
+using FewRoute = Route<kFewTokens>;
+using FewTemp = RouteTemp<kFewTokens>;
+constexpr uint32_t kFewBytes = kRouteBytes<kFewTokens>;
+
+// Sixteen warps' sums of a 16 x 8 product, left as they lie in the accumulators: eight lanes for a column of the pile, two warps' parts
+// each, always in the same order.  f(lane of the accumulator, its four sums) is called once for every column.
 template <class F>
-__device__ __forceinline__ void sum_over_warps(const float4 *pile, int tiles, F f) {
-    const uint32_t lane = lane_id(), warp = threadIdx.x >> 5, part = lane >> 2;
-#pragma unroll 1
-    for (uint32_t c0 = warp * 4u; c0 < (uint32_t)tiles * 32u; c0 += kMoeWarps * 4u) {
-        const uint32_t col = c0 + (lane & 3u);
-        float4 s = pile[(size_t)(part * 2u) * tiles * 32u + col];
-        const float4 v = pile[(size_t)(part * 2u + 1u) * tiles * 32u + col];
-        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+__device__ __forceinline__ void sum_over_warps(const float4 *pile, F f) {
+    const uint32_t lane = lane_id(), warp = threadIdx.x >> 5, part = lane >> 2, col = warp * 4u + (lane & 3u);
+    if (warp >= 8u) return;
+    float4 s = pile[part * 64u + col];
+    const float4 v = pile[part * 64u + 32u + col];
+    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
 #pragma unroll
-        for (int o = 4; o < 32; o <<= 1) {
-            s.x += __shfl_xor_sync(0xffffffffu, s.x, o); s.y += __shfl_xor_sync(0xffffffffu, s.y, o);
-            s.z += __shfl_xor_sync(0xffffffffu, s.z, o); s.w += __shfl_xor_sync(0xffffffffu, s.w, o);
-        }
-        if (part == 0u) f(col >> 5, col & 31u, s);
+    for (int o = 4; o < 32; o <<= 1) {
+        s.x += __shfl_xor_sync(0xffffffffu, s.x, o); s.y += __shfl_xor_sync(0xffffffffu, s.y, o);
+        s.z += __shfl_xor_sync(0xffffffffu, s.z, o); s.w += __shfl_xor_sync(0xffffffffu, s.w, o);
     }
+    if (part == 0u) f(col, s);
 }
 
 __device__ __forceinline__ uint4 ld_input(const uint16_t *p) { return __ldg(reinterpret_cast<const uint4 *>(p)); }
@@ -41,26 +45,23 @@ __device__ __forceinline__ uint4 ld_after16(const uint16_t *p) {                
     uint4 v; asm volatile("ld.global.cg.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p)); return v;
 }
 
-// Shared memory of the up kernel: the choice, the pile of sums (twice where there is room), the rings.  kTiles: tiles of eight tokens that an
-// entry has at most.
-template <int kTiles> constexpr uint32_t kPiles = kTiles == 4 ? 1u : 2u;
-template <int kTiles, int kTokens> constexpr uint32_t kUpRingAt = kRouteBytes<kTokens> + kPiles<kTiles> * kMoeWarps * kTiles * 512u;
-template <int kTiles, int kTokens, int kRing> constexpr uint32_t up_smem() { return kUpRingAt<kTiles, kTokens> + kMoeWarps * kRing * 1024u; }
+// Shared memory of the up kernel: the choice, the pile of sums twice, the rings.
+constexpr uint32_t kUpRingAt = kFewBytes + 2u * kMoeWarps * 512u, kUpSmem = kUpRingAt + kMoeWarps * kUpRing * 1024u;
 
 // Items of eight gate rows and the same eight up rows (rows 0..7 and 8..15 of one product, so a thread's sums hold both), one item a
 // block at a time, the sum over `hidden` split among its warps in steps of 32; the ring runs on into the next item while an item's sums
 // are joined.  Activations, which L1 or L2 holds, are asked for a step ahead.
-template <class Ty, int kTiles, int kTokens, int kRing, int kBlocks>
-__global__ void __launch_bounds__(kMoeThreads, kBlocks)
+template <class Ty>
+__global__ void __launch_bounds__(kMoeThreads, 1)
 k_moe_up(const __grid_constant__ MoeDev m) {
     extern __shared__ __align__(128) unsigned char smem[];
-    Route<kTokens> &r = *reinterpret_cast<Route<kTokens> *>(smem);
+    FewRoute &r = *reinterpret_cast<FewRoute *>(smem);
     const uint32_t lane = lane_id(), warp = threadIdx.x >> 5, row = lane >> 2, quad = lane & 3u;
     pdl_trigger();
-    route<false>(m, r, *reinterpret_cast<RouteTemp<kTokens> *>(smem + kRouteBytes<kTokens>), kTiles * 8u, blockIdx.x == 0);
+    route<false>(m, r, *reinterpret_cast<FewTemp *>(smem + kFewBytes), kFewTokens, blockIdx.x == 0);
     const uint32_t slices = m.I / 8u, n_items = r.n_entries * slices;
     const uint32_t steps = ((m.D + 31u) / 32u + kMoeWarps - 1u) / kMoeWarps;               // of a warp, an item
-    const uint32_t ring = smem_addr(smem) + kUpRingAt<kTiles, kTokens> + warp * (kRing * 1024u) + lane * 16u, k0 = warp * 32u + quad * 8u;
+    const uint32_t ring = smem_addr(smem) + kUpRingAt + warp * (kUpRing * 1024u) + lane * 16u, k0 = warp * 32u + quad * 8u;
     constexpr uint32_t kStride = kMoeWarps * 32u;
 
     uint32_t in_item = blockIdx.x, in_k = k0, in_left = steps, in_slot = 0u;
@@ -76,7 +77,7 @@ k_moe_up(const __grid_constant__ MoeDev m) {
             const uint16_t *g = in ? gate + in_k : m.experts;
             copy_async16(ring + in_slot * 1024u, g, in);
             copy_async16(ring + in_slot * 1024u + 512u, in ? g + (size_t)m.I * m.D : g, in);
-            in_slot = in_slot + 1u == kRing ? 0u : in_slot + 1u;
+            in_slot = in_slot + 1u == kUpRing ? 0u : in_slot + 1u;
             in_k += kStride;
             if (--in_left == 0u) { in_left = steps; in_k = k0; in_item += gridDim.x; place(); }
         }
@@ -84,51 +85,35 @@ k_moe_up(const __grid_constant__ MoeDev m) {
     };
     place();
 #pragma unroll 1
-    for (int i = 0; i < kRing; ++i) issue();
+    for (int i = 0; i < kUpRing; ++i) issue();
 
     uint32_t slot = 0u, turn = 0u;
     for (uint32_t item = blockIdx.x; item < n_items; item += gridDim.x, turn ^= 1u) {
         const uint32_t en = div32(item, m.div_slices), sl = item - en * slices, n = r.count[en], pair0 = r.pair0[en];
-        const int tiles = (int)((n + 7u) / 8u);
-        const uint16_t *x[kTiles];
-        uint4 now[kTiles];
         const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-        float acc[kTiles][4];
-#pragma unroll
-        for (int j = 0; j < kTiles; ++j) {
-            x[j] = j * 8u + row < n ? m.x + (int64_t)r.token[pair0 + j * 8u + row] * m.x_stride : nullptr;
-            now[j] = x[j] && k0 < m.D ? ld_input(x[j] + k0) : zero;
-            acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
-        }
+        const uint16_t *x = row < n ? m.x + (int64_t)r.token[pair0 + row] * m.x_stride : nullptr;
+        uint4 now = x && k0 < m.D ? ld_input(x + k0) : zero;
+        float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 1
         for (uint32_t s = 0, k = k0 + kStride; s < steps; ++s, k += kStride) {
-            uint4 next[kTiles];
-#pragma unroll
-            for (int j = 0; j < kTiles; ++j) next[j] = x[j] && k < m.D && s + 1u < steps ? ld_input(x[j] + k) : zero;
-            copy_wait<kRing - 1>();
+            const uint4 next = x && k < m.D && s + 1u < steps ? ld_input(x + k) : zero;
+            copy_wait<kUpRing - 1>();
             const uint4 g = ld_shared16(ring + slot * 1024u), u = ld_shared16(ring + slot * 1024u + 512u);
-            slot = slot + 1u == kRing ? 0u : slot + 1u;
-#pragma unroll
-            for (int j = 0; j < kTiles; ++j)
-                if (j < tiles) {
-                    Ty::mma(acc[j], g.x, u.x, g.y, u.y, now[j].x, now[j].y);
-                    Ty::mma(acc[j], g.z, u.z, g.w, u.w, now[j].z, now[j].w);
-                }
+            slot = slot + 1u == kUpRing ? 0u : slot + 1u;
+            Ty::mma(acc, g.x, u.x, g.y, u.y, now.x, now.y);
+            Ty::mma(acc, g.z, u.z, g.w, u.w, now.z, now.w);
             issue();
-#pragma unroll
-            for (int j = 0; j < kTiles; ++j) now[j] = next[j];
+            now = next;
         }
         // two piles in turn: a warp that is ahead writes the other one, and passes the next barrier only with all
-        float4 *pile = reinterpret_cast<float4 *>(smem + kRouteBytes<kTokens>) + (kPiles<kTiles> == 2u ? (size_t)turn * kMoeWarps * kTiles * 32u : 0u);
-#pragma unroll
-        for (int j = 0; j < kTiles; ++j)
-            if (j < tiles) pile[((size_t)warp * tiles + j) * 32u + lane] = make_float4(acc[j][0], acc[j][1], acc[j][2], acc[j][3]);
+        float4 *pile = reinterpret_cast<float4 *>(smem + kFewBytes) + turn * (kMoeWarps * 32u);
+        pile[warp * 32u + lane] = make_float4(acc[0], acc[1], acc[2], acc[3]);
         __syncthreads();
-        sum_over_warps(pile, tiles, [&](uint32_t tile, uint32_t l, const float4 &v) {
+        sum_over_warps(pile, [&](uint32_t l, const float4 &v) {
             const uint32_t i = sl * 8u + (l >> 2);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const uint32_t rank = tile * 8u + (l & 3u) * 2u + k;
+                const uint32_t rank = (l & 3u) * 2u + k;
                 if (rank >= n) continue;
                 const float g = k ? v.y : v.x, u = k ? v.w : v.z;
                 const float h = r.weight[pair0 + rank] * (g / (1.0f + expf(-g)) * u);
@@ -140,55 +125,52 @@ k_moe_up(const __grid_constant__ MoeDev m) {
                 reinterpret_cast<typename Ty::type *>(m.h_lo)[at] = isfinite(Ty::to(hi)) ? lo : Ty::from(0.0f);
             }
         });
-        if (kPiles<kTiles> == 1u) __syncthreads();
     }
     copy_wait<0>();
 }
 
 // Shared memory of the down kernel: the choice, every warp's sums of 16 rows for all tokens, the rings.
 __host__ __device__ constexpr uint32_t down_sums(uint32_t tokens) { return kMoeWarps * tokens * 64u; }
-template <int kTokens, int kRing, int kWide> constexpr uint32_t down_smem(uint32_t tokens) {
-    const uint32_t more = down_sums(tokens) + kMoeWarps * kRing * kWide * 1024u, tmp = (sizeof(RouteTemp<kTokens>) + 127u) / 128u * 128u;
-    return kRouteBytes<kTokens> + (more > tmp ? more : tmp);
-}
+constexpr uint32_t down_smem(uint32_t tokens) { return kFewBytes + down_sums(tokens) + kMoeWarps * kDownRing * kDownWide * 1024u; }
+static_assert(kUpSmem <= 227 * 1024 && down_smem(kFewTokens) <= 227 * 1024 && sizeof(FewTemp) <= kMoeWarps * 1024u, "shared memory");
 
-// A block keeps up to 16 rows of the output for all tokens and walks the steps of the entries in use, 32 kWide each, a stretch of
-// them a warp.  An entry's products have its tokens as columns; a warp adds them to its sums in shared memory when it comes to the next entry:
+// A block keeps up to 16 rows of the output for all tokens and walks the steps of the experts in use, 32 kDownWide each, a stretch of
+// them a warp.  An expert's products have its tokens as columns; a warp adds them to its sums in shared memory when it comes to the next one:
 // a token's sums grow only by what its own experts hold, and in the order of the experts.  The ring's first weights are on their way while the
 // kernel before still runs; activations, which L2 holds, are asked for a step ahead.
-template <class Ty, int kTiles, int kTokens, int kRing, int kWide, int kBlocks>
-__global__ void __launch_bounds__(kMoeThreads, kBlocks)
+template <class Ty>
+__global__ void __launch_bounds__(kMoeThreads, 1)
 k_moe_down(const __grid_constant__ MoeDev m) {
     extern __shared__ __align__(128) unsigned char smem[];
-    Route<kTokens> &r = *reinterpret_cast<Route<kTokens> *>(smem);
+    FewRoute &r = *reinterpret_cast<FewRoute *>(smem);
     const uint32_t tid = threadIdx.x, lane = lane_id(), warp = tid >> 5, row = lane >> 2, quad = lane & 3u;
-    route<false>(m, r, *reinterpret_cast<RouteTemp<kTokens> *>(smem + kRouteBytes<kTokens>), kTiles * 8u, false);
-    float *sums = reinterpret_cast<float *>(smem + kRouteBytes<kTokens>);                   // [warp][token][16]
+    route<false>(m, r, *reinterpret_cast<FewTemp *>(smem + kFewBytes), kFewTokens, false);
+    float *sums = reinterpret_cast<float *>(smem + kFewBytes);                              // [warp][token][16]
     float *mine = sums + (size_t)warp * m.T * 16u;
-    constexpr uint32_t kStep = kWide * 32u, kSlot = kWide * 1024u;
+    constexpr uint32_t kStep = kDownWide * 32u, kSlot = kDownWide * 1024u;
     const uint32_t steps = (m.I + kStep - 1u) / kStep, n_steps = r.n_entries * steps;
     const uint32_t first = (uint32_t)((uint64_t)n_steps * warp / kMoeWarps), last = (uint32_t)((uint64_t)n_steps * (warp + 1u) / kMoeWarps);
     const uint32_t en0 = first / steps, s0 = first - en0 * steps;
-    const uint32_t ring = smem_addr(smem) + kRouteBytes<kTokens> + down_sums(m.T) + warp * (kRing * kSlot) + lane * 16u;
+    const uint32_t ring = smem_addr(smem) + kFewBytes + down_sums(m.T) + warp * (kDownRing * kSlot) + lane * 16u;
     const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+    const size_t h_lo = (size_t)(m.h_lo - m.h_hi);
     bool waited = false;
     for (uint32_t d0 = blockIdx.x * m.rows; d0 < m.D; d0 += gridDim.x * m.rows) {
         const uint32_t rows = min(m.rows, m.D - d0);
         const bool row0 = row < rows, row1 = row + 8u < rows;
-        const uint16_t *down = m.experts + (size_t)2 * m.I * m.D + (size_t)(d0 + row) * m.I;
+        const uint16_t *down = m.experts + (size_t)2 * m.I * m.D + (size_t)(d0 + row) * m.I, *w = down;
         uint32_t in_left = last - first, in_en = en0, in_s = s0, in_slot = 0u;
-        const uint16_t *w = down;
         auto place = [&]() { if (in_left) w = down + (int64_t)r.expert[in_en] * m.expert_stride; };
         auto issue = [&]() {
             if (in_left) {
 #pragma unroll
-                for (int b = 0; b < kWide; ++b) {
+                for (int b = 0; b < kDownWide; ++b) {
                     const uint32_t k = in_s * kStep + b * 32u + quad * 8u, at = ring + in_slot * kSlot + b * 1024u;
                     const bool in = k < m.I;
                     copy_async16(at, in && row0 ? w + k : m.experts, in && row0);
                     copy_async16(at + 512u, in && row1 ? w + (size_t)8 * m.I + k : m.experts, in && row1);
                 }
-                in_slot = in_slot + 1u == kRing ? 0u : in_slot + 1u;
+                in_slot = in_slot + 1u == kDownRing ? 0u : in_slot + 1u;
                 --in_left;
                 if (++in_s == steps) { in_s = 0u; ++in_en; place(); }
             }
@@ -196,79 +178,62 @@ k_moe_down(const __grid_constant__ MoeDev m) {
         };
         place();
 #pragma unroll 1
-        for (int i = 0; i < kRing; ++i) issue();
+        for (int i = 0; i < kDownRing; ++i) issue();
         for (uint32_t i = lane; i < m.T * 16u; i += 32u) mine[i] = 0.0f;
         __syncwarp();
         if (!waited) { pdl_wait(); waited = true; }
-        uint32_t en = en0, s = s0, slot = 0u, n = 0u, pair0 = 0u;
-        uint4 now[kTiles][kWide][2];
-        const uint16_t *h = m.h_hi;                          // this lane's row of the entry's first tile
-        const size_t h_lo = (size_t)(m.h_lo - m.h_hi);
+        uint32_t en = en0, s = s0, slot = 0u, n = 0u, pair0 = 0u, left = last - first;
+        const uint16_t *h = m.h_hi;                          // this lane's row of the expert's tokens
         auto enter = [&]() { n = r.count[en]; pair0 = r.pair0[en]; h = m.h_hi + (size_t)(pair0 + row) * m.I; };
-        auto load = [&](uint4 (&v)[kTiles][kWide][2], uint32_t step) {
+        auto load = [&](uint4 (&v)[kDownWide][2], uint32_t step) {
 #pragma unroll
-            for (int j = 0; j < kTiles; ++j) {
-                if (j && j * 8u >= n) break;
-                const bool there = j * 8u + row < n;
-#pragma unroll
-                for (int b = 0; b < kWide; ++b) {
-                    const uint32_t k = step * kStep + b * 32u + quad * 8u;
-                    const bool in = there && k < m.I;
-                    const uint16_t *at = h + j * 8u * m.I + k;
-                    v[j][b][0] = in ? ld_after16(at) : zero;
-                    v[j][b][1] = in ? ld_after16(at + h_lo) : zero;
-                }
+            for (int b = 0; b < kDownWide; ++b) {
+                const uint32_t k = step * kStep + b * 32u + quad * 8u;
+                const bool in = row < n && k < m.I;
+                v[b][0] = in ? ld_after16(h + k) : zero;
+                v[b][1] = in ? ld_after16(h + h_lo + k) : zero;
             }
         };
-        if (first < last) { enter(); load(now, s); }
-        float acc[kTiles][2][4];                             // two chains of products each
+        uint4 now[kDownWide][2], then[kDownWide][2];
+        if (left) { enter(); load(now, s); }
+        float acc[2][4];                                     // two chains of products: the first and the second numbers
         auto clear = [&]() {
 #pragma unroll
-            for (int j = 0; j < kTiles; ++j)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) acc[j][0][c] = acc[j][1][c] = 0.0f;
+            for (int c = 0; c < 4; ++c) acc[0][c] = acc[1][c] = 0.0f;
         };
         clear();
-        uint32_t left = last - first;
-        auto turn = [&](uint4 (&cur)[kTiles][kWide][2], uint4 (&next)[kTiles][kWide][2]) {
+        auto turn = [&](uint4 (&cur)[kDownWide][2], uint4 (&next)[kDownWide][2]) {
             const uint32_t n_now = n, pair_now = pair0;
-            const bool done = ++s == steps || left == 1u;    // the entry is done, or this warp's part of it
+            const bool done = ++s == steps || left == 1u;    // the expert is done, or this warp's part of it
             if (s == steps) { s = 0u; ++en; if (left > 1u) enter(); }
             if (left > 1u) load(next, s);
-            copy_wait<kRing - 1>();
+            copy_wait<kDownRing - 1>();
 #pragma unroll
-            for (int b = 0; b < kWide; ++b) {
+            for (int b = 0; b < kDownWide; ++b) {
                 const uint4 w0 = ld_shared16(ring + slot * kSlot + b * 1024u), w1 = ld_shared16(ring + slot * kSlot + b * 1024u + 512u);
 #pragma unroll
-                for (int j = 0; j < kTiles; ++j)
-                    if (j == 0 || j * 8u < n_now) {
-                        const uint4 hi = cur[j][b][0], lo = cur[j][b][1];
-                        Ty::mma(acc[j][0], w0.x, w1.x, w0.y, w1.y, hi.x, hi.y);
-                        Ty::mma(acc[j][1], w0.x, w1.x, w0.y, w1.y, lo.x, lo.y);
-                        Ty::mma(acc[j][0], w0.z, w1.z, w0.w, w1.w, hi.z, hi.w);
-                        Ty::mma(acc[j][1], w0.z, w1.z, w0.w, w1.w, lo.z, lo.w);
-                    }
+                for (int c = 0; c < 2; ++c) {
+                    Ty::mma(acc[c], w0.x, w1.x, w0.y, w1.y, cur[b][c].x, cur[b][c].y);
+                    Ty::mma(acc[c], w0.z, w1.z, w0.w, w1.w, cur[b][c].z, cur[b][c].w);
+                }
             }
-            slot = slot + 1u == kRing ? 0u : slot + 1u;
+            slot = slot + 1u == kDownRing ? 0u : slot + 1u;
             issue();
             if (done) {
 #pragma unroll
-                for (int j = 0; j < kTiles; ++j)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const uint32_t rank = j * 8u + quad * 2u + c;
-                        if (rank < n_now) {
-                            float *to = mine + r.token[pair_now + rank] * 16u + row;
-                            to[0] += acc[j][0][c] + acc[j][1][c];
-                            to[8] += acc[j][0][c + 2] + acc[j][1][c + 2];
-                        }
+                for (int c = 0; c < 2; ++c) {
+                    const uint32_t rank = quad * 2u + c;
+                    if (rank < n_now) {
+                        float *to = mine + r.token[pair_now + rank] * 16u + row;
+                        to[0] += acc[0][c] + acc[1][c];
+                        to[8] += acc[0][c + 2] + acc[1][c + 2];
                     }
+                }
                 clear();
                 __syncwarp();
             }
             --left;
         };
-        uint4 then[kTiles][kWide][2];
 #pragma unroll 1
         while (left) {
             turn(now, then);
@@ -324,10 +289,10 @@ static bool moe_pointers_ok(const hbf_moe_t *m) {
 }
 // Whether the layer goes through k_moe_up and k_moe_down: two launches instead of four, some 8 us less, but 4.0 to 5.3 TB/s where moe_tiles.cu
 // reaches 5.7; the sides are even at about 220 MB of weights (2048 x 768, top 8 of 128: 2 tokens 40 us against 45, 3 tokens 53 against 52, 6 tokens
-// 86 against 68).  The number of experts in use is the router's; the most that there can be are counted.
+// 86 against 68; before the rings of now).  The number of experts in use is the router's; the most that there can be are counted.
 static bool moe_few(const hbf_moe_t *m) {
     const uint64_t pairs = (uint64_t)m->tokens * m->top_k, used = pairs < m->n_experts ? pairs : m->n_experts;
-    return m->tokens <= 8u && used * m->hidden * m->inter * 6u <= (220ull << 20);
+    return m->tokens <= (uint32_t)kFewTokens && used * m->hidden * m->inter * 6u <= (220ull << 20);
 }
 // The activations between the products, and past a few tokens the parts' sums and the choice; 0: the device cannot be asked.
 static size_t moe_bytes(const hbf_moe_t *m, uint32_t *groups) {
@@ -351,33 +316,23 @@ static MoeDev moe_dev(const hbf_moe_t *m) {
     return d;
 }
 
-// Up to 8 tokens a layer is a few tens of microseconds, and what counts is that nothing waits: both kernels fit an SM together, so
-// that the second has made its choice and has its first weights on their way when the first one ends.  Beyond, each has the SM to itself,
-// with longer rings; two tiles an entry where an expert has 16 tokens or fewer on average, else four.
-template <class Ty, int kTiles, int kTokens, int kUpRing, int kDownRing, int kWide, int kBlocks>
-static cudaError_t launch_moe_as(const MoeDev &d, uint32_t n_sm, cudaStream_t st) {
-    constexpr uint32_t up = up_smem<kTiles, kTokens, kUpRing>(), most_down = down_smem<kTokens, kDownRing, kWide>(kTokens);
-    static_assert(up <= 227 * 1024 && most_down <= 227 * 1024 && kRouteBytes<kTokens> + sizeof(RouteTemp<kTokens>) <= up, "shared memory");
-    static_assert(kBlocks == 1 || up + most_down <= 226 * 1024, "both kernels on an SM");
-    const auto up_k = k_moe_up<Ty, kTiles, kTokens, kUpRing, kBlocks>;
-    const auto down_k = k_moe_down<Ty, kTiles, kTokens, kDownRing, kWide, kBlocks>;
-    cudaError_t e = ensure_dyn_smem((const void *)up_k, up);
-    if (e == cudaSuccess) e = ensure_dyn_smem((const void *)down_k, most_down);
-    if (e != cudaSuccess) return e;
-    const uint64_t pairs = (uint64_t)d.T * d.K, most = (pairs < d.E + pairs / (kTiles * 8) ? pairs : d.E + pairs / (kTiles * 8)) * (d.I / 8u);
-    up_k<<<(unsigned)(most < n_sm ? most : n_sm), kMoeThreads, up, st>>>(d);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    const uint32_t blocks = (d.D + d.rows - 1u) / d.rows;
-    g_kernel_launches += 2;
-    return launch_pdl(down_k, blocks < n_sm ? blocks : n_sm, kMoeThreads, down_smem<kTokens, kDownRing, kWide>(d.T), st, d);
-}
 template <class Ty>
 static cudaError_t launch_moe(MoeDev d, bool few, uint32_t n_sm, cudaStream_t st) {
     d.div_slices = make_div32(d.I / 8u);
     // an even share of the output's rows to every SM, 16 at most: 2,048 rows are 14 a block on 147 blocks
     const uint32_t rounds = (d.D + 16u * n_sm - 1u) / (16u * n_sm);
     d.rows = (d.D + rounds * n_sm - 1u) / (rounds * n_sm);
-    if (few) return launch_moe_as<Ty, 1, 8, 5, 4, 1, 2>(d, n_sm, st);
+    if (few) {
+        cudaError_t e = ensure_dyn_smem((const void *)k_moe_up<Ty>, kUpSmem);
+        if (e == cudaSuccess) e = ensure_dyn_smem((const void *)k_moe_down<Ty>, down_smem(kFewTokens));
+        if (e != cudaSuccess) return e;
+        const uint64_t pairs = (uint64_t)d.T * d.K, most = (pairs < d.E ? pairs : d.E) * (d.I / 8u);
+        k_moe_up<Ty><<<(unsigned)(most < n_sm ? most : n_sm), kMoeThreads, kUpSmem, st>>>(d);
+        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        const uint32_t blocks = (d.D + d.rows - 1u) / d.rows;
+        g_kernel_launches += 2;
+        return launch_pdl(k_moe_down<Ty>, blocks < n_sm ? blocks : n_sm, kMoeThreads, down_smem(d.T), st, d);
+    }
     return launch_moe_tiles(d, std::is_same<Ty, Bf16>::value, n_sm, st);
 }
 
