@@ -1,4 +1,4 @@
-// A mixture-of-experts layer for up to eight tokens in two kernels (moe_tiles.cu has the form for more, or for many bytes of weights).
+// A mixture-of-experts layer for up to eight tokens in two kernels (moe_tiles.cu has the form for more).
 //
 //   choice      the top_k largest of a token's scores, ties to the lowest expert; weights w = softmax over the chosen (or over all)
 //   k_moe_up    h[pair] = w * silu(gate x) * (up x)             for every (expert, token that chose it) pair
@@ -287,13 +287,9 @@ static bool moe_pointers_ok(const hbf_moe_t *m) {
     if (!m->scores || !m->experts || (uintptr_t)m->experts % 16 || (uintptr_t)m->scores % 4 || m->scores_stride < (int64_t)m->n_experts) return false;
     return true;
 }
-// Whether the layer goes through k_moe_up and k_moe_down: two launches instead of four, some 8 us less, but 4.0 to 5.3 TB/s where moe_tiles.cu
-// reaches 5.7; the sides are even at about 220 MB of weights (2048 x 768, top 8 of 128: 2 tokens 40 us against 45, 3 tokens 53 against 52, 6 tokens
-// 86 against 68; before the rings of now).  The number of experts in use is the router's; the most that there can be are counted.
-static bool moe_few(const hbf_moe_t *m) {
-    const uint64_t pairs = (uint64_t)m->tokens * m->top_k, used = pairs < m->n_experts ? pairs : m->n_experts;
-    return m->tokens <= (uint32_t)kFewTokens && used * m->hidden * m->inter * 6u <= (220ull << 20);
-}
+// Whether the layer goes through k_moe_up and k_moe_down: two launches instead of four, and for these few tokens faster whatever the
+// weights (2048 x 768, top 8 of 128, 8 tokens, 351 MB in use: 75.6 us against 93.8; 4096 x 2048, top 2 of 8: 64.6 against 78.8).
+static bool moe_few(const hbf_moe_t *m) { return m->tokens <= (uint32_t)kFewTokens; }
 // The activations between the products, and past a few tokens the parts' sums and the choice; 0: the device cannot be asked.
 static size_t moe_bytes(const hbf_moe_t *m, uint32_t *groups) {
     const size_t pairs = (size_t)m->tokens * m->top_k, h = (pairs * m->inter * 4u + 255u) / 256u * 256u;
