@@ -432,7 +432,8 @@ HBF_API int hbf_get_retention_totals(hbf_ctx *ctx, hbf_retention_totals_t *out);
  * ..._workspace_bytes function gives for the same arguments on the same device (0 = arguments refused); two calls that may overlap,
  * on two streams or in two graphs that are replayed at once, need one each.  Every call can be captured into a CUDA graph; a replay reads
  * the tables, lengths and scores anew.  Counts in the structs are fixed at capture.
- * Values are bf16 or fp16, products exact, sums in 32 bits, outputs rounded once. */
+ * Values are bf16 or fp16, products exact, sums in 32 bits, outputs rounded once.  Kernels that wait on copies or products of their own wait a
+ * bounded number of polls; should that run out, what depends on it is NaN. */
 enum { HBF_BF16 = 0, HBF_FP16 = 1 };
 
 /* A paged key/value cache of one layer: the key of slot s of page g, key head h, begins at k + g * page_stride + s * slot_stride +

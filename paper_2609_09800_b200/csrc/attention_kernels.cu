@@ -401,7 +401,7 @@ static void attention_pieces(const hbf_attention_t *a, uint32_t n_sm, AttnDev &p
     p.row_tiles = (p.B * G + p.prefix_rows - 1u) / p.prefix_rows;
     p.group_tiles = (G + p.rows - 1u) / p.rows;
     p.prefix_pieces = 0u; p.prefix_chunk = 64u;
-    if (a->prefix_len) {
+    if (a->prefix_len && p.B) {
         // (k_prefix_tiles: a block an SM, tiles of 128 keys)
         const uint32_t step = p.prefix_rows == 256u ? 128u : 64u, there = p.prefix_rows == 256u ? n_sm : blocks;
         const uint32_t pairs = p.row_tiles * p.Hk, most = (a->prefix_len + step - 1u) / step;
@@ -410,7 +410,7 @@ static void attention_pieces(const hbf_attention_t *a, uint32_t n_sm, AttnDev &p
         p.prefix_pieces = (a->prefix_len + p.prefix_chunk - 1u) / p.prefix_chunk;
     }
     p.own_pieces = 0u; p.own_chunk = 64u;
-    if (a->max_own_len) {
+    if (a->max_own_len && p.B) {
         const uint64_t lists = (uint64_t)p.B * p.Hk * p.group_tiles;
         const uint64_t want = lists < 2u * blocks ? 2u * blocks / lists : 1u;
         uint64_t chunk = (a->max_own_len + want - 1u) / want;
@@ -439,7 +439,7 @@ static AttnDev attention_dev(const hbf_attention_t *a, uint32_t n_sm) {
     return p;
 }
 static size_t attention_bytes(const AttnDev &p, uint32_t dim) {
-    if (p.pieces <= 1u) return 256u;
+    if (p.pieces <= 1u || p.B == 0u) return 256u;
     return ((size_t)p.pieces * p.B * p.Hq * (dim * 4u + 8u) + 255u) / 256u * 256u;
 }
 

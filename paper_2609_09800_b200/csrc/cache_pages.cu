@@ -19,7 +19,7 @@ struct PagesCtrl { int32_t code, moves, n_live; };   // the first words of the w
 
 struct PagesDev {
     unsigned char *base; uint64_t page_bytes, page_stride, slab_stride;
-    uint32_t n_slabs, n_pages, page_tokens, rows, cols; int64_t table_stride;
+    uint32_t n_slabs, n_pages, page_tokens, rows, cols, most; int64_t table_stride;      // most: moves that the workspace has places for
     int32_t *refs, *lens, *tables, *result;
     PagesCtrl *ctrl; int32_t *src, *dst, *extra;             // moves; for a fork the rows' lengths and new pages, for a compaction the pages' new numbers
     Div32 div_slabs;
@@ -312,7 +312,7 @@ k_plan_compact(const __grid_constant__ PagesDev p, int alone) {
 // at address 0, outside every range.
 __global__ void __launch_bounds__(kMoveThreads)
 k_pages_accesses(const __grid_constant__ PagesDev p, int64_t issue_ns, int64_t gap_ns, hbf_access_t *acc, uint64_t n) {
-    const uint64_t moves = p.ctrl->code == HBF_OK ? (uint64_t)p.ctrl->moves : 0u;
+    const uint64_t moves = p.ctrl->code == HBF_OK ? min((uint32_t)p.ctrl->moves, p.most) : 0u;          // (whatever lies there)
     for (uint64_t i = (uint64_t)blockIdx.x * kMoveThreads + threadIdx.x; i < n; i += (uint64_t)gridDim.x * kMoveThreads) {
         hbf_access_t v = {0, issue_ns + (int64_t)i * gap_ns, 1, 0};
         const uint64_t u = i >> 1;
@@ -351,7 +351,7 @@ static PagesDev pages_dev(const hbf_pages_t *p, void *ws, int32_t *result) {
     d.n_slabs = p->n_slabs; d.n_pages = p->n_pages; d.page_tokens = p->page_tokens; d.rows = p->rows; d.cols = p->rows ? p->table_cols : 0u; d.table_stride = p->table_stride;
     d.refs = p->refs; d.lens = p->lens; d.tables = p->tables; d.result = result;
     const size_t most = p->n_pages > p->rows ? p->n_pages : p->rows;
-    d.ctrl = static_cast<PagesCtrl *>(ws);
+    d.most = (uint32_t)most; d.ctrl = static_cast<PagesCtrl *>(ws);
     d.src = reinterpret_cast<int32_t *>(static_cast<unsigned char *>(ws) + 256); d.dst = d.src + most; d.extra = d.dst + most;
     d.div_slabs = make_div32(p->n_slabs);
     return d;

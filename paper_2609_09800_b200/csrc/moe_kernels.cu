@@ -338,7 +338,7 @@ using namespace hbf;
 
 extern "C" size_t hbf_moe_workspace_bytes(const hbf_moe_t *m) {
     if (!moe_ok(m)) return 0;
-    return moe_bytes(m, nullptr);
+    return m->tokens ? moe_bytes(m, nullptr) : 256u;
 }
 
 extern "C" int hbf_moe_layer(const hbf_moe_t *m, void *d_workspace, size_t workspace_bytes, void *cuda_stream) {

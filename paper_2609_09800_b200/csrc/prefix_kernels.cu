@@ -397,6 +397,14 @@ static cudaError_t launch_tiles(const AttnDev &p, cudaStream_t st) {
     const auto k = k_prefix_tiles<Ty, D, kBf16>;
     cudaError_t e = ensure_dyn_smem((const void *)k, pf_smem<D>());
     if (e != cudaSuccess) return e;
+    // the warps' shares of the registers add up to what a block is launched with only if that is 80 a thread
+    static std::atomic<int> regs{0};
+    if (regs.load(std::memory_order_relaxed) == 0) {
+        cudaFuncAttributes at = {};
+        if ((e = cudaFuncGetAttributes(&at, k)) != cudaSuccess) return e;
+        regs.store(at.numRegs, std::memory_order_relaxed);
+    }
+    if (regs.load(std::memory_order_relaxed) != 80) return cudaErrorInvalidKernelImage;
     g_kernel_launches += 1;
     CUtensorMap k_map = {}, v_map = {};
     uint32_t box = p.page_tokens & (0u - p.page_tokens);     // the largest power of two that a page is a multiple of

@@ -143,6 +143,31 @@ def test_wide_against_64_bits(torch, serving, shape, dtype):
     c.check(c.plan(serving)(c.q, lse=lse), lse)
 
 
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 12)])
+def test_wide_in_one_piece(torch, serving, d, page):
+    """So many rows that every block has all keys of its rows and writes the output itself."""
+    c = Case(torch, 1216, 64, 8, d, page, 300, 0, seed=9)
+    lse = torch.empty(c.B, c.Hq, device="cuda")
+    c.check(c.plan(serving)(c.q, lse=lse), lse)
+
+
+def test_nobody(torch, serving):
+    """A batch of no requests: nothing is read or written, by any of the calls."""
+    from paper_2609_09800_b200 import hbf
+    import ctypes as C
+    c = Case(torch, 2, 8, 2, 64, 16, 40, 20, poison=False)
+    a = c.plan(serving)._a
+    a.batch = 0
+    lib = hbf.lib()
+    assert lib.hbf_attention_workspace_bytes(C.byref(a)) == 256
+    assert lib.hbf_prefix_attention(C.byref(a), None, 0, None) == hbf.OK
+    n = lib.hbf_attention_access_count(C.byref(a))
+    assert n == 6
+    rec = torch.empty(n, 3, dtype=torch.int64, device="cuda")
+    assert lib.hbf_attention_accesses(C.byref(a), 0, 0, rec.data_ptr(), n, None) == hbf.OK
+    assert (rec[:, 0] > 0).all()
+
+
 @pytest.mark.parametrize("layout", ["heads", "gaps"])
 @pytest.mark.parametrize("d", [64, 128])
 def test_wide_page_layouts(torch, serving, layout, d):
@@ -306,6 +331,15 @@ def test_nan_and_infinity_in_keys_in_use_are_not_lost(torch, serving, B):
     c.k[c.op[1, 0].long(), 0, 0] = math.nan
     out = c.plan(serving)(c.q)
     assert torch.isnan(out[1, :4]).all() and torch.isfinite(out[1, 4:]).all() and torch.isfinite(out[0]).all()
+
+
+@pytest.mark.parametrize("what", ["pages", "heads"])
+def test_a_stride_of_zero(torch, serving, what):
+    """Pages, or key heads, that are all the same memory."""
+    for B in (3, 128):
+        c = Case(torch, B, 32, 4, 64, 16, 900, 20, poison=False)
+        c.k, c.v = (t[:1].expand(t.shape) if what == "pages" else t[:, :, :1].expand(t.shape) for t in (c.k, c.v))
+        c.check(c.plan(serving)(c.q))
 
 
 def test_offsets_past_32_bits(torch, serving):

@@ -258,6 +258,37 @@ def test_captured_and_replayed(torch, serving):
         torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("pages", [392_100, 393_216, 1 << 20])
+def test_caches_of_many_pages(torch, serving, pages):
+    """Marks of all pages in shared memory, at its sizes' border and at the most pages that there may be."""
+    data = torch.zeros(1, pages, 4, dtype=torch.int32, device="cuda")
+    data[0, :, 0] = torch.arange(pages, device="cuda")
+    refs, lens = torch.zeros(pages, dtype=torch.int32, device="cuda"), torch.tensor([2, 0], dtype=torch.int32, device="cuda")
+    held = torch.tensor([pages - 1, 7], device="cuda", dtype=torch.int32)
+    refs[held.long()] = 1
+    tables = torch.stack([held, torch.full_like(held, -1)])
+    plan = serving.CachePages(data, refs, tables, lens, 1)
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    plan.copy(ints(5), ints(pages - 2))
+    assert plan.result()["moved"] == 1 and int(data[0, pages - 2, 0]) == 5
+    plan.fork(ints(0), ints(1))
+    plan.result()
+    plan.compact()
+    assert plan.result() == {"moved": 2, "in_use": 2}
+    assert tables.tolist() == [[1, 0], [1, 0]] and data[0, :2, 0].tolist() == [7, pages - 1] and refs[:3].tolist() == [2, 2, 0]
+
+
+def test_records_before_any_call(torch, serving):
+    c = Cache(torch, 2, 30, 8, 4, 6, 5)
+    plan = c.plan(serving)
+    assert plan.accesses().shape[0] == 0
+    plan._ws.random_(0, 256)                                 # whatever lies in a workspace
+    plan._ws[:4] = 0
+    plan._moves = 40
+    rec = plan.accesses()
+    assert rec.shape[0] == 160
+
+
 def test_offsets_past_32_bits(torch, serving):
     pages, words = 5000, 4096 * 64                           # 5.2 GB
     data = torch.zeros(1, pages, words, dtype=torch.int32, device="cuda")
