@@ -192,50 +192,53 @@ k_plan_fork(const __grid_constant__ PagesDev p, const int32_t *parents, const in
     __shared__ int s_bad;
     pdl_trigger();
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = lane_id();
+    const bool free0 = tid < p.n_pages && p.refs[tid] == 0;  // (asked for now: what the pages' search begins with)
     for (uint32_t i = tid; i < (p.rows + 31u) / 32u; i += kPlanThreads) bits[i] = 0u;
     if (tid == 0) s_bad = 0;
     __syncthreads();
+    // The rows of the list: their lengths; the begun pages, in the order of the list; where another parent than the one before it begins (in
+    // p.dst for now).  One scan for both counts.
     int bad = 0;
-    for (uint32_t i = tid; i < n; i += kPlanThreads) {
-        const uint32_t a = (uint32_t)parents[i], c = (uint32_t)children[i];
-        if (a >= p.rows || c >= p.rows || len_bad(p, p.lens[a]) || p.lens[c] != 0) bad = 1;
-        else if ((atomicOr(&bits[c >> 5], 1u << (c & 31u)) >> (c & 31u)) & 1u) bad = 1;
-        else p.extra[i] = p.lens[a];
+    uint32_t need = 0u, runs = 0u;
+    for (uint32_t i0 = 0; i0 < n; i0 += kPlanThreads) {
+        const uint32_t i = i0 + tid;
+        uint32_t begun = 0u, run = 0u;
+        int32_t from = 0;
+        if (i < n) {
+            const uint32_t a = (uint32_t)parents[i], c = (uint32_t)children[i], before = i ? (uint32_t)parents[i - 1u] : ~a;
+            const int32_t len = a < p.rows ? p.lens[a] : -1;
+            if (a >= p.rows || c >= p.rows || len_bad(p, len) || p.lens[c] != 0) bad = 1;
+            else if ((atomicOr(&bits[c >> 5], 1u << (c & 31u)) >> (c & 31u)) & 1u) bad = 1;
+            else {
+                p.extra[i] = len;
+                run = a != before ? 1u : 0u;
+                begun = (uint32_t)len % p.page_tokens ? 1u : 0u;
+                if (begun) from = p.tables[(int64_t)a * p.table_stride + (uint32_t)len / p.page_tokens];
+            }
+        }
+        uint32_t total;
+        const uint32_t at = block_scan(run << 16 | begun, &total, warps);
+        if (run) p.dst[runs + (at >> 16)] = (int32_t)i;
+        if (begun) { p.src[need + (at & 0xffffu)] = from; p.extra[n + i] = (int32_t)(need + (at & 0xffffu)); }
+        need += total & 0xffffu; runs += total >> 16;
     }
     if (bad) s_bad = 1;
     __syncthreads();
     if (s_bad) { finish_plan<kDoFork>(p, HBF_E_INVAL, 0u, 0u, parents, children, n, 0); return; }
     // the parents' pages, a parent named several times in a row once: few parents by the whole block, many by a warp each
-    uint32_t runs = 0u;
-    for (uint32_t i = tid; i < n; i += kPlanThreads) runs += i == 0u || parents[i] != parents[i - 1u] ? 1u : 0u;
-    uint32_t all_runs;
-    block_scan(runs, &all_runs, warps);
-    const bool wide = all_runs <= 4u;
-    for (uint32_t i = wide ? 0u : warp; i < n; i += wide ? 1u : kPlanThreads / 32) {
-        if (i && parents[i] == parents[i - 1u]) continue;
+    const bool wide = runs <= 4u;
+    for (uint32_t k = wide ? 0u : warp; k < runs; k += wide ? 1u : kPlanThreads / 32) {
+        const uint32_t i = (uint32_t)p.dst[k];
         bad |= row_bad(p, (uint32_t)parents[i], p.extra[i], wide ? tid : lane, wide ? kPlanThreads : 32u);
     }
     if (bad) s_bad = 1;
-    // the begun pages in the order of the list
-    uint32_t need = 0u;
-    for (uint32_t i0 = 0; i0 < n; i0 += kPlanThreads) {
-        const uint32_t i = i0 + tid;
-        const int32_t len = i < n ? p.extra[i] : 0;
-        const uint32_t begun = (uint32_t)len % p.page_tokens ? 1u : 0u;
-        uint32_t total;
-        const uint32_t at = need + block_scan(begun, &total, warps);
-        if (begun) {
-            p.src[at] = p.tables[(int64_t)parents[i] * p.table_stride + (uint32_t)len / p.page_tokens];
-            p.extra[n + i] = (int32_t)at;
-        }
-        need += total;
-    }
+    __syncthreads();
     if (s_bad) { finish_plan<kDoFork>(p, HBF_E_INVAL, 0u, 0u, parents, children, n, 0); return; }
     // as many free pages, the lowest
     uint32_t found = 0u;
     for (uint32_t i0 = 0; i0 < p.n_pages && found < need; i0 += kPlanThreads) {
         const uint32_t i = i0 + tid;
-        const bool free = i < p.n_pages && p.refs[i] == 0;
+        const bool free = i0 ? i < p.n_pages && p.refs[i] == 0 : free0;
         const unsigned b = __ballot_sync(0xffffffffu, free);
         if (lane == 0u) warps[warp] = __popc(b);
         __syncthreads();
