@@ -50,7 +50,7 @@ __device__ uint32_t block_scan(uint32_t v, uint32_t *total, uint32_t *warps) {
 }
 
 // Every thread of the plan's block ends with this; with `alone` the block goes on with what the other kernel would do.
-template <int kDo, uint32_t kThreads> __device__ __forceinline__ void apply_plan(const PagesDev &p, const int32_t *a, const int32_t *b, uint32_t n, bool bulk);
+template <int kDo, uint32_t kThreads> __device__ __forceinline__ void apply_plan(const PagesDev &p, const int32_t *a, const int32_t *b, uint32_t n);
 template <int kDo>
 __device__ __forceinline__ void finish_plan(const PagesDev &p, int code, uint32_t moves, uint32_t n_live, const int32_t *a, const int32_t *b, uint32_t n, int alone) {
     if (threadIdx.x == 0) {
@@ -60,55 +60,13 @@ __device__ __forceinline__ void finish_plan(const PagesDev &p, int code, uint32_
     }
     if (!alone) return;
     __syncthreads();                                         // (the moves that other threads wrote are there, too)
-    apply_plan<kDo, kPlanThreads>(p, a, b, n, false);
+    apply_plan<kDo, kPlanThreads>(p, a, b, n);
 }
 
-
-// Pages through shared memory by bulk copies, in pieces of up to 16 KB, that one thread of a block issues: a piece's store begins three pieces
-// after its load, and its place is loaded again when that store has read it.
-constexpr uint32_t kPiece = 16384, kPieces = 6, kBehind = 3;
-constexpr uint32_t kBulkSmem = kPiece * kPieces;
-__device__ __forceinline__ void move_bulk(const PagesDev &p, uint32_t units) {
-    extern __shared__ __align__(128) unsigned char piece_smem[];
-    __shared__ uint64_t full[kPieces];
-    if (threadIdx.x != 0) return;
-    const uint32_t bars = smem_addr(full), ring = smem_addr(piece_smem);
-    for (uint32_t i = 0; i < kPieces; ++i) bar_init(bars + i * 8u, 1u);
-    bar_init_done();
-    asm volatile("fence.proxy.async;" ::: "memory");
-    const uint32_t per = ((uint32_t)p.page_bytes + kPiece - 1u) / kPiece;
-    const uint64_t all = (uint64_t)units * per, mine = all > blockIdx.x ? (all - blockIdx.x + gridDim.x - 1u) / gridDim.x : 0u;
-    bool live = true;
-    auto place = [&](uint64_t i, const int32_t *pages, uint32_t &bytes) {
-        const uint64_t q = blockIdx.x + i * gridDim.x;
-        const uint32_t u = (uint32_t)(q / per), off = (uint32_t)(q - (uint64_t)u * per) * kPiece, k = div32(u, p.div_slabs);
-        bytes = min(kPiece, (uint32_t)p.page_bytes - off);
-        return p.base + (uint64_t)(u - k * p.n_slabs) * p.slab_stride + (uint64_t)pages[k] * p.page_stride + off;
-    };
-    for (uint64_t i = 0; i < mine + kBehind; ++i) {
-        uint32_t bytes;
-        if (i >= kBehind) {
-            const uint64_t j = i - kBehind;
-            const uint32_t s = (uint32_t)(j % kPieces);
-            live = bar_wait(bars + s * 8u, (uint32_t)(j / kPieces) & 1u, live);
-            unsigned char *to = place(j, p.dst, bytes);
-            if (live) bulk_store(to, ring + s * kPiece, bytes);
-        }
-        if (i < mine && live) {
-            const uint32_t s = (uint32_t)(i % kPieces);
-            if (i >= kPieces) bulk_read_wait<kPieces - kBehind>();
-            const unsigned char *from = place(i, p.src, bytes);
-            bar_arrive_bytes(bars + s * 8u, bytes);
-            bulk_load(ring + s * kPiece, from, bytes, bars + s * 8u);
-        }
-    }
-    bulk_done_wait();
-    if (!live && p.result) p.result[0] = HBF_E_TIMEOUT;
-}
 
 // What the plan found: the rows' tables and the references, then the pages' bytes, a page of a slab a block at a time.
 template <int kDo, uint32_t kThreads>
-__device__ __forceinline__ void apply_plan(const PagesDev &p, const int32_t *a, const int32_t *b, uint32_t n, bool bulk) {
+__device__ __forceinline__ void apply_plan(const PagesDev &p, const int32_t *a, const int32_t *b, uint32_t n) {
     const PagesCtrl c = *p.ctrl;
     if (c.code != HBF_OK) return;
     const uint32_t moves = (uint32_t)c.moves;
@@ -161,10 +119,6 @@ __device__ __forceinline__ void apply_plan(const PagesDev &p, const int32_t *a, 
         return;
     }
     const uint32_t units = moves * p.n_slabs;
-    if (bulk) {
-        move_bulk(p, units);
-        return;
-    }
     for (uint32_t u = blockIdx.x; u < units; u += gridDim.x) {
         const uint32_t k = div32(u, p.div_slabs), s = u - k * p.n_slabs;
         const unsigned char *from = p.base + s * p.slab_stride + (uint64_t)p.src[k] * p.page_stride;
@@ -189,9 +143,9 @@ __device__ __forceinline__ void apply_plan(const PagesDev &p, const int32_t *a, 
 
 template <int kDo>
 __global__ void __launch_bounds__(kMoveThreads)
-k_pages_apply(const __grid_constant__ PagesDev p, const int32_t *a, const int32_t *b, uint32_t n, int bulk) {
+k_pages_apply(const __grid_constant__ PagesDev p, const int32_t *a, const int32_t *b, uint32_t n) {
     pdl_wait();
-    apply_plan<kDo, kMoveThreads>(p, a, b, n, bulk != 0);
+    apply_plan<kDo, kMoveThreads>(p, a, b, n);
 }
 
 // The listed pairs are sound if every page exists, no destination is named twice and none is a source too (their order would count).
@@ -374,7 +328,6 @@ k_pages_accesses(const __grid_constant__ PagesDev p, int64_t issue_ns, int64_t g
     }
 }
 
-constexpr uint64_t kBulkPage = 4096;
 static bool pages_ok(const hbf_pages_t *p) {
     if (!p || !p->base || (uintptr_t)p->base % 16 || p->page_bytes == 0 || p->page_bytes % 16 || p->page_bytes > 0xfffffff0ull) return false;
     if (p->page_stride % 16 || p->slab_stride % 16 || p->page_stride < p->page_bytes || p->n_slabs == 0 || p->n_slabs > 65536u) return false;
@@ -425,13 +378,9 @@ static int pages_call(const hbf_pages_t *p, const int32_t *a, const int32_t *b, 
     plan<<<1, kPlanThreads, smem, st>>>(d, args..., alone);
     if (cudaGetLastError() != cudaSuccess) return HBF_E_CUDA;
     if (alone) { g_kernel_launches += 1; return HBF_OK; }
-    // pages of some KB by bulk copies, two blocks an SM
-    const bool bulk = p->page_bytes >= kBulkPage;
-    const uint64_t there = (bulk ? 2ull : 8ull) * n_sm, blocks = work < 1 ? 1 : work < there ? work : there;
-    const size_t move_smem = bulk ? kBulkSmem : 0u;
-    if (ensure_dyn_smem((const void *)k_pages_apply<kDo>, move_smem) != cudaSuccess) return HBF_E_CUDA;
+    const uint64_t blocks = work < 1 ? 1 : work < 8ull * n_sm ? work : 8ull * n_sm;
     g_kernel_launches += 2;
-    return launch_pdl(k_pages_apply<kDo>, (unsigned)blocks, kMoveThreads, move_smem, st, d, a, b, n, bulk ? 1 : 0) == cudaSuccess ? HBF_OK : HBF_E_CUDA;
+    return launch_pdl(k_pages_apply<kDo>, (unsigned)blocks, kMoveThreads, 0, st, d, a, b, n) == cudaSuccess ? HBF_OK : HBF_E_CUDA;
 }
 
 }  // namespace hbf
