@@ -284,7 +284,7 @@ class ServedLayer:
             full, started = divmod(prefix_tokens, page_tokens)
             mine = -(-(started + own_tokens) // page_tokens)      # pages of a request behind the full ones that it shares
             held = full + (1 if started else 0)
-            pages = held + batch * mine + 1
+            pages = max(held + batch * mine, 1) + 1           # (the last is nobody's: see `append`)
             self.kv = rnd(2, pages, page_tokens, kv_heads, head_dim)
             i32 = lambda *s: torch.full(s, -1, dtype=torch.int32, device=dev)
             self.refs, self.lens, self.tables = i32(pages).fill_(0), i32(batch + 1).fill_(0), i32(batch + 1, full + mine + 1)
@@ -293,7 +293,7 @@ class ServedLayer:
             self.lens[0] = prefix_tokens
             self.own_len = torch.zeros(batch, dtype=torch.int32, device=dev)
             self._rows = torch.arange(1, batch + 1, device=dev, dtype=torch.int32)
-        self.cache = CachePages(self.kv, self.refs, self.tables, self.lens, page_tokens, stream=ctx.stream)
+        self.cache = CachePages(self.kv[:, :-1], self.refs[:-1], self.tables, self.lens, page_tokens, stream=ctx.stream)
         self.cache.fork(torch.zeros_like(self._rows), self._rows)
         self.cache.result()
         with torch.cuda.stream(ctx.stream):                       # the pages that the requests will grow into, the lowest free ones
@@ -312,13 +312,18 @@ class ServedLayer:
             offset += -(-t.numel() * t.element_size() // (1 << 20)) << 20
 
     def append(self, k, v):
-        """Every request's next token: k, v [batch, kv_heads, head_dim] go into its cache."""
+        """Every request's next token: k, v [batch, kv_heads, head_dim] go into its cache.  A request that has no page for it (its room is used up, or
+        its row was freed) stays as it is.  Returns who took it, bool [batch], on the device."""
         import torch
         with torch.cuda.stream(self.ctx.stream):
             at = self.lens[1:].long()
-            page = self.tables[1:].gather(1, (at // self.page)[:, None])[:, 0].long()
+            col, last = at // self.page, self.tables.shape[1] - 1
+            page = self.tables[1:].gather(1, col.clamp(max=last)[:, None])[:, 0].long()
+            took = (page >= 0) & (col <= last)
+            page = torch.where(took, page, self.kv.shape[1] - 1)
             self.kv[0, page, at % self.page], self.kv[1, page, at % self.page] = k, v
-            self.lens[1:] += 1
+            self.lens[1:] += took
+        return took
 
     def step(self, q, x, scores, issue_ns=0, gap_ns=0):
         """Attention of the requests' queries q [batch, q_heads, head_dim], then the experts on x [batch, hidden] by the router's scores [batch,

@@ -109,6 +109,38 @@ def test_a_serving_loop(torch, mods):
     assert close(torch, after[keep], want[keep])
 
 
+@pytest.mark.parametrize("prefix, own", [(40, 5), (48, 16), (7, 0), (0, 3), (0, 0)])
+def test_requests_stop_growing_where_their_room_ends(torch, mods, prefix, own):
+    hbf, serving = mods
+    ctx = hbf.Context(wl.load_profile("nominal", **wl.GEOMETRY["serving"]))
+    layer = serving.ServedLayer(ctx, **dict(SMALL, batch=3, prefix_tokens=prefix, own_tokens=own))
+    room = -(-(prefix % 16 + own) // 16) * 16 - prefix % 16      # tokens that the pages hold
+    rnd = lambda *s: torch.randn(*s, device="cuda").bfloat16()
+    for i in range(room + 40):
+        full = layer.kv.clone() if i >= room else None
+        assert layer.append(rnd(3, 4, 64), rnd(3, 4, 64)).tolist() == [i < room] * 3
+        assert layer.lens.tolist() == [prefix] + [prefix + min(i + 1, room)] * 3
+        assert full is None or torch.equal(full[:, :-1], layer.kv[:, :-1])
+    q = rnd(3, 16, 64)
+    out, _, _ = layer.step(q, rnd(3, 256), torch.randn(3, 12, device="cuda"))
+    assert close(torch, out, reference(torch, layer, q))
+
+
+def test_a_freed_request_takes_no_token(torch, mods):
+    hbf, serving = mods
+    ctx = hbf.Context(wl.load_profile("nominal", **wl.GEOMETRY["serving"]))
+    layer = serving.ServedLayer(ctx, **dict(SMALL, batch=3, prefix_tokens=40, own_tokens=5))
+    rnd = lambda *s: torch.randn(*s, device="cuda").bfloat16()
+    layer.cache.free(torch.tensor([2], device="cuda", dtype=torch.int32))
+    layer.cache.result()
+    assert layer.append(rnd(3, 4, 64), rnd(3, 4, 64)).tolist() == [True, False, True] and layer.lens.tolist() == [40, 41, 0, 41]
+    layer.cache.fork(torch.tensor([0], device="cuda", dtype=torch.int32), torch.tensor([2], device="cuda", dtype=torch.int32))
+    layer.cache.result()
+    q = rnd(3, 16, 64)
+    out, _, _ = layer.step(q, rnd(3, 256), torch.randn(3, 12, device="cuda"))
+    assert layer.lens.tolist() == [40, 41, 40, 41] and close(torch, out, reference(torch, layer, q))
+
+
 def test_serving_needs_the_same_stream(torch, mods):
     hbf, serving = mods
     ctx = hbf.Context(wl.load_profile("nominal", **wl.GEOMETRY["tiny"]))
