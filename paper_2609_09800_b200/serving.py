@@ -166,6 +166,7 @@ class MoeLayer(_Operator):
         m.scores, m.scores_stride = scores.data_ptr(), ss[0] if n > 1 else m.n_experts
         m.out, m.out_stride = out.data_ptr(), os[0] if n > 1 else m.hidden
         m.chosen, m.weights = None if chosen is None else chosen.data_ptr(), None if weights is None else weights.data_ptr()
+        self._last = None                                    # a call that is refused has no accesses
         rc = self._lib.hbf_moe_layer(self._ref, self._ws_ptr, self._ws_bytes, self._st)
         if rc:
             self._raise(rc, "hbf_moe_layer")

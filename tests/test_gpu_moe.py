@@ -278,3 +278,17 @@ def test_records(torch, serving):
     want = [[c.w.data_ptr() + e * row + o, min(5000, size - o)] for e in used for o in range(0, size, 5000)]
     want += [[0, 1]] * (15 * 3 - len(want))
     assert [[a, b] for a, _, b in rec] == want and [i for _, i, _ in rec] == [50 + 3 * k for k in range(45)]
+
+
+@pytest.mark.parametrize("T", [4, 20])
+def test_a_refused_call_has_no_records(torch, serving, T):
+    from paper_2609_09800_b200 import hbf
+    c = Case(torch, T, 64, 32, 8, 2)
+    plan = c.plan(serving, tile_bytes=4096)
+    plan(c.x, c.scores)
+    assert plan.accesses().shape[0] == plan.access_count() > 0
+    with pytest.raises(hbf.HbfError):                        # not on a 16-byte boundary
+        plan(torch.empty(T * 64 + 8, dtype=c.dt, device="cuda")[4:][:T * 64].view(T, 64), c.scores.clone())
+    assert plan.access_count() == 0 and plan.accesses().shape[0] == 0
+    plan(c.x[:1], c.scores[:1])
+    assert plan.access_count() == 2 * 3
