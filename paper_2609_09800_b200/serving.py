@@ -220,9 +220,9 @@ class CachePages(_Operator):
         return t.data_ptr()
 
     def _done(self, rc, what, moves):
-        self._what, self._moves = what, moves
-        if rc:
+        if rc:                                               # refused here: `result` and `accesses` stay those of the call before
             self._raise(rc, what)
+        self._what, self._moves = what, moves
 
     def copy(self, src, dst):
         """Page src[i]'s bytes to page dst[i], in every slab."""

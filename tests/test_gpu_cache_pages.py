@@ -334,3 +334,19 @@ def test_binding_refuses(torch, serving, hbf):
         serving.CachePages(c.data[:, :, :6].contiguous(), c.refs, c.tables, c.lens, 4)      # pages of 24 bytes
     with pytest.raises(hbf.HbfError):
         plan.free(c.ints([0] * 7))                           # more than there are rows
+
+
+def test_a_call_refused_at_once_leaves_the_records_of_the_one_before(torch, serving, hbf):
+    c = Cache(torch, 2, 30, 8, 4, 6, 5)
+    c.fill(0, 10)
+    c.upload()
+    plan = c.plan(serving)
+    plan.copy(c.ints([1, 2, 3]), c.ints([11, 12, 13]))
+    n, want = plan.access_count(), plan.accesses(7, 2).tolist()
+    assert n == 2 * 3 * 2
+    with pytest.raises(hbf.HbfError):
+        plan.free(c.ints([0] * 7))                           # more than there are rows
+    assert plan.access_count() == n and plan.accesses(7, 2).tolist() == want and plan.result()["moved"] == 3
+    with pytest.raises(hbf.HbfError):
+        plan.copy(c.ints([1] * 31), c.ints([2] * 31))        # more than there are pages
+    assert plan.access_count() == n and plan.accesses(7, 2).tolist() == want
