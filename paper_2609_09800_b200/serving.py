@@ -270,7 +270,9 @@ class ServedLayer:
     key/value cache lie in ranges registered with a context, and every step serves the accesses that its operators make.
 
     Row 0 of the cache holds the shared prefix; the requests, rows 1 to batch, are forked from it, so that they share its full pages and
-    begin with a copy of a page that it had begun; each then has room for own_tokens more.  Values are random (seed)."""
+    begin with a copy of a page that it had begun; each then has room for own_tokens more, on pages that ``append`` takes as it comes to them.
+    A page in use is thus always one that some row's length counts, as ``cache`` (a ``CachePages``) has it: requests may be freed through it,
+    begin again as a fork of row 0 or of another request, and the cache may be compacted, in any order.  Values are random (seed)."""
 
     def __init__(self, ctx, batch=64, prefix_tokens=8192, own_tokens=64, page_tokens=16, hidden=2048, inter=768, n_experts=128, top_k=8, q_heads=32,
                  kv_heads=4, head_dim=128, seed=0):
@@ -294,16 +296,11 @@ class ServedLayer:
             self.lens[0] = prefix_tokens
             self.own_len = torch.zeros(batch, dtype=torch.int32, device=dev)
             self._rows = torch.arange(1, batch + 1, device=dev, dtype=torch.int32)
+            self._pages = torch.arange(pages - 1, device=dev)
         self.cache = CachePages(self.kv[:, :-1], self.refs[:-1], self.tables, self.lens, page_tokens, stream=ctx.stream)
         self.cache.fork(torch.zeros_like(self._rows), self._rows)
         self.cache.result()
-        with torch.cuda.stream(ctx.stream):                       # the pages that the requests will grow into, the lowest free ones
-            free = torch.nonzero(self.refs == 0).flatten().to(torch.int32)
-            more = mine - (1 if started else 0)
-            grow = free[:batch * more].view(batch, more)
-            self.tables[1:, full + (1 if started else 0):full + mine] = grow
-            self.refs[grow.flatten().long()] = 1
-            self.base_tokens = full * page_tokens
+        self.prefix_tokens, self.base_tokens = prefix_tokens, full * page_tokens
         self.attention = PrefixAttention(self.kv[0], self.kv[1], batch, q_heads, self.tables[0, :full].contiguous() if full else None, self.base_tokens,
                                          self.tables[1:, full:], self.own_len, mine * page_tokens, stream=ctx.stream)
         self.moe = MoeLayer(self.experts, hidden, inter, top_k, batch, stream=ctx.stream)
@@ -313,17 +310,31 @@ class ServedLayer:
             offset += -(-t.numel() * t.element_size() // (1 << 20)) << 20
 
     def append(self, k, v):
-        """Every request's next token: k, v [batch, kv_heads, head_dim] go into its cache.  A request that has no page for it (its room is used up, or
-        its row was freed) stays as it is.  Returns who took it, bool [batch], on the device."""
+        """Every request's next token: k, v [batch, kv_heads, head_dim] go into its cache; a request whose pages are full takes the lowest free one, in
+        the order of the requests.  A request that has no place for it stays as it is: its room is used up, no page is free, or its row was freed
+        (holds less than the prefix; without a prefix an empty row is a request without tokens).  Returns who took it, bool [batch], on the
+        device."""
         import torch
         with torch.cuda.stream(self.ctx.stream):
-            at = self.lens[1:].long()
-            col, last = at // self.page, self.tables.shape[1] - 1
-            page = self.tables[1:].gather(1, col.clamp(max=last)[:, None])[:, 0].long()
-            took = (page >= 0) & (col <= last)
-            page = torch.where(took, page, self.kv.shape[1] - 1)
-            self.kv[0, page, at % self.page], self.kv[1, page, at % self.page] = k, v
-            self.lens[1:] += took
+            rows, lens, nobody = self.tables[1:], self.lens[1:], self.kv.shape[1] - 1
+            last = self.tables.shape[1] - 1                       # (an entry of -1, past the room)
+            col, at = (lens // self.page).long(), (lens % self.page).long()
+            fits = (lens >= self.prefix_tokens) & (col < last)
+            col.clamp_(min=0, max=last)
+            # the n-th request that begins a page takes the n-th free one
+            begins = fits & (at == 0)
+            free = self.refs[:-1] == 0
+            nth = torch.where(free, free.cumsum(0) - 1, self.batch).clamp_(max=self.batch)
+            lowest = torch.full((self.batch + 1,), -1, dtype=torch.int64, device=nth.device).scatter_(0, nth, self._pages)
+            lowest[self.batch] = -1                               # (where all that are not asked for ended)
+            taken = torch.where(begins, lowest[(begins.cumsum(0) - 1).clamp_(min=0)], -1)
+            page = torch.where(begins, taken, rows.gather(1, col[:, None])[:, 0].long())
+            took = fits & (page >= 0) & (page < nobody)
+            rows.scatter_(1, col[:, None], torch.where(took, page, rows.gather(1, col[:, None])[:, 0].long()).int()[:, None])
+            page = torch.where(took, page, nobody)
+            self.refs.index_add_(0, page, (begins & took).int())
+            self.kv[0, page, at], self.kv[1, page, at] = k, v
+            lens += took
         return took
 
     def step(self, q, x, scores, issue_ns=0, gap_ns=0):

@@ -1,0 +1,129 @@
+"""The cache of an executed layer through forks, frees and compactions: every row holds its own tokens, and every page is held by as many rows as say so."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+from paper_2609_09800_b200 import workloads as wl
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch as t
+    if not t.cuda.is_available():
+        pytest.skip("no CUDA device")
+    from paper_2609_09800_b200 import build
+    build.build()
+    return t
+
+
+@pytest.fixture(scope="module")
+def mods(torch):
+    from paper_2609_09800_b200 import hbf, serving
+    return hbf, serving
+
+
+SMALL = dict(hidden=256, inter=64, n_experts=12, top_k=3, q_heads=16, kv_heads=4, head_dim=64)
+
+
+class Rows:
+    """A layer and, beside it on the host, the tokens that each of its rows should hold: lists of [2, kv_heads, head_dim]."""
+
+    def __init__(self, torch, mods, batch, prefix, own, seed=0, page=16, stream=None):
+        hbf, serving = mods
+        self.torch, self.batch, self.prefix, self.page = torch, batch, prefix, page
+        self.ctx = hbf.Context(wl.load_profile("nominal", **wl.GEOMETRY["serving"]), stream=stream)
+        self.layer = serving.ServedLayer(self.ctx, batch=batch, prefix_tokens=prefix, own_tokens=own, page_tokens=page, seed=seed, **SMALL)
+        self.room = prefix // page * page + -(-(prefix % page + own) // page) * page      # a row's most tokens
+        self.g = torch.Generator(device="cuda"); self.g.manual_seed(seed + 1)
+        first = list(self.gather(0))
+        self.rows = [list(first) for _ in range(batch + 1)]
+
+    def gather(self, row):
+        L = self.layer
+        n = int(L.lens[row])
+        pages = L.tables[row, :-(-n // self.page)].long()
+        return L.kv[:, pages].flatten(1, 2)[:, :n].transpose(0, 1).clone()
+
+    def ints(self, v):
+        return self.torch.tensor(v, dtype=self.torch.int32, device="cuda")
+
+    def append(self):
+        k, v = (self.torch.randn(self.batch, 4, 64, device="cuda", generator=self.g).bfloat16() for _ in range(2))
+        took = self.layer.append(k, v).tolist()
+        for b in range(self.batch):
+            row = self.rows[b + 1]
+            assert took[b] == (self.prefix <= len(row) < self.room), (b, len(row))
+            if took[b]:
+                row.append(self.torch.stack([k[b], v[b]]))
+
+    def free(self, rows):
+        self.layer.cache.free(self.ints(rows)); self.layer.cache.result()
+        for r in rows:
+            self.rows[r] = []
+
+    def fork(self, parents, children):
+        self.layer.cache.fork(self.ints(parents), self.ints(children)); self.layer.cache.result()
+        for p, c in zip(parents, children):
+            self.rows[c] = list(self.rows[p])
+
+    def compact(self):
+        self.layer.cache.compact()
+        return self.layer.cache.result()
+
+    def check(self):
+        L, torch = self.layer, self.torch
+        held = [0] * (L.refs.numel())
+        for r, want in enumerate(self.rows):
+            assert int(L.lens[r]) == len(want)
+            got = self.gather(r)
+            assert len(want) == 0 or torch.equal(got, torch.stack(want)), "row %d" % r
+            for p in L.tables[r, :-(-len(want) // self.page)].tolist():
+                held[p] += 1
+        assert L.refs.tolist() == held
+
+
+@pytest.mark.parametrize("prefix, own", [(40, 60), (48, 70), (7, 40), (0, 50)])
+def test_rows_keep_their_tokens(torch, mods, prefix, own):
+    r = Rows(torch, mods, 3, prefix, own)
+    r.check()
+    for _ in range(5):
+        r.append()
+    r.free([1])
+    r.check()
+    r.compact()
+    r.check()
+    for _ in range(9):                                       # into a page of their own behind the one that they were in
+        r.append()
+    r.check()
+    if prefix:
+        r.fork([0], [1])                                     # takes the lowest free page, which nobody may still write
+        r.check()
+    for _ in range(20):
+        r.append()
+        r.check()
+    r.free([3]); r.compact(); r.fork([2], [3])
+    for _ in range(r.room):
+        r.append()
+    r.check()
+
+
+def test_pages_come_back_however_often_rows_begin_again(torch, mods):
+    r = Rows(torch, mods, 6, 30, 50, seed=4)
+    pick = torch.Generator().manual_seed(2)
+    rnd = lambda n: int(torch.randint(0, n, (1,), generator=pick))
+    for turn in range(12):
+        for _ in range(rnd(30)):
+            r.append()
+        gone = sorted({1 + rnd(6) for _ in range(1 + rnd(4))})
+        r.free(gone)
+        if rnd(2):
+            r.compact()
+            assert r.compact()["moved"] == 0
+        r.check()
+        stay = [0] + [i for i in range(1, 7) if i not in gone]
+        r.fork([stay[rnd(len(stay))] for _ in gone], gone)
+        r.check()
+    for _ in range(r.room):                                  # all the room that there ever was
+        r.append()
+    r.check()
+    assert all(len(t) == r.room for t in r.rows[1:])
