@@ -100,11 +100,10 @@ __device__ __forceinline__ void apply_plan(const PagesDev &p, const int32_t *a, 
         const uint32_t live = (uint32_t)c.n_live;
         for (uint64_t k = first; k < (uint64_t)p.rows * p.cols; k += step) {
             const uint32_t i = (uint32_t)(k / p.cols), j = (uint32_t)(k - (uint64_t)i * p.cols);
-            const int32_t len = p.lens[i];
-            if (len_bad(p, len) || j >= held_pages(p, len)) continue;
+            if (j >= held_pages(p, p.lens[i])) continue;
             int32_t *t = p.tables + (int64_t)i * p.table_stride + j;
             const uint32_t id = (uint32_t)*t;
-            if (id >= live && id < p.n_pages && p.extra[id] >= 0) *t = p.extra[id];
+            if (id >= live) *t = p.extra[id];                // (the plan has seen that it is a page in use: one that moves)
         }
         for (uint64_t k = first; k < moves; k += step) { p.refs[p.dst[k]] = p.refs[p.src[k]]; p.refs[p.src[k]] = 0; }
     }
@@ -282,6 +281,36 @@ k_plan_free(const __grid_constant__ PagesDev p, const int32_t *rows, uint32_t n,
     finish_plan<kDoFree>(p, s_bad ? HBF_E_INVAL : HBF_OK, 0u, 0u, rows, nullptr, n, alone);
 }
 
+// Whether any row of the cache has a length or a counting entry that cannot be.  A warp takes up to 32 rows, an even share of them, and their
+// entries one behind the other (at most 2^29, table_cols being 2^24 at most), an entry a lane, so that the loads of short rows are on their way together.
+__device__ __forceinline__ int rows_bad(const PagesDev &p) {
+    const uint32_t lane = lane_id(), share = min(32u, (p.rows + kPlanThreads / 32u - 1u) / (kPlanThreads / 32u));
+    int bad = 0;
+    for (uint32_t r0 = (threadIdx.x >> 5) * share; r0 < p.rows; r0 += kPlanThreads / 32u * share) {
+        const int32_t len = lane < share && r0 + lane < p.rows ? p.lens[r0 + lane] : 0;
+        const bool sound = !len_bad(p, len);
+        if (!sound) bad = 1;
+        const uint32_t held = sound ? held_pages(p, len) : 0u;
+        uint32_t end = held;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) { const uint32_t u = __shfl_up_sync(0xffffffffu, end, o); if (lane >= (uint32_t)o) end += u; }
+        const uint32_t first = end - held, total = __shfl_sync(0xffffffffu, end, 31);
+#pragma unroll 4
+        for (uint32_t e0 = 0; e0 < total; e0 += 32u) {
+            const uint32_t e = e0 + lane;
+            uint32_t at = 0u;                                // the last row whose entries begin no later than e
+#pragma unroll
+            for (uint32_t o = 16; o > 0u; o >>= 1) if (__shfl_sync(0xffffffffu, first, at + o) <= e) at += o;
+            const uint32_t j = e - __shfl_sync(0xffffffffu, first, at);
+            if (e < total) {
+                const uint32_t id = (uint32_t)p.tables[(int64_t)(r0 + at) * p.table_stride + j];
+                if (id >= p.n_pages || p.refs[id] <= 0) bad = 1;
+            }
+        }
+    }
+    return bad;
+}
+
 // The k-th page in use behind the first n_live moves into the k-th free one among them.
 __global__ void __launch_bounds__(kPlanThreads)
 k_plan_compact(const __grid_constant__ PagesDev p, int alone) {
@@ -289,6 +318,7 @@ k_plan_compact(const __grid_constant__ PagesDev p, int alone) {
     __shared__ uint32_t warps[32];
     pdl_trigger();
     const uint32_t tid = threadIdx.x, lane = lane_id(), words = (p.n_pages + 31u) / 32u;
+    const int bad = rows_bad(p);
     uint32_t mine = 0u;
     for (uint32_t w = tid >> 5; w < words; w += kPlanThreads / 32) {
         const uint32_t i = w * 32u + lane;
@@ -311,7 +341,8 @@ k_plan_compact(const __grid_constant__ PagesDev p, int alone) {
     for (uint32_t i = live + tid; i < p.n_pages; i += kPlanThreads) p.extra[i] = -1;
     __syncthreads();
     for (uint32_t k = tid; k < moves; k += kPlanThreads) p.extra[p.src[k]] = p.dst[k];
-    finish_plan<kDoCompact>(p, HBF_OK, moves, live, nullptr, nullptr, 0u, alone);
+    const int any = __syncthreads_or(bad);
+    finish_plan<kDoCompact>(p, any ? HBF_E_INVAL : HBF_OK, moves, live, nullptr, nullptr, 0u, alone);
 }
 
 // The records of the moves of the call before: for each page and slab a read and a program; the places behind them hold records of one byte
