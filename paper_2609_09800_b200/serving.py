@@ -272,7 +272,8 @@ class ServedLayer:
     Row 0 of the cache holds the shared prefix; the requests, rows 1 to batch, are forked from it, so that they share its full pages and
     begin with a copy of a page that it had begun; each then has room for own_tokens more, on pages that ``append`` takes as it comes to them.
     A page in use is thus always one that some row's length counts, as ``cache`` (a ``CachePages``) has it: requests may be freed through it,
-    begin again as a fork of row 0 or of another request, and the cache may be compacted, in any order.  Values are random (seed)."""
+    begin again as a fork of row 0 or of another request, and the cache may be compacted, in any order.  Values are random (seed).  All of it
+    runs on the context's stream; tensors of another stream are the caller's to order before it."""
 
     def __init__(self, ctx, batch=64, prefix_tokens=8192, own_tokens=64, page_tokens=16, hidden=2048, inter=768, n_experts=128, top_k=8, q_heads=32,
                  kv_heads=4, head_dim=128, seed=0):
@@ -297,8 +298,9 @@ class ServedLayer:
             self.own_len = torch.zeros(batch, dtype=torch.int32, device=dev)
             self._rows = torch.arange(1, batch + 1, device=dev, dtype=torch.int32)
             self._pages = torch.arange(pages - 1, device=dev)
+            parents = torch.zeros_like(self._rows)
         self.cache = CachePages(self.kv[:, :-1], self.refs[:-1], self.tables, self.lens, page_tokens, stream=ctx.stream)
-        self.cache.fork(torch.zeros_like(self._rows), self._rows)
+        self.cache.fork(parents, self._rows)
         self.cache.result()
         self.prefix_tokens, self.base_tokens = prefix_tokens, full * page_tokens
         self.attention = PrefixAttention(self.kv[0], self.kv[1], batch, q_heads, self.tables[0, :full].contiguous() if full else None, self.base_tokens,

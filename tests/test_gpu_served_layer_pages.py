@@ -127,3 +127,17 @@ def test_pages_come_back_however_often_rows_begin_again(torch, mods):
         r.append()
     r.check()
     assert all(len(t) == r.room for t in r.rows[1:])
+
+
+def test_a_layer_on_a_stream_of_its_own(torch, mods):
+    """Everything that a layer is made of is made on its context's stream: work that the current stream still has to do delays none of it."""
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    wrong = [torch.full((20,), 7, dtype=torch.int32, device="cuda") for _ in range(64)]      # what memory of that size may hold
+    torch.cuda.synchronize()
+    del wrong
+    torch.cuda._sleep(200_000_000)                           # some 0.1 s of the current stream
+    r = Rows(torch, mods, 20, 40, 30, stream=stream)
+    torch.cuda.synchronize()
+    r.check()
+    assert r.layer.lens.tolist() == [40] * 21
