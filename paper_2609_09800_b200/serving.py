@@ -43,9 +43,14 @@ class _Operator:
         with self._torch.cuda.stream(self.stream):
             return self._torch.empty(nbytes, dtype=self._torch.uint8, device=self.device)
 
-    def _records(self, n):
-        with self._torch.cuda.stream(self.stream):
-            return self._torch.empty(n, _RECORD_WORDS, dtype=self._torch.int64, device=self.device)
+    def _records(self, n, out):
+        """Room for n records: the caller's, of exactly as many, or new."""
+        if out is None:
+            with self._torch.cuda.stream(self.stream):
+                return self._torch.empty(n, _RECORD_WORDS, dtype=self._torch.int64, device=self.device)
+        _check(out.dtype == self._torch.int64 and out.shape == (n, _RECORD_WORDS) and out.device == self.device and out.is_contiguous(),
+               "out has to be a contiguous int64 tensor of [%d, %d] on %s" % (n, _RECORD_WORDS, self.device))
+        return out
 
     def _raise(self, rc, what):
         if rc != 0:
@@ -118,7 +123,7 @@ class PrefixAttention(_Operator):
     def accesses(self, issue_ns=0, gap_ns=0, out=None):
         """Records of the pages that a call reads, the prefix's once: int64 [n, 3]."""
         n = self.access_count()
-        out = self._records(n) if out is None else out
+        out = self._records(n, out)
         self._raise(self._lib.hbf_attention_accesses(self._ref, issue_ns, gap_ns, out.data_ptr(), n, self._st), "hbf_attention_accesses")
         return out
 
@@ -179,7 +184,7 @@ class MoeLayer(_Operator):
     def accesses(self, issue_ns=0, gap_ns=0, out=None):
         """Records of the experts that the last call read, from its scores as they are now: int64 [n, 3]."""
         n = self.access_count()
-        out = self._records(n) if out is None else out
+        out = self._records(n, out)
         self._raise(self._lib.hbf_moe_accesses(self._ref, self.tile_bytes, issue_ns, gap_ns, out.data_ptr(), n, self._st) if n else 0, "hbf_moe_accesses")
         return out
 
@@ -260,7 +265,7 @@ class CachePages(_Operator):
         """Records of the last call's moves, a read and a program for each page and slab: int64 [n, 3]; n is the most that the call can have
         moved, places past its moves are native."""
         n = self.access_count()
-        out = self._records(n) if out is None else out
+        out = self._records(n, out)
         self._raise(self._lib.hbf_pages_accesses(self._ref, self._ws_ptr, issue_ns, gap_ns, out.data_ptr(), n, self._st) if n else 0, "hbf_pages_accesses")
         return out
 
