@@ -433,8 +433,12 @@ HBF_API int hbf_get_retention_totals(hbf_ctx *ctx, hbf_retention_totals_t *out);
  * on two streams or in two graphs that are replayed at once, need one each.  Every call can be captured into a CUDA graph; a replay reads
  * the tables, lengths and scores anew.  Counts in the structs are fixed at capture.
  * Values are bf16 or fp16, products exact, sums in 32 bits, outputs rounded once.  Kernels that wait on copies or products of their own wait a
- * bounded number of polls; should that run out, what depends on it is NaN. */
+ * bounded number of polls; should that run out, what depends on it is NaN and the kernel ends with nothing on its way. */
 enum { HBF_BF16 = 0, HBF_FP16 = 1 };
+
+/* Test support, off by default: the polls after which a wait of these kernels gives up, for calls from now on (a captured graph keeps its own); 0:
+ * every wait gives up at once; negative: the default, 2^20, some 1.7 s.  Nothing here makes a kernel wait without a bound. */
+HBF_API int hbf_debug_operator_waits(int32_t poll_limit);
 
 /* A paged key/value cache of one layer: the key of slot s of page g, key head h, begins at k + g * page_stride + s * slot_stride +
  * h * head_stride; its head_dim elements lie side by side; values alike.  head_dim 64 or 128; any page_tokens up to 2^20; pointers

@@ -23,6 +23,7 @@ struct AttnDev {
     float *part_o; float2 *part_ml;
     uint32_t pieces;                                         // own_pieces + prefix_pieces of every row; 1: written straight to `out`
     uint32_t behind;                                         // k_attend was launched to overlap k_prefix_tiles
+    uint32_t polls;                                          // of a wait in k_prefix_tiles
 };
 
 // The place of key `i` of a table's sequence; false: its page is none of the cache's.

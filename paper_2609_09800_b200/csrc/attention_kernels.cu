@@ -435,6 +435,7 @@ static AttnDev attention_dev(const hbf_attention_t *a, uint32_t n_sm) {
     p.lse = a->lse; p.scale_log2 = a->scale * 1.4426950408889634f;
     p.prefix_len = a->prefix_len; p.max_own = a->max_own_len; p.own_stride = a->own_pages_stride;
     p.prefix_pages = a->prefix_pages; p.own_pages = a->own_pages; p.own_len = a->own_len;
+    p.polls = g_operator_polls.load(std::memory_order_relaxed);
     attention_pieces(a, n_sm, p);
     return p;
 }
@@ -473,6 +474,11 @@ static cudaError_t launch_attention(AttnDev p, bool bf16, cudaStream_t st) {
 }  // namespace hbf
 
 using namespace hbf;
+
+extern "C" int hbf_debug_operator_waits(int32_t poll_limit) {
+    g_operator_polls.store(poll_limit < 0 ? kBarPolls : (uint32_t)poll_limit, std::memory_order_relaxed);
+    return HBF_OK;
+}
 
 extern "C" size_t hbf_attention_workspace_bytes(const hbf_attention_t *a) {
     uint32_t n_sm = 0;

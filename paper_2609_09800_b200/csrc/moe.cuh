@@ -18,6 +18,7 @@ struct MoeDev {
     float *part; uint32_t groups;                            // moe_tiles.cu: [groups][T][D], the sums of a group's experts
     uint16_t *route_e; float *route_w;                       // and [T][K]: the choice, made by a kernel of its own (0xfffe: the token has none)
     Div32 div_slices, div_k;                                 // I / 8; K
+    uint32_t polls;                                          // of a wait in moe_tiles.cu
 };
 
 // What the choice leaves in shared memory, the same in every block that makes it.  An entry is an expert in use with up to `chunk` of its

@@ -309,6 +309,7 @@ static MoeDev moe_dev(const hbf_moe_t *m) {
     d.experts = static_cast<const uint16_t *>(m->experts); d.expert_stride = m->expert_stride;
     d.out = static_cast<uint16_t *>(m->out); d.out_stride = m->out_stride;
     d.chosen = m->chosen; d.weights = m->weights; d.div_k = make_div32(d.K);
+    d.polls = g_operator_polls.load(std::memory_order_relaxed);
     return d;
 }
 

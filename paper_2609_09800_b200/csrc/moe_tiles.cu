@@ -20,8 +20,8 @@ constexpr uint32_t kUpStageBytes = kMtA + kMtB, kDownStageBytes = kMtA + 2u * kM
 
 struct MtShared {
     Route<kMtTokens> route;
-    uint64_t full[kUpStages], empty[kUpStages], acc_full[2], acc_empty[2];
-    uint32_t tmem;
+    uint64_t full[kUpStages], empty[kUpStages], acc_full[2], acc_empty[2], products_done;
+    uint32_t tmem, gave_up, copied;                          // copied: stages whose weights were asked for
 };
 constexpr uint32_t kUpTilesSmem = 1024u + kUpStages * kUpStageBytes + 2u * kMtChunk * 64u * 4u + sizeof(MtShared);
 constexpr uint32_t down_tiles_smem(uint32_t tokens) { return 1024u + kDownStages * kDownStageBytes + tokens * 512u + sizeof(MtShared); }
@@ -39,6 +39,8 @@ __device__ __forceinline__ void begin_tiles(const MoeDev &m, MtShared &sh, unsig
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) { bar_init(smem_addr(&sh.full[i]), 129u); bar_init(smem_addr(&sh.empty[i]), 1u); }
         for (int i = 0; i < 2; ++i) { bar_init(smem_addr(&sh.acc_full[i]), 1u); bar_init(smem_addr(&sh.acc_empty[i]), 128u); }
+        bar_init(smem_addr(&sh.products_done), 1u);
+        sh.gave_up = sh.copied = 0u;
         bar_init_done();
     }
     if ((threadIdx.x >> 5) == 9u) { tensor_alloc(smem_addr(&sh.tmem), 128u); tensor_fence_before(); }
@@ -47,32 +49,51 @@ __device__ __forceinline__ void begin_tiles(const MoeDev &m, MtShared &sh, unsig
     __syncthreads();
     tensor_fence_after();
 }
-__device__ __forceinline__ void end_tiles(const MtShared &sh) {
+// Where a wait was given up, weights may be on their way: the stages that were asked for get the arrivals of the activations' threads that did not come
+// to them (a stage is asked for only when the one a round before it was used), so that their barriers end when the copies have.  told: stages
+// that this thread, of warps 4 to 7, said were there.
+template <int kStages>
+__device__ __forceinline__ void end_tiles(MtShared &sh, bool live, uint32_t told) {
+    const uint32_t warp = threadIdx.x >> 5;
     tensor_fence_before();
-    __syncthreads();
-    if ((threadIdx.x >> 5) == 9u) { __syncwarp(); tensor_fence_after(); tensor_free(sh.tmem, 128u); }
+    if (__syncthreads_or(live ? 0 : 1)) {
+        const uint32_t copied = *(volatile uint32_t *)&sh.copied;
+        if (warp >= 4u && warp < 8u) for (uint32_t n = told; n < copied; ++n) bar_arrive(smem_addr(&sh.full[n % kStages]));
+        if (warp == 8u) for (uint32_t n = copied > (uint32_t)kStages ? copied - kStages : 0u; n < copied; ++n) wait_for_own(smem_addr(&sh.full[n % kStages]), (n / kStages) & 1u);
+    }
+    if (warp == 9u) { __syncwarp(); tensor_fence_after(); tensor_free(sh.tmem, 128u); }
+}
+// Nothing of the block is on its way when it gives its tensor memory back.
+__device__ __forceinline__ void end_products(MtShared &sh) {
+    products_arrive(smem_addr(&sh.products_done));
+    wait_for_own(smem_addr(&sh.products_done), 0u);
 }
 
 // The activations' side of a ring: stage g's copies are issued by `copy(stage address)`; they are said to be there kMtLag stages later, and before
-// a wait for a free stage.
+// a wait for a free stage.  stage: false when a wait was given up.
 template <int kStages, uint32_t kBytes>
 struct Gather {
-    uint32_t ring, full, empty, g = 0u;
-    bool live = true;
-    __device__ __forceinline__ void tell(uint32_t n) {
+    uint32_t ring, full, empty, polls;
+    uint32_t gave_up;
+    bool live;
+    uint32_t g = 0u, told = 0u;
+    __device__ __forceinline__ void tell() {
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        bar_arrive(full + (n % kStages) * 8u);
+        bar_arrive(full + (told % kStages) * 8u);
+        ++told;
     }
-    template <class F> __device__ __forceinline__ void stage(F copy) {
-        if (g >= (uint32_t)kMtLag) { copy_wait<kMtLag - 1>(); tell(g - kMtLag); }
-        live = bar_wait(empty + (g % kStages) * 8u, ((g / kStages) & 1u) ^ 1u, live);
+    template <class F> __device__ __forceinline__ bool stage(F copy) {
+        if (g >= (uint32_t)kMtLag) { copy_wait<kMtLag - 1>(); tell(); }
+        live = bar_wait(empty + (g % kStages) * 8u, ((g / kStages) & 1u) ^ 1u, live, polls, gave_up);
+        if (!live) return false;
         copy(ring + (g % kStages) * kBytes + kMtA);
         copy_commit();
         ++g;
+        return true;
     }
     __device__ __forceinline__ void finish() {
         copy_wait<0>();
-        for (uint32_t n = g > (uint32_t)kMtLag ? g - kMtLag : 0u; n < g; ++n) tell(n);
+        while (live && told < g) tell();
     }
 };
 
@@ -107,51 +128,55 @@ k_moe_up_tiles(const __grid_constant__ MoeDev m, const __grid_constant__ UpMaps 
     }
     const uint32_t tiles = (m.I + rows - 1u) / rows, n_items = r.n_entries * tiles, chunks = (m.D + 63u) / 64u;
     const uint32_t full = smem_addr(sh.full), empty = smem_addr(sh.empty), acc_full = smem_addr(sh.acc_full), acc_empty = smem_addr(sh.acc_empty);
-    bool live = true;
+    bool live = m.polls != 0u;
+    uint32_t told = 0u;
+    auto wait = [&](uint32_t bar, uint32_t parity) { live = bar_wait(bar, parity, live, m.polls, smem_addr(&sh.gave_up)); };
     if (warp == 8u) {
         if (lane == 0u) {
             uint32_t g = 0u;
             const CUtensorMap *map = &maps.rows[(64u - rows) / 16u];
-            for (uint32_t item = blockIdx.x; item < n_items; item += gridDim.x) {
+            for (uint32_t item = blockIdx.x; item < n_items && live; item += gridDim.x) {
                 const uint32_t en = item / tiles, i0 = (item - en * tiles) * rows, e = r.expert[en];
                 for (uint32_t c = 0; c < chunks; ++c, ++g) {
                     const uint32_t s = g % kUpStages, at = ring + s * kUpStageBytes, bar = full + s * 8u;
-                    live = bar_wait(empty + s * 8u, ((g / kUpStages) & 1u) ^ 1u, live);
-                    bar_arrive_bytes(bar, live ? rows * 256u : 0u);
-                    if (live) {
-                        tensor_copy3(at, map, (int32_t)(c * 64u), (int32_t)i0, (int32_t)e, bar);
-                        tensor_copy3(at + 8192u, map, (int32_t)(c * 64u), (int32_t)(m.I + i0), (int32_t)e, bar);
-                    }
+                    wait(empty + s * 8u, ((g / kUpStages) & 1u) ^ 1u);
+                    if (!live) break;
+                    bar_arrive_bytes(bar, rows * 256u);
+                    tensor_copy3(at, map, (int32_t)(c * 64u), (int32_t)i0, (int32_t)e, bar);
+                    tensor_copy3(at + 8192u, map, (int32_t)(c * 64u), (int32_t)(m.I + i0), (int32_t)e, bar);
                 }
             }
+            sh.copied = g;
         }
     } else if (warp >= 4u && warp < 8u) {
         const uint32_t t = tid - 128u, col = t & 7u, row = t >> 3, to = row * 128u + ((col ^ (row & 7u)) * 16u);
-        Gather<kUpStages, kUpStageBytes> in{ring, full, empty};
-        for (uint32_t item = blockIdx.x; item < n_items; item += gridDim.x) {
+        Gather<kUpStages, kUpStageBytes> in{ring, full, empty, m.polls, smem_addr(&sh.gave_up), live};
+        for (uint32_t item = blockIdx.x; item < n_items && in.live; item += gridDim.x) {
             const uint32_t en = item / tiles, n = r.count[en], pair0 = r.pair0[en];
             const uint16_t *x0 = row < n ? m.x + (int64_t)r.token[pair0 + row] * m.x_stride : nullptr;
             const uint16_t *x1 = row + 16u < n ? m.x + (int64_t)r.token[pair0 + row + 16u] * m.x_stride : nullptr;
             for (uint32_t c = 0; c < chunks; ++c)
-                in.stage([&](uint32_t at) {
+                if (!in.stage([&](uint32_t at) {
                     const uint32_t k = c * 64u + col * 8u;
                     const bool is = k < m.D;
                     if (x0) copy_async16_shared(at + to, is ? x0 + k : m.x, is);
                     if (x1) copy_async16_shared(at + 2048u + to, is ? x1 + k : m.x, is);
-                });
+                })) break;
         }
         in.finish();
+        live = in.live; told = in.told;
     } else if (warp == 9u) {
         if (lane == 0u) {
             uint32_t g = 0u, it = 0u;
             const TileDesc a0(ring, 16u, 1024u), b0(ring + kMtA, 16u, 1024u);
-            for (uint32_t item = blockIdx.x; item < n_items; item += gridDim.x, ++it) {
+            for (uint32_t item = blockIdx.x; item < n_items && live; item += gridDim.x, ++it) {
                 const uint32_t n = r.count[item / tiles], buf = it & 1u, id = product_desc(kBf16, false, 128u, n <= 16u ? 16u : 32u);
-                live = bar_wait(acc_empty + buf * 8u, ((it >> 1) & 1u) ^ 1u, live);
+                wait(acc_empty + buf * 8u, ((it >> 1) & 1u) ^ 1u);
                 tensor_fence_after();
                 for (uint32_t c = 0; c < chunks; ++c, ++g) {
                     const uint32_t s = g % kUpStages;
-                    live = bar_wait(full + s * 8u, (g / kUpStages) & 1u, live);
+                    wait(full + s * 8u, (g / kUpStages) & 1u);
+                    if (!live) break;
                     tensor_fence_after();
                     TileDesc a = a0, b = b0;
                     a.lo += s * (kUpStageBytes >> 4); b.lo += s * (kUpStageBytes >> 4);
@@ -159,17 +184,19 @@ k_moe_up_tiles(const __grid_constant__ MoeDev m, const __grid_constant__ UpMaps 
                     for (uint32_t k = 0; k < 4u; ++k) product_ss(sh.tmem + buf * 32u, a.at(k * 32u), b.at(k * 32u), id, c || k ? 1u : 0u);
                     products_arrive(empty + s * 8u);
                 }
-                products_arrive(acc_full + buf * 8u);
+                if (live) products_arrive(acc_full + buf * 8u);
             }
+            end_products(sh);
         }
         __syncwarp();
     } else if (warp < 4u) {
         uint32_t it = 0u;
         for (uint32_t item = blockIdx.x; item < n_items; item += gridDim.x, ++it) {
             const uint32_t en = item / tiles, i0 = (item - en * tiles) * rows, n = r.count[en], pair0 = r.pair0[en], buf = it & 1u;
-            live = bar_wait(acc_full + buf * 8u, (it >> 1) & 1u, live);
+            wait(acc_full + buf * 8u, (it >> 1) & 1u);
             __syncwarp();
             tensor_fence_after();
+            const bool sound = live && !ld_flag(smem_addr(&sh.gave_up));
             uint32_t v[32];
             tensor_load(sh.tmem + buf * 32u + ((warp * 32u) << 16), v);   // (columns past the tokens hold anything)
             tensor_loaded(v);
@@ -187,7 +214,7 @@ k_moe_up_tiles(const __grid_constant__ MoeDev m, const __grid_constant__ UpMaps 
                 for (int c = 0; c < kMtChunk; ++c)
                     if ((uint32_t)c < n) {
                         const float g = __uint_as_float(v[c]), u = up[c * 64 + row];
-                        const float h = live ? r.weight[pair0 + c] * (g / (1.0f + expf(-g)) * u) : __int_as_float(0x7fc00000);
+                        const float h = sound ? r.weight[pair0 + c] * (g / (1.0f + expf(-g)) * u) : __int_as_float(0x7fc00000);
                         // (held as the sum of two numbers: see k_moe_up)
                         const typename Ty::type hi = Ty::from(h), lo = Ty::from(isfinite(h) ? h - Ty::to(hi) : 0.0f);
                         const size_t at = (size_t)(pair0 + c) * m.I + i0 + row;
@@ -197,7 +224,7 @@ k_moe_up_tiles(const __grid_constant__ MoeDev m, const __grid_constant__ UpMaps 
             }
         }
     }
-    end_tiles(sh);
+    end_tiles<kUpStages>(sh, live, told);
 }
 
 template <class Ty, bool kBf16>
@@ -215,49 +242,55 @@ k_moe_down_tiles(const __grid_constant__ MoeDev m, const __grid_constant__ CUten
     const uint32_t d_tiles = (m.D + 127u) / 128u, group = blockIdx.x / d_tiles, d0 = (blockIdx.x - group * d_tiles) * 128u, chunks = (m.I + 63u) / 64u;
     const uint32_t en0 = r.n_entries * group / m.groups, en1 = r.n_entries * (group + 1u) / m.groups;
     const uint32_t full = smem_addr(sh.full), empty = smem_addr(sh.empty), acc_full = smem_addr(sh.acc_full), acc_empty = smem_addr(sh.acc_empty);
-    bool live = true;
+    bool live = m.polls != 0u;
+    uint32_t told = 0u;
+    auto wait = [&](uint32_t bar, uint32_t parity) { live = bar_wait(bar, parity, live, m.polls, smem_addr(&sh.gave_up)); };
     if (warp == 8u) {                                        // weights: as far ahead as the ring goes while the kernel before still runs
         if (lane == 0u) {
             uint32_t g = 0u;
-            for (uint32_t en = en0; en < en1; ++en)
+            for (uint32_t en = en0; en < en1 && live; ++en)
                 for (uint32_t c = 0; c < chunks; ++c, ++g) {
                     const uint32_t s = g % kDownStages, bar = full + s * 8u;
-                    live = bar_wait(empty + s * 8u, ((g / kDownStages) & 1u) ^ 1u, live);
-                    bar_arrive_bytes(bar, live ? kMtA : 0u);
-                    if (live) tensor_copy3(ring + s * kDownStageBytes, &w_map, (int32_t)(c * 64u), (int32_t)d0, (int32_t)r.expert[en], bar);
+                    wait(empty + s * 8u, ((g / kDownStages) & 1u) ^ 1u);
+                    if (!live) break;
+                    bar_arrive_bytes(bar, kMtA);
+                    tensor_copy3(ring + s * kDownStageBytes, &w_map, (int32_t)(c * 64u), (int32_t)d0, (int32_t)r.expert[en], bar);
                 }
+            sh.copied = g;
         }
     } else if (warp >= 4u && warp < 8u) {
         const uint32_t t = tid - 128u, col = t & 7u, row = t >> 3, to = row * 128u + ((col ^ (row & 7u)) * 16u);
-        Gather<kDownStages, kDownStageBytes> in{ring, full, empty};
+        Gather<kDownStages, kDownStageBytes> in{ring, full, empty, m.polls, smem_addr(&sh.gave_up), live};
         pdl_wait();
-        for (uint32_t en = en0; en < en1; ++en) {
+        for (uint32_t en = en0; en < en1 && in.live; ++en) {
             const uint32_t n = r.count[en], pair0 = r.pair0[en];
             const size_t h0 = (size_t)(pair0 + row) * m.I, h1 = (size_t)(pair0 + row + 16u) * m.I;
             const bool is0 = row < n, is1 = row + 16u < n;
             const uint32_t second = n <= 16u ? 2048u : kMtB; // rows 16 or 32 and on: the second numbers
             for (uint32_t c = 0; c < chunks; ++c)
-                in.stage([&](uint32_t at) {
+                if (!in.stage([&](uint32_t at) {
                     const uint32_t k = c * 64u + col * 8u;
                     const bool is = k < m.I;
                     const size_t a = is ? h0 + k : 0u, b = is ? h1 + k : 0u;
                     if (is0) { copy_async16(at + to, m.h_hi + a, is); copy_async16(at + second + to, m.h_lo + a, is); }
                     if (is1) { copy_async16(at + 2048u + to, m.h_hi + b, is); copy_async16(at + second + 2048u + to, m.h_lo + b, is); }
-                });
+                })) break;
         }
         in.finish();
+        live = in.live; told = in.told;
     } else if (warp == 9u) {
         if (lane == 0u) {
             uint32_t g = 0u, it = 0u;
             const TileDesc a0(ring, 16u, 1024u), b0(ring + kMtA, 16u, 1024u);
-            for (uint32_t en = en0; en < en1; ++en, ++it) {
+            for (uint32_t en = en0; en < en1 && live; ++en, ++it) {
                 // first and second numbers are columns of one product (a product of 128 rows takes 60 cycles up to 64 columns)
                 const uint32_t buf = it & 1u, id = product_desc(kBf16, false, 128u, r.count[en] <= 16u ? 32u : 64u);
-                live = bar_wait(acc_empty + buf * 8u, ((it >> 1) & 1u) ^ 1u, live);
+                wait(acc_empty + buf * 8u, ((it >> 1) & 1u) ^ 1u);
                 tensor_fence_after();
                 for (uint32_t c = 0; c < chunks; ++c, ++g) {
                     const uint32_t s = g % kDownStages;
-                    live = bar_wait(full + s * 8u, (g / kDownStages) & 1u, live);
+                    wait(full + s * 8u, (g / kDownStages) & 1u);
+                    if (!live) break;
                     tensor_fence_after();
                     TileDesc a = a0, b = b0;
                     a.lo += s * (kDownStageBytes >> 4); b.lo += s * (kDownStageBytes >> 4);
@@ -265,8 +298,9 @@ k_moe_down_tiles(const __grid_constant__ MoeDev m, const __grid_constant__ CUten
                     for (uint32_t k = 0; k < 4u; ++k) product_ss(sh.tmem + buf * 64u, a.at(k * 32u), b.at(k * 32u), id, c || k ? 1u : 0u);
                     products_arrive(empty + s * 8u);
                 }
-                products_arrive(acc_full + buf * 8u);
+                if (live) products_arrive(acc_full + buf * 8u);
             }
+            end_products(sh);
         }
         __syncwarp();
     } else if (warp < 4u) {
@@ -275,7 +309,7 @@ k_moe_down_tiles(const __grid_constant__ MoeDev m, const __grid_constant__ CUten
         uint32_t it = 0u;
         for (uint32_t en = en0; en < en1; ++en, ++it) {
             const uint32_t n = r.count[en], pair0 = r.pair0[en], buf = it & 1u;
-            live = bar_wait(acc_full + buf * 8u, (it >> 1) & 1u, live);
+            wait(acc_full + buf * 8u, (it >> 1) & 1u);
             __syncwarp();
             tensor_fence_after();
             const uint32_t from = sh.tmem + buf * 64u + ((warp * 32u) << 16);
@@ -289,13 +323,14 @@ k_moe_down_tiles(const __grid_constant__ MoeDev m, const __grid_constant__ CUten
             tensor_fence_before();
             bar_arrive(acc_empty + buf * 8u);
         }
+        const bool sound = live && !ld_flag(smem_addr(&sh.gave_up));
         if (d0 + row < m.D)
             for (uint32_t t = 0; t < m.T; ++t) {
-                const bool bad = !live || (r.bad[t >> 5] >> (t & 31u)) & 1u;
+                const bool bad = !sound || (r.bad[t >> 5] >> (t & 31u)) & 1u;
                 m.part[((size_t)group * m.T + t) * m.D + d0 + row] = bad ? __int_as_float(0x7fc00000) : sums[t * 128u + row];
             }
     }
-    end_tiles(sh);
+    end_tiles<kDownStages>(sh, live, told);
 }
 
 template <class Ty>

@@ -18,10 +18,10 @@ constexpr float kPfGrow = 8.0f;                              // sums are scaled 
 
 // What lies in shared memory behind the tiles.
 struct PfShared {
-    uint64_t kv_full[kPfSlots], kv_empty[kPfSlots], q_full, s_full[2], p_full[2], o_full[2];
+    uint64_t kv_full[kPfSlots], kv_empty[kPfSlots], q_full, s_full[2], p_full[2], o_full[2], products_done;
     int64_t place[2][kPfTile];                               // offset of each key of a tile; -1: none
     float other[2][2][kPfTile];                              // what the two threads of a row tell each other
-    uint32_t tmem, bad;
+    uint32_t tmem, bad, gave_up, most_copied;
 };
 template <int D> constexpr uint32_t kPfTileBytes = kPfTile * D * 2;
 template <int D> constexpr uint32_t pf_smem() { return (2u + kPfSlots) * kPfTileBytes<D> + sizeof(PfShared) + 1024u; }
@@ -65,7 +65,9 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
         for (int i = 0; i < kPfSlots; ++i) { bar_init(smem_addr(&sh.kv_full[i]), 128u); bar_init(smem_addr(&sh.kv_empty[i]), 1u); }
         bar_init(smem_addr(&sh.q_full), 128u);
         for (int t = 0; t < 2; ++t) { bar_init(smem_addr(&sh.s_full[t]), 1u); bar_init(smem_addr(&sh.p_full[t]), 256u); bar_init(smem_addr(&sh.o_full[t]), 1u); }
-        sh.bad = 0u;
+        bar_init(smem_addr(&sh.products_done), 1u);
+        sh.bad = sh.most_copied = 0u;
+        sh.gave_up = p.polls == 0u ? 1u : 0u;
         bar_init_done();
     }
     if (warp == 20u) {
@@ -75,11 +77,16 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
     __syncthreads();
     tensor_fence_after();
     const uint32_t tmem = sh.tmem;                           // S (and P) of both tiles, then O of both
-    bool live = true;
+    bool live = true;                                        // (without polls: set below, where it costs nothing; the rows' threads see gave_up)
+    auto wait = [&](uint32_t bar, uint32_t parity) { live = bar_wait(bar, parity, live, p.polls, smem_addr(&sh.gave_up)); };
+    // boxes of `box` slots (0: none): whole tiles; the stages of keys or values that this thread's warp has asked for (copies' warps)
+    const uint32_t whole = box ? (end - begin) / kPfTile : 0u;
+    uint32_t copied = 0u;
 
     // the registers that the block was launched with, 80 a thread, as 96 for the weights, 56 for the copies, 40 for the products
     if (warp >= 16u && warp < 20u) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        live = p.polls != 0u;
         // ---- keys and values: eight lanes a row of 128 bytes
         const uint32_t t = tid - (uint32_t)kPfRowThreads, w4 = warp - 16u, col = t & 7u, row = t >> 3;
         auto swizzled = [&](uint32_t r) { return r * 128u + ((col ^ (r & 7u)) * 16u); };
@@ -94,8 +101,8 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
             sh.place[i & 1u][t] = at;
         };
         auto arrive = [&](uint32_t bar) { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); bar_arrive(bar); };
-        // boxes of `box` slots (0: none): whole tiles; warp w takes the boxes w, w + 4, ...
-        const uint32_t whole = box ? (end - begin) / kPfTile : 0u, boxes = box ? kPfTile / box : 0u, my_boxes = boxes > w4 ? (boxes - w4 + 3u) / 4u : 0u;
+        // warp w takes the boxes w, w + 4, ...
+        const uint32_t boxes = box ? kPfTile / box : 0u, my_boxes = boxes > w4 ? (boxes - w4 + 3u) / 4u : 0u;
         int32_t page = 0;                                    // lane l: that of this warp's box l
         uint32_t slot0 = 0u;
         auto look = [&](uint32_t i) {
@@ -116,7 +123,7 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
             }
         copy_commit();
         if (whole) {
-            for (uint32_t i = 0; i < whole; ++i) {
+            for (uint32_t i = 0; i < whole && live; ++i) {
                 if (lane < my_boxes && (uint32_t)page >= p.n_pages) { sh.bad = 1u; page = -1; }        // (such a box is zeros)
                 const int32_t page_now = page;
                 const uint32_t slot_now = slot0;
@@ -124,14 +131,16 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
 #pragma unroll 1
                 for (uint32_t kv = 0; kv < 2u; ++kv) {
                     const uint32_t n = 2u * i + kv, slot = n % kPfSlots, full = smem_addr(&sh.kv_full[slot]);
-                    live = bar_wait(smem_addr(&sh.kv_empty[slot]), ((n / kPfSlots) & 1u) ^ 1u, live);
-                    __syncwarp();
-                    if (lane == 0u) bar_arrive_bytes(full, live ? my_boxes * box * D * 2u : 0u);
+                    wait(smem_addr(&sh.kv_empty[slot]), ((n / kPfSlots) & 1u) ^ 1u);
+                    live = __all_sync(0xffffffffu, live);
+                    if (!live) break;
+                    if (lane == 0u) bar_arrive_bytes(full, my_boxes * box * D * 2u);
                     else bar_arrive(full);
+                    copied = n + 1u;
                     for (uint32_t j = 0; j < my_boxes; ++j) {
                         const int32_t pg = __shfl_sync(0xffffffffu, page_now, j);
                         const int32_t sl = (int32_t)__shfl_sync(0xffffffffu, slot_now, j);
-                        if (lane == 0u && live) {
+                        if (lane == 0u) {
                             const uint32_t dst = kv_at + slot * kBytes + (w4 + j * 4u) * box * 128u;
 #pragma unroll
                             for (int x = 0; x < D / 64; ++x) tensor_copy(dst + x * 16384u, kv ? &v_map : &k_map, x * 64, sl, (int32_t)head, pg, full);
@@ -149,9 +158,11 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
                 for (uint32_t kv = 0; kv < 2u; ++kv) {
                     const uint32_t n = 2u * i + kv, slot = n % kPfSlots, first = 2u * whole;
                     // what has come is said to be there before the wait for a free slot, which needs it to be used
-                    if (n == 1u) { copy_wait<1>(); arrive(smem_addr(&sh.q_full)); }
-                    if (n >= first + 2u) { copy_wait<1>(); arrive(smem_addr(&sh.kv_full[(n - 2u) % kPfSlots])); }
-                    live = bar_wait(smem_addr(&sh.kv_empty[slot]), ((n / kPfSlots) & 1u) ^ 1u, live);
+                    if (n == 1u && live) { copy_wait<1>(); arrive(smem_addr(&sh.q_full)); }
+                    if (n >= first + 2u && live) { copy_wait<1>(); arrive(smem_addr(&sh.kv_full[(n - 2u) % kPfSlots])); }
+                    wait(smem_addr(&sh.kv_empty[slot]), ((n / kPfSlots) & 1u) ^ 1u);
+                    if (!live) continue;                     // (to the barriers that the four warps meet at)
+                    copied = n + 1u;
                     const uint32_t dst = kv_at + slot * kBytes;
                     const uint16_t *src = (kv ? p.v : p.k) + (int64_t)head * p.head_stride + col * 8u;
 #pragma unroll
@@ -165,13 +176,15 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
                 }
                 barrier_of(1, 128);                          // the next tile's places are there, this one's are done with
             }
-            copy_wait<1>(); arrive(smem_addr(&sh.kv_full[(2u * n_tiles - 2u) % kPfSlots]));
-            copy_wait<0>(); arrive(smem_addr(&sh.kv_full[(2u * n_tiles - 1u) % kPfSlots]));
+            copy_wait<1>(); if (live) arrive(smem_addr(&sh.kv_full[(2u * n_tiles - 2u) % kPfSlots]));
+            copy_wait<0>(); if (live) arrive(smem_addr(&sh.kv_full[(2u * n_tiles - 1u) % kPfSlots]));
         }
+        copy_wait<0>();
     } else if (warp >= 20u) {
         // ---- the products
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
         if (warp == 20u && lane == 0u) {
+            live = p.polls != 0u;
             const uint32_t id_s = product_desc(kBf16, false, 128u, 128u), id_o = product_desc(kBf16, true, 128u, D);
             const uint32_t tiles = two ? 2u : 1u;
             const uint32_t s_full = smem_addr(sh.s_full), o_full = smem_addr(sh.o_full);
@@ -193,26 +206,32 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
                 for (int k = 0; k < kPfTile / 16; ++k) product_ts(d, a + k * 8u, v.at(k * 2048u), id_o, k ? 1u : add);
                 products_arrive(o_full + t * 8u);
             };
-            live = bar_wait(smem_addr(&sh.q_full), 0u, live);
-            live = bar_wait(smem_addr(&sh.kv_full[0]), 0u, live);
-            tensor_fence_after();
-            for (uint32_t t = 0; t < tiles; ++t) scores(t, 0u);
-            products_arrive(smem_addr(&sh.kv_empty[0]));
-            for (uint32_t i = 0; i < n_tiles; ++i) {
+            wait(smem_addr(&sh.q_full), 0u);
+            wait(smem_addr(&sh.kv_full[0]), 0u);
+            if (live) {
+                tensor_fence_after();
+                for (uint32_t t = 0; t < tiles; ++t) scores(t, 0u);
+                products_arrive(smem_addr(&sh.kv_empty[0]));
+            }
+            for (uint32_t i = 0; i < n_tiles && live; ++i) {
                 const uint32_t nv = 2u * i + 1u, sv = nv % kPfSlots, nk = 2u * i + 2u, sk = nk % kPfSlots;
                 const bool more = i + 1u < n_tiles;
-                live = bar_wait(smem_addr(&sh.kv_full[sv]), (nv / kPfSlots) & 1u, live);
-                if (more) live = bar_wait(smem_addr(&sh.kv_full[sk]), (nk / kPfSlots) & 1u, live);
+                wait(smem_addr(&sh.kv_full[sv]), (nv / kPfSlots) & 1u);
+                if (more) wait(smem_addr(&sh.kv_full[sk]), (nk / kPfSlots) & 1u);
                 for (uint32_t t = 0; t < tiles; ++t) {
-                    live = bar_wait(smem_addr(&sh.p_full[t]), i & 1u, live);
+                    wait(smem_addr(&sh.p_full[t]), i & 1u);
+                    if (!live) break;
                     tensor_fence_after();
                     values(t, sv, i ? 1u : 0u);
                     if (more) scores(t, sk);
                 }
+                if (!live) break;
                 products_arrive(smem_addr(&sh.kv_empty[sv]));
                 if (more) products_arrive(smem_addr(&sh.kv_empty[sk]));
             }
-            if (!live) sh.bad = 1u;
+            // nothing of this block is on its way when it gives its memory back
+            products_arrive(smem_addr(&sh.products_done));
+            wait_for_own(smem_addr(&sh.products_done), 0u);
         }
         __syncwarp();
     } else {
@@ -226,7 +245,7 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
             const uint64_t scales = two_of(scale, scale);
             float m = -INFINITY, l = 0.0f;
             for (uint32_t i = 0; i < n_tiles; ++i) {
-                live = bar_wait(smem_addr(&sh.s_full[t]), i & 1u, live);
+                wait(smem_addr(&sh.s_full[t]), i & 1u);
                 __syncwarp();
                 tensor_fence_after();
                 const uint32_t left = min((uint32_t)kPfTile, end - begin - i * kPfTile), valid = left > half * kHalf ? min(left - half * kHalf, (uint32_t)kHalf) : 0u;
@@ -269,7 +288,7 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
                 const bool grow = m != -INFINITY && best > m + kPfGrow;
                 if (__any_sync(0xffffffffu, grow)) {         // the sums so far, scaled to the new maximum: when the products before are done
                     const float f = grow ? exp2_fast(m - best) : 1.0f;
-                    live = bar_wait(smem_addr(&sh.o_full[t]), (i - 1u) & 1u, live);
+                    wait(smem_addr(&sh.o_full[t]), (i - 1u) & 1u);
                     __syncwarp();
                     tensor_fence_after();
 #pragma unroll 1
@@ -308,10 +327,10 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
                 tensor_fence_before();
                 bar_arrive(smem_addr(&sh.p_full[t]));
             }
-            live = bar_wait(smem_addr(&sh.o_full[t]), (n_tiles - 1u) & 1u, live);
+            wait(smem_addr(&sh.o_full[t]), (n_tiles - 1u) & 1u);
             __syncwarp();
             tensor_fence_after();
-            if (!live || *(volatile uint32_t *)&sh.bad) l = __int_as_float(0x7fc00000);
+            if (!live || (*(volatile uint32_t *)&sh.bad | *(volatile uint32_t *)&sh.gave_up)) l = __int_as_float(0x7fc00000);
             barrier_of(2u + t, 256u);
             sh.other[t][half][r] = l;
             barrier_of(2u + t, 256u);
@@ -372,7 +391,15 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
             tensor_fence_before();
         }
     }
-    __syncthreads();
+    if (__syncthreads_or(live ? 0 : 1) && warp >= 16u && warp < 20u) {
+        // A wait was given up: tensor copies may be on their way.  A stage that some warps of the four have asked for gets the others' arrivals (none is
+        // two rounds of the ring ahead of another), so that its barrier ends when the copies have; stages that were used before need no wait.
+        atomicMax(&sh.most_copied, copied);
+        barrier_of(1, 128);
+        const uint32_t most = *(volatile uint32_t *)&sh.most_copied, by_box = min(most, 2u * whole);
+        for (uint32_t n = copied; n < by_box; ++n) bar_arrive(smem_addr(&sh.kv_full[n % kPfSlots]));
+        for (uint32_t n = most > kPfSlots ? most - kPfSlots : 0u; n < by_box; ++n) wait_for_own(smem_addr(&sh.kv_full[n % kPfSlots]), (n / kPfSlots) & 1u);
+    }
     __syncwarp();
     if (warp == 20u) {
         tensor_fence_after();

@@ -36,7 +36,7 @@ EXPORTS = ("hbf_create", "hbf_destroy", "hbf_register_range", "hbf_clear_ranges"
            "hbf_attach_rom", "hbf_get_rom_temps",
            "hbf_enable_retention", "hbf_retention_advance", "hbf_retention_decay", "hbf_get_retention_blocks",
            "hbf_get_retention_plan", "hbf_get_retention_totals",
-           "hbf_attention_workspace_bytes", "hbf_prefix_attention", "hbf_attention_access_count", "hbf_attention_accesses",
+           "hbf_debug_operator_waits", "hbf_attention_workspace_bytes", "hbf_prefix_attention", "hbf_attention_access_count", "hbf_attention_accesses",
            "hbf_moe_workspace_bytes", "hbf_moe_layer", "hbf_moe_access_count", "hbf_moe_accesses",
            "hbf_pages_workspace_bytes", "hbf_pages_copy", "hbf_pages_fork", "hbf_pages_free", "hbf_pages_compact", "hbf_pages_accesses")
 BF16, FP16 = 0, 1
@@ -182,6 +182,7 @@ def lib():
         for name in ("attention", "moe", "pages"):
             f = getattr(L, "hbf_%s_workspace_bytes" % name)
             f.argtypes, f.restype = [vp], sz
+        L.hbf_debug_operator_waits.argtypes = [C.c_int32]
         L.hbf_prefix_attention.argtypes = [vp, vp, sz, vp]
         L.hbf_attention_access_count.argtypes = [vp]
         L.hbf_attention_access_count.restype = u64
