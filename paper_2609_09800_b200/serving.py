@@ -346,11 +346,13 @@ class ServedLayer:
 
     def step(self, q, x, scores, issue_ns=0, gap_ns=0):
         """Attention of the requests' queries q [batch, q_heads, head_dim], then the experts on x [batch, hidden] by the router's scores [batch,
-        n_experts].  Returns (attention's output, experts' output, [what ``Context.serve`` returns for each])."""
+        n_experts].  Returns (attention's output, experts' output, [what ``Context.serve`` returns for each]).  A request whose row holds no token
+        (it was freed, or has none yet) attends to nothing: zeros."""
         import torch
         with torch.cuda.stream(self.ctx.stream):
             torch.sub(self.lens[1:], self.base_tokens, out=self.own_len)
-        o = self.attention(q)
+            o = self.attention(q)
+            o.masked_fill_((self.lens[1:] == 0)[:, None, None], 0.0)      # (of a length below the prefix's shared pages `attention` makes NaN)
         a = self.ctx.serve(self.attention, issue_ns, gap_ns)
         y = self.moe(x, scores)
         b = self.ctx.serve(self.moe, issue_ns + gap_ns * a[0].shape[0], gap_ns)

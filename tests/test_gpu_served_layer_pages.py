@@ -141,3 +141,25 @@ def test_a_layer_on_a_stream_of_its_own(torch, mods):
     torch.cuda.synchronize()
     r.check()
     assert r.layer.lens.tolist() == [40] * 21
+
+
+@pytest.mark.parametrize("prefix", [40, 7, 0])
+def test_a_request_without_tokens_attends_to_nothing(torch, mods, prefix):
+    r = Rows(torch, mods, 4, prefix, 30)
+    for _ in range(3):
+        r.append()
+    r.free([2, 4])
+    rnd = lambda *s: torch.randn(*s, device="cuda").bfloat16()
+    q, x, scores = rnd(4, 16, 64), rnd(4, 256), torch.randn(4, 12, device="cuda")
+    out, y, served = r.layer.step(q, x, scores)
+    assert not out[[1, 3]].any() and torch.isfinite(y).all()
+    for b in (0, 2):
+        k, v = torch.stack(r.rows[b + 1]).double().unbind(1)
+        p = torch.softmax(torch.einsum("hgd,lhd->hgl", q[b].double().view(4, 4, 64), k) * 64 ** -0.5, -1)
+        want = torch.einsum("hgl,lhd->hgd", p, v).reshape(16, 64)
+        size = torch.einsum("hgl,lhd->hgd", p, v.abs()).reshape(16, 64)
+        # the output rounded once, the weights at most once, the rest in 32 bits
+        assert ((out[b].double() - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -8 + 2.0 ** -16) * size).all()
+    # the pages of requests without tokens are not read
+    pages = served[0][0][:, 0].view(-1, 2)[prefix // 16:].view(4, -1, 2)
+    assert not pages[[1, 3]].any() and pages[[0, 2], 0].all()
