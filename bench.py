@@ -610,6 +610,7 @@ def run_served(args):
 
     gap = 20                                                  # ns between the accesses of a step
     o, y = torch.empty_like(q), torch.empty_like(x)
+    layer.step(q, x, scores, 0, gap)                          # (a step tells the attention how many tokens each request has)
     attention_us, moe_us = timed(lambda: layer.attention(q, o)), timed(lambda: layer.moe(x, scores, y))
     step_us = timed(lambda: (ctx.reset(), layer.step(q, x, scores, 0, gap)))
     ctx.reset()
