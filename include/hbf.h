@@ -432,8 +432,12 @@ HBF_API int hbf_get_retention_totals(hbf_ctx *ctx, hbf_retention_totals_t *out);
  * ..._workspace_bytes function gives for the same arguments on the same device (0 = arguments refused); two calls that may overlap,
  * on two streams or in two graphs that are replayed at once, need one each.  Every call can be captured into a CUDA graph; a replay reads
  * the tables, lengths and scores anew.  Counts in the structs are fixed at capture.
- * Values are bf16 or fp16, products exact, sums in 32 bits, outputs rounded once.  Kernels that wait on copies or products of their own wait a
- * bounded number of polls; should that run out, what depends on it is NaN and the kernel ends with nothing on its way. */
+ * Values are bf16 or fp16, products exact, sums in 32 bits, outputs rounded once.  What goes from one product into another is held as the
+ * sum of two numbers of the type, with one exception: where many query rows stand before a long prefix (more than 16 a key head, and
+ * more than 48 MiB of keys and values to read again for every 16 of them), the softmax's weights p against the prefix are rounded once to the
+ * type, half of its spacing at 1 relative to each, so the output is off by at most as much of sum p |v| as well.  Kernels that wait on
+ * copies or products of their own wait a bounded number of polls; should that run out, what depends on it is NaN and the kernel ends with
+ * nothing on its way. */
 enum { HBF_BF16 = 0, HBF_FP16 = 1 };
 
 /* Test support, off by default: the polls after which a wait of these kernels gives up, for calls from now on (a captured graph keeps its own); 0:

@@ -320,6 +320,8 @@ k_prefix_tiles(const __grid_constant__ AttnDev p, const __grid_constant__ CUtens
                     }
                     tensor_store16(s_at + half * 32u + c * 16u, w);
                 }
+                // (The weights' sum is of what they were before they were rounded, which the logarithm of the sum needs.  A second sum, of the rounded ones,
+                // to divide by, took 9 % of a call: 128 requests behind 32K 154 us against 141.)
                 float s0, s1;
                 of_two(add_two(sum[0], sum[1]), s0, s1);
                 if (m != -INFINITY) l += s0 + s1;
