@@ -335,15 +335,16 @@ class Context:
                                             _ptr(d_status), _ptr(d_die_stats), _ptr(d_workspace),
                                             d_workspace.numel() * d_workspace.element_size())
 
-    def serve(self, op, issue_ns: int = 0, gap_ns: int = 0):
+    def serve(self, op, issue_ns: int = 0, gap_ns: int = 0, **which):
         """Serves the accesses of an operator's last call (``serving.PrefixAttention``, ``MoeLayer``, ``CachePages``, whose stream
         has to be this context's): its records, ``hbf_submit_batch``.  Returns (records, completion, stall, die stats) as device tensors:
-        int64 [n, 3], [n], [n], [dies, 6]; the outcome is read with ``last_result``."""
+        int64 [n, 3], [n], [n], [dies, 6]; the outcome is read with ``last_result``.  which: what else the operator's ``accesses`` takes to tell
+        its records (moved, of ``CachePages``)."""
         torch = self._torch
         if op.stream.cuda_stream != self.stream.cuda_stream:
             raise ValueError("the operator runs on another stream than the context")
         with torch.cuda.stream(self.stream):
-            acc = op.accesses(issue_ns, gap_ns)
+            acc = op.accesses(issue_ns, gap_ns, **which)
             n = acc.shape[0]
             comp, stall = (torch.empty(n, dtype=torch.int64, device=acc.device) for _ in range(2))
             stats = torch.empty(self.n_dies, 6, dtype=torch.int64, device=acc.device)

@@ -258,13 +258,15 @@ class CachePages(_Operator):
         self._raise(code, self._what)
         return {"moved": moved, "in_use": in_use}
 
-    def access_count(self):
-        return 2 * self._moves * self._p.n_slabs
+    def access_count(self, moved=None):
+        _check(moved is None or 0 <= moved <= self._moves, "the last call moves from 0 to %d pages" % self._moves)
+        return 2 * (self._moves if moved is None else moved) * self._p.n_slabs
 
-    def accesses(self, issue_ns=0, gap_ns=0, out=None):
+    def accesses(self, issue_ns=0, gap_ns=0, out=None, moved=None):
         """Records of the last call's moves, a read and a program for each page and slab: int64 [n, 3]; n is the most that the call can have
-        moved, places past its moves are native."""
-        n = self.access_count()
+        moved, places past its moves are native.  The most is half of all pages for a compaction, however few moved: with moved, which
+        ``result`` tells, there are as many records as that many pages make."""
+        n = self.access_count(moved)
         out = self._records(n, out)
         self._raise(self._lib.hbf_pages_accesses(self._ref, self._ws_ptr, issue_ns, gap_ns, out.data_ptr(), n, self._st) if n else 0, "hbf_pages_accesses")
         return out

@@ -63,3 +63,32 @@ def test_no_records_want_no_room(torch, serving):
     assert op.accesses().shape == (0, 3)
     with pytest.raises(ValueError):
         op.accesses(0, 0, torch.zeros(1, 3, dtype=torch.int64, device="cuda"))
+
+
+def test_records_of_the_pages_that_a_compaction_moved(torch, serving):
+    from paper_2609_09800_b200 import hbf, workloads as wl
+    slabs, pages = 4, 10_000
+    data = torch.zeros(slabs, pages, 8, dtype=torch.int32, device="cuda")
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    refs, lens, tables = torch.zeros(pages, dtype=torch.int32, device="cuda"), ints(6, 4), ints([0, 9_000], [5_000, -1])
+    refs[[0, 5_000, 9_000]] = 1
+    op = serving.CachePages(data, refs, tables, lens, 4)
+    op.compact()
+    moved = op.result()["moved"]
+    assert moved == 2 and op.access_count() == pages * slabs and op.access_count(moved) == 2 * 2 * slabs
+    some, every = op.accesses(100, 3, moved=moved), op.accesses(100, 3)
+    assert torch.equal(some, every[:16]) and (some[:, 0] != 0).all() and not every[16:, 0].any()
+    for wrong in (-1, pages // 2 + 1):
+        with pytest.raises(ValueError):
+            op.accesses(moved=wrong)
+    with pytest.raises(ValueError):
+        op.accesses(0, 0, torch.empty_like(every), moved=moved)
+    ctx = hbf.Context(wl.load_profile("nominal", **wl.GEOMETRY["tiny"]))
+    ctx.register_range(data.data_ptr(), data.numel() * 4, 3)
+    acc, comp, stall, stats = ctx.serve(op, 100, 3, moved=moved)
+    res = ctx.last_result()
+    assert torch.equal(acc, some) and res["code"] == 0 and res["n_modeled"] == 16 and res["n_native"] == 0
+    op.compact()                                             # nothing is left to move: no records, and nothing to serve
+    assert op.result()["moved"] == 0
+    acc, comp, _, _ = ctx.serve(op, 100, 3, moved=0)
+    assert acc.shape == (0, 3) and comp.numel() == 0
