@@ -33,7 +33,7 @@ class _Operator:
         self._dev, self._i32, self._f32 = self.device.index, torch.int32, torch.float32
 
     def _int32(self, t, what, dims):
-        _check(t.dtype == self._torch.int32 and t.dim() == dims and t.device == self.device and (t.numel() == 0 or t.stride(-1) == 1),
+        _check(t.dtype == self._torch.int32 and t.dim() == dims and t.device == self.device and (t.shape[-1] < 2 or t.numel() == 0 or t.stride(-1) == 1),
                "%s has to be an int32 tensor of %d dimension(s) on %s" % (what, dims, self.device))
         return t
 
@@ -57,6 +57,15 @@ class _Operator:
             raise hbf.HbfError(rc, what)
 
 
+def _strides(t):
+    """Strides, those of dimensions of size one (which may be anything) as if the tensor were dense."""
+    out, dense = [], 1
+    for n, st in zip(reversed(t.shape), reversed(t.stride())):
+        out.append(st if n > 1 else dense)
+        dense *= n
+    return tuple(reversed(out))
+
+
 def _dtype_of(t, torch):
     _check(t.dtype in (torch.bfloat16, torch.float16), "values have to be bfloat16 or float16")
     return hbf.BF16 if t.dtype == torch.bfloat16 else hbf.FP16
@@ -72,13 +81,13 @@ class PrefixAttention(_Operator):
     def __init__(self, k, v, batch, q_heads, prefix_pages=None, prefix_len=0, own_pages=None, own_len=None, max_own_len=0, scale=None, stream=None):
         super().__init__(k, stream)
         torch = self._torch
-        _check(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and v.device == self.device and k.stride(3) == 1,
+        _check(k.dim() == 4 and k.shape == v.shape and _strides(k) == _strides(v) and k.dtype == v.dtype and v.device == self.device and k.stride(3) == 1,
                "k and v have to be alike: [pages, page_tokens, kv_heads, head_dim], dense in the last dimension")
         a = self._a = hbf.hbf_attention_t()
         a.kv.n_pages, a.kv.page_tokens, a.kv.kv_heads, a.kv.head_dim = k.shape
         a.kv.dtype = _dtype_of(k, torch)
         a.kv.k, a.kv.v = k.data_ptr(), v.data_ptr()
-        a.kv.page_stride, a.kv.slot_stride, a.kv.head_stride = k.stride()[:3]
+        a.kv.page_stride, a.kv.slot_stride, a.kv.head_stride = _strides(k)[:3]
         a.batch, a.q_heads, a.prefix_len, a.max_own_len = batch, q_heads, prefix_len, max_own_len
         a.scale = scale if scale is not None else a.kv.head_dim ** -0.5
         pages_for = lambda n: -(-n // a.kv.page_tokens)
@@ -96,7 +105,7 @@ class PrefixAttention(_Operator):
         self._ref = C.byref(a)
         self._ws = self._room(self._lib.hbf_attention_workspace_bytes(self._ref))
         self._ws_ptr, self._ws_bytes = self._ws.data_ptr(), self._ws.numel()
-        self._shape, self._dtype = torch.Size((batch, q_heads, k.shape[3])), k.dtype
+        self._shape, self._dtype, self._alone = torch.Size((batch, q_heads, k.shape[3])), k.dtype, batch == 1 or q_heads == 1
 
     def __call__(self, q, out=None, lse=None):
         """q: [batch, q_heads, head_dim]; returns out (made if not given).  lse: float32 [batch, q_heads], filled if given."""
@@ -111,6 +120,8 @@ class PrefixAttention(_Operator):
             _check(lse.shape == self._shape[:2] and lse.dtype == self._torch.float32 and lse.device == self.device and lse.is_contiguous(), "lse has to be float32 [batch, q_heads]")
         a = self._a
         a.q, a.out, a.lse = q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr()
+        if self._alone:                                      # (one row, or one head)
+            qs, os = _strides(q), _strides(out)
         a.q_row_stride, a.q_head_stride, a.out_row_stride, a.out_head_stride = qs[0], qs[1], os[0], os[1]
         rc = self._lib.hbf_prefix_attention(self._ref, self._ws_ptr, self._ws_bytes, self._st)
         if rc:
@@ -161,7 +172,7 @@ class MoeLayer(_Operator):
         if n > self.max_tokens or x.shape != want or out.shape != want or x.dtype is not self._dtype or out.dtype is not self._dtype or xs[1] != 1 or os[1] != 1 or \
                 x.get_device() != dev or out.get_device() != dev:
             raise ValueError("x and out have to be [tokens <= max_tokens, hidden] of the experts' type, rows dense")
-        if scores.shape != (n, m.n_experts) or scores.dtype is not self._f32 or scores.get_device() != dev or ss[1] != 1:
+        if scores.shape != (n, m.n_experts) or scores.dtype is not self._f32 or scores.get_device() != dev or (ss[1] != 1 and m.n_experts > 1):
             raise ValueError("scores has to be float32 [tokens, n_experts], rows dense")
         for t, dt in ((chosen, self._i32), (weights, self._f32)):
             if t is not None and (t.shape != (n, m.top_k) or t.dtype is not dt or t.get_device() != dev or not t.is_contiguous()):
