@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import os
+import re
 import subprocess
 import sys
 
@@ -17,6 +18,9 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
 # (measured: relocatable code costs the in-order serve kernel about 1.3 %).
 RDC_SOURCES = {"submit_kernels.cu"}
 OBJ_DIR = os.path.join(HERE, "build")
+# Kernels whose warps share out the registers that a block is launched with: their source counts on exactly so many a thread (a share past the
+# launch's would wait for good), so another number ends the build.  (The launch looks again, and refuses.)
+REGISTERS = {"prefix_kernels.cu": {"k_prefix_tiles": 80}}
 
 
 def _nvcc() -> str:
@@ -24,6 +28,16 @@ def _nvcc() -> str:
         if cand and (os.path.sep not in cand or os.path.exists(cand)):
             return cand
     return "nvcc"
+
+
+def check_registers(wanted: dict, ptxas_log: str) -> None:
+    """Raises if a kernel of `wanted` (a part of its name: registers a thread) is missing in what ``ptxas -v`` printed or has another number."""
+    got = re.findall(r"Compiling entry function '(\w+)'.*?Used (\d+) registers", ptxas_log, re.S)
+    for name, registers in wanted.items():
+        have = {int(n) for entry, n in got if name in entry}
+        if have != {registers}:
+            raise RuntimeError("%s was compiled to %s registers a thread; its shares of the block's registers are made for %d"
+                               % (name, sorted(have) or "no", registers))
 
 
 def is_stale() -> bool:
@@ -49,7 +63,15 @@ def build(force: bool = False, verbose: bool = False, extra_flags=(), out: str |
     def compile_one(src):
         obj = os.path.join(OBJ_DIR, src.replace(".cu", tag + ".o"))
         mode = ["-dc"] if src in RDC_SOURCES else ["-c"]
-        subprocess.check_call([nvcc] + NVCC_FLAGS + extra + mode + [os.path.join(CSRC, src), "-o", obj])
+        cmd = [nvcc] + NVCC_FLAGS + extra + mode + [os.path.join(CSRC, src), "-o", obj]
+        if src not in REGISTERS:
+            subprocess.check_call(cmd)
+            return obj
+        run = subprocess.run(cmd + ([] if verbose else ["-Xptxas", "-v"]), stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        if run.returncode or verbose:
+            print(run.stdout, file=sys.stderr, end="")
+        run.check_returncode()
+        check_registers(REGISTERS[src], run.stdout)
         return obj
 
     with ThreadPoolExecutor(max(1, min(len(SOURCES), os.cpu_count() or 1))) as pool:
