@@ -460,7 +460,8 @@ typedef struct {
  * A row without any key is zeros.  What lies in a page behind a sequence's end is not read into the result, whatever it is.  A page
  * number outside 0..n_pages-1, or a length outside 0..max_own_len, makes the rows that need it NaN (nothing is read there).
  * lse (nullable, [batch][q_heads]): natural logarithm of the sum of exp(scale * q k_i), -inf for a row without keys.
- * q and out: rows and heads at their strides (multiples of 8), 16-byte aligned; out may be q.  Lengths up to HBF_ATTENTION_MAX_LEN. */
+ * q and out: rows and heads at their strides (multiples of 8; out's not 0), 16-byte aligned; out may be q, and otherwise
+ * shares no memory with it.  Lengths up to HBF_ATTENTION_MAX_LEN. */
 #define HBF_ATTENTION_MAX_LEN (1u << 30)
 typedef struct {
     hbf_kv_t kv;

@@ -491,6 +491,7 @@ extern "C" int hbf_prefix_attention(const hbf_attention_t *a, void *d_workspace,
     if (a->batch == 0) return HBF_OK;
     if (!attention_pointers_ok(a) || !a->q || !a->out || (uintptr_t)a->q % 16 || (uintptr_t)a->out % 16 || (uintptr_t)a->lse % 4) return HBF_E_INVAL;
     if (a->q_row_stride % 8 || a->q_head_stride % 8 || a->out_row_stride % 8 || a->out_head_stride % 8) return HBF_E_INVAL;
+    if ((a->batch > 1 && a->out_row_stride == 0) || (a->q_heads > 1 && a->out_head_stride == 0)) return HBF_E_INVAL;      // rows on top of each other
     uint32_t n_sm = 0;
     const int rc = device_of(a->kv.k, &n_sm);
     if (rc != HBF_OK) return rc;
