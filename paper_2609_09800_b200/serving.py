@@ -33,7 +33,7 @@ class _Operator:
         self._dev, self._i32, self._f32 = self.device.index, torch.int32, torch.float32
 
     def _int32(self, t, what, dims):
-        _check(t.dtype == self._torch.int32 and t.dim() == dims and t.device == self.device and (t.shape[-1] < 2 or t.numel() == 0 or t.stride(-1) == 1),
+        _check(t is not None and t.dtype == self._torch.int32 and t.dim() == dims and t.device == self.device and (t.shape[-1] < 2 or t.numel() == 0 or t.stride(-1) == 1),
                "%s has to be an int32 tensor of %d dimension(s) on %s" % (what, dims, self.device))
         return t
 
@@ -209,7 +209,7 @@ class CachePages(_Operator):
     def __init__(self, data, refs, tables, lens, page_tokens, stream=None):
         super().__init__(data, stream)
         torch = self._torch
-        _check(data.dim() >= 3 and data[0, 0].is_contiguous(), "data has to be [slabs, pages, ...] with dense pages")
+        _check(data.dim() >= 3 and data.numel() > 0 and data[0, 0].is_contiguous(), "data has to be [slabs, pages, ...] with dense pages")
         self._int32(refs, "refs", 1), self._int32(tables, "tables", 2), self._int32(lens, "lens", 1)
         _check(refs.numel() == data.shape[1] and lens.numel() == tables.shape[0], "refs has to hold the pages, lens the rows")
         p = self._p = hbf.hbf_pages_t()

@@ -49,3 +49,14 @@ def test_pages_of_one(torch, serving):  # noqa: F811
     plan = serving.CachePages(odd(data, 5, None, None), refs, odd(tables, 7, 9), odd(lens, 3), 4)
     plan.compact()
     assert plan.result() == {"moved": 1, "in_use": 1} and tables.tolist() == [[0]] and torch.equal(data[0, 0], before[0, 4])
+
+
+def test_what_is_not_there(torch, serving):  # noqa: F811
+    c = Attention(torch, 2, 8, 2, 64, 16, 40, 20, poison=False)
+    for args in ((None, 40, c.op, c.lens, 20), (c.pp, 40, None, c.lens, 20), (c.pp, 40, c.op, None, 20)):
+        with pytest.raises(ValueError):
+            serving.PrefixAttention(c.k, c.v, 2, 8, *args)
+    ints = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")
+    for shape in ((0, 4, 8), (2, 0, 8), (2, 4, 0)):
+        with pytest.raises(ValueError):
+            serving.CachePages(ints(*shape), ints(shape[1]), ints(2, 3), ints(2), 4)
