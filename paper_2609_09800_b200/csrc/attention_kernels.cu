@@ -463,8 +463,9 @@ static cudaError_t launch_attention(AttnDev p, bool bf16, cudaStream_t st) {
     }
     if (p.pieces == 1u) return e;
     g_kernel_launches += 1;
-    // many rows: two warps each (64 requests, 17 pieces a row: 43.1 us, with eight 45.1), else eight
-    const uint32_t per = p.B * p.Hq >= 1024u && p.pieces <= kMostPieces / 4u ? 2u : kJoinWarps, rows = kJoinWarps / per;
+    // many rows: two warps each, else eight.  The whole call with two and with eight, 8K keys in common and 512 of each: 512 rows 22.8 and 19.3 us,
+    // 1,024 28.4 and 24.9, 1,280 29.9 and 30.8, 2,048 35.5 and 38.7, 4,096 55.4 and 66.8; 32K in common 1,280 rows 49.7 and 49.3; none 36.6 and 38.6.
+    const uint32_t per = p.B * p.Hq > 1024u && p.pieces <= kMostPieces / 4u ? 2u : kJoinWarps, rows = kJoinWarps / per;
     const auto join = per == 2u ? k_attend_join<Ty, D, 2> : k_attend_join<Ty, D, kJoinWarps>;
     const uint32_t blocks = (p.B * p.Hq + rows - 1u) / rows;
     if (p.pieces == 0u) { join<<<blocks, kJoinWarps * 32, 0, st>>>(p); return cudaGetLastError(); }
