@@ -407,8 +407,10 @@ static int pages_call(const hbf_pages_t *p, const int32_t *a, const int32_t *b, 
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const size_t smem = ((size_t)mark_bits + 31u) / 32u * 4u;
     if (ensure_dyn_smem((const void *)plan, smem + 1024u) != cudaSuccess) return HBF_E_CUDA;          // (with what the plans hold besides)
-    // up to 128 KB to move and 32 entries a thread, one block is done about when a second kernel would begin
-    const int alone = most_moves * p->n_slabs * p->page_bytes <= 128u * 1024u && entries <= 32u * kPlanThreads;
+    // One block alone while it is done about when a second kernel would begin.  A copy alone and with one: 32 KB 3.3 and 4.5 us, 64 KB 4.1 and 4.6,
+    // 80 KB 4.6 and 4.6, 128 KB 5.6 and 4.6; rows freed: 1,024 entries 3.3 and 3.8, 2,048 3.8 and 3.9, 4,096 4.8 and 3.9, 32,768 18.4 and 4.2 (in a
+    // graph; launched one by one 64 KB take 6.2 and 10.1).
+    const int alone = most_moves * p->n_slabs * p->page_bytes <= 64u * 1024u && entries <= 2u * kPlanThreads;
     plan<<<1, kPlanThreads, smem, st>>>(d, args..., alone);
     if (cudaGetLastError() != cudaSuccess) return HBF_E_CUDA;
     if (alone) { g_kernel_launches += 1; return HBF_OK; }
