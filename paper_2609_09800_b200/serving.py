@@ -335,6 +335,8 @@ class ServedLayer:
         (holds less than the prefix; without a prefix an empty row is a request without tokens).  Returns who took it, bool [batch], on the
         device."""
         import torch
+        want, dev = (self.batch,) + tuple(self.kv.shape[3:]), self.kv.device
+        _check(all(tuple(t.shape) == want and t.dtype == self.kv.dtype and t.device == dev for t in (k, v)), "k and v have to be %s %s on %s" % (self.kv.dtype, want, dev))
         with torch.cuda.stream(self.ctx.stream):
             rows, lens, nobody = self.tables[1:], self.lens[1:], self.kv.shape[1] - 1
             last = self.tables.shape[1] - 1                       # (an entry of -1, past the room)
@@ -350,10 +352,10 @@ class ServedLayer:
             taken = torch.where(begins, lowest[(begins.cumsum(0) - 1).clamp_(min=0)], -1)
             page = torch.where(begins, taken, rows.gather(1, col[:, None])[:, 0].long())
             took = fits & (page >= 0) & (page < nobody)
+            place = torch.where(took, page, nobody)
+            self.kv[0, place, at], self.kv[1, place, at] = k, v
             rows.scatter_(1, col[:, None], torch.where(took, page, rows.gather(1, col[:, None])[:, 0].long()).int()[:, None])
-            page = torch.where(took, page, nobody)
-            self.refs.index_add_(0, page, (begins & took).int())
-            self.kv[0, page, at], self.kv[1, page, at] = k, v
+            self.refs.index_add_(0, place, (begins & took).int())
             lens += took
         return took
 

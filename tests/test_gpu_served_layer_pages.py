@@ -163,3 +163,15 @@ def test_a_request_without_tokens_attends_to_nothing(torch, mods, prefix):
     # the pages of requests without tokens are not read
     pages = served[0][0][:, 0].view(-1, 2)[prefix // 16:].view(4, -1, 2)
     assert not pages[[1, 3]].any() and pages[[0, 2], 0].all()
+
+
+def test_a_refused_token_takes_no_page(torch, mods):
+    r = Rows(torch, mods, 3, 16, 40)
+    good, L = torch.randn(3, 4, 64, device="cuda").bfloat16(), r.layer
+    for bad in (good.float(), good[:2], good[:, :3], good.cpu(), good[:, :, :32], good[None], good[:1]):
+        for k, v in ((good, bad), (bad, good)):
+            with pytest.raises(ValueError):
+                L.append(k, v)
+    r.check()                                                # a page of its own would have begun
+    r.append()
+    r.check()
