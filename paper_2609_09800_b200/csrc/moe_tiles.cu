@@ -196,7 +196,6 @@ k_moe_up_tiles(const __grid_constant__ MoeDev m, const __grid_constant__ UpMaps 
             wait(acc_full + buf * 8u, (it >> 1) & 1u);
             __syncwarp();
             tensor_fence_after();
-            const bool sound = live && !ld_flag(smem_addr(&sh.gave_up));
             uint32_t v[32];
             tensor_load(sh.tmem + buf * 32u + ((warp * 32u) << 16), v);   // (columns past the tokens hold anything)
             tensor_loaded(v);
@@ -209,6 +208,7 @@ k_moe_up_tiles(const __grid_constant__ MoeDev m, const __grid_constant__ UpMaps 
                 for (int c = 0; c < kMtChunk; ++c) if ((uint32_t)c < n) up[c * 64 + row] = __uint_as_float(v[c]);
             }
             barrier_of(1, 128);                              // (the buffer after next is written behind the next one's barrier)
+            const bool sound = live && !ld_flag(smem_addr(&sh.gave_up));          // (here: the other rows' threads may have given up)
             if (warp < 2u && row < rows && i0 + row < m.I) {
 #pragma unroll
                 for (int c = 0; c < kMtChunk; ++c)
