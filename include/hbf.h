@@ -457,7 +457,8 @@ typedef struct {
  * kv_heads), out = sum_i softmax(scale * q k_i) v_i over the prefix_len keys in prefix_pages and then the own_len[b] keys in
  * own_pages[b * own_pages_stride ...].  The prefix is read once for the batch.  prefix_pages [ceil(prefix_len / page_tokens)]; own_len
  * [batch], 0..max_own_len; own_pages_stride >= ceil(max_own_len / page_tokens); with max_own_len 0 both may be NULL.
- * A row without any key is zeros.  What lies in a page behind a sequence's end is not read into the result, whatever it is.  A page
+ * A row without any key is zeros.  What lies in a page behind a sequence's end is not read into the result, whatever it is.  An infinite value in
+ * use is infinite or NaN in the result: NaN where its weight is next to nothing (in fp16 below some 2^-32 of the row's largest weight).  A page
  * number outside 0..n_pages-1, or a length outside 0..max_own_len, makes the rows that need it NaN (nothing is read there).
  * lse (nullable, [batch][q_heads]): natural logarithm of the sum of exp(scale * q k_i), -inf for a row without keys.
  * q and out: rows and heads at their strides (multiples of 8; out's not 0), 16-byte aligned; out may be q, and otherwise
@@ -474,7 +475,7 @@ typedef struct {
 } hbf_attention_t;
 HBF_API size_t hbf_attention_workspace_bytes(const hbf_attention_t *a);
 HBF_API int hbf_prefix_attention(const hbf_attention_t *a, void *d_workspace, size_t workspace_bytes, void *cuda_stream);
-/* Records of the step's reads, n = hbf_attention_access_count(a): two per page (keys, values), whole pages, the prefix's once, then
+/* Records of the step's reads, n = hbf_attention_access_count(a): two per page (keys, values), whole pages, the prefix's once (for a batch of 0, too), then
  * ceil(max_own_len / page_tokens) pages for every request in turn; record i is issued at issue_ns + i * gap_ns.  Pages that a request does not
  * have (its length is read on the device), or that are none, give records of one byte at address 0, which is outside every range (so not to be
  * used with a range registered at 0).  Needs pages that are one stretch of memory (HBF_E_INVAL otherwise).  q and out may be NULL here. */
@@ -486,7 +487,7 @@ HBF_API int hbf_attention_accesses(const hbf_attention_t *a, int64_t issue_ns, i
  * out[t] = sum over the chosen of weight * down_e (silu(gate_e x_t) * (up_e x_t)).  Expert e's matrices lie one behind the other at experts +
  * e * expert_stride: gate [inter][hidden], up [inter][hidden], down [hidden][inter].  hidden and inter multiples of 8 up to 2^20, x and experts
  * 16-byte aligned, x_stride and expert_stride multiples of 8.  silu(..) * (..) * weight is held between the products as the sum of two
- * numbers of the values' type (in fp16 its magnitude must stay below 65,504, as the output's).
+ * numbers of the values' type (in fp16 its magnitude must stay below 65,504, as the output's), so that an infinity in a down matrix may give NaN.
  * A score of -inf is never chosen; a token with fewer than top_k others has -1 (weight 0) in the places left, and zeros when none is.  A token
  * with a NaN among its scores has no choice: chosen -1, out NaN.  chosen [tokens][top_k], weights [tokens][top_k]: nullable outputs. */
 #define HBF_MOE_MAX_TOKENS 128

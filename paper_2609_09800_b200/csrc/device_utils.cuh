@@ -26,7 +26,9 @@ __device__ __forceinline__ void st_relaxed_s64(int64_t *p, int64_t v) {
 
 // Programmatic dependent launch: a kernel launched with the attribute may begin while the one before it still runs; up to its
 // pdl_wait it touches only what no kernel writes, and behind it everything the kernels before left is visible.  Every path of
-// such a kernel passes its pdl_wait (the kernel behind it counts on that).  pdl_trigger lets the next one begin.
+// such a kernel passes its pdl_wait (the kernel behind it counts on that).  pdl_trigger lets the next one begin.  (Two operators' kernels are told apart
+// from this rule where they are launched: k_attend behind k_prefix_tiles, of which one block waits, and k_moe_down_tiles, which reads in front of its wait
+// what the kernel before the last wrote.)
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 

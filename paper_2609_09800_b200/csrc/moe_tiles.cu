@@ -374,6 +374,8 @@ static cudaError_t launch_tiles(const MoeDev &m, uint32_t n_sm, cudaStream_t st)
     k_moe_choose<<<m.T, 32, 0, st>>>(m);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     g_kernel_launches += 4;
+    // k_moe_down_tiles may begin when every block of the up kernel has let it, which each does behind its own pdl_wait: the choice, written one kernel
+    // before that, is there, and is read in front of the wait.  What the up kernel writes is read behind it (warps 4 to 7 of every block).
     if ((e = launch_pdl(up, n_sm, kMoeThreads, kUpTilesSmem, st, m, up_maps)) != cudaSuccess) return e;
     if ((e = launch_pdl(down, (m.D + 127u) / 128u * m.groups, kMoeThreads, down_tiles_smem(m.T), st, m, down_map)) != cudaSuccess) return e;
     return launch_pdl(k_moe_sum<Ty>, (unsigned)(((uint64_t)m.T * (m.D / 2u) + 255u) / 256u), 256, 0, st, m);

@@ -290,8 +290,8 @@ class ServedLayer:
     Row 0 of the cache holds the shared prefix; the requests, rows 1 to batch, are forked from it, so that they share its full pages and
     begin with a copy of a page that it had begun; each then has room for own_tokens more, on pages that ``append`` takes as it comes to them.
     A page in use is thus always one that some row's length counts, as ``cache`` (a ``CachePages``) has it: requests may be freed through it,
-    begin again as a fork of row 0 or of another request, and the cache may be compacted, in any order.  Values are random (seed).  All of it
-    runs on the context's stream; tensors of another stream are the caller's to order before it."""
+    begin again as a fork of row 0 or of another request, and the cache may be compacted, in any order.  Row 0 stays: attention reads the prefix by its
+    table.  Values are random (seed).  All of it runs on the context's stream; tensors of another stream are the caller's to order before it."""
 
     def __init__(self, ctx, batch=64, prefix_tokens=8192, own_tokens=64, page_tokens=16, hidden=2048, inter=768, n_experts=128, top_k=8, q_heads=32,
                  kv_heads=4, head_dim=128, seed=0):
@@ -321,7 +321,7 @@ class ServedLayer:
         self.cache.fork(parents, self._rows)
         self.cache.result()
         self.prefix_tokens, self.base_tokens = prefix_tokens, full * page_tokens
-        self.attention = PrefixAttention(self.kv[0], self.kv[1], batch, q_heads, self.tables[0, :full].contiguous() if full else None, self.base_tokens,
+        self.attention = PrefixAttention(self.kv[0], self.kv[1], batch, q_heads, self.tables[0, :full] if full else None, self.base_tokens,
                                          self.tables[1:, full:], self.own_len, mine * page_tokens, stream=ctx.stream)
         self.moe = MoeLayer(self.experts, hidden, inter, top_k, batch, stream=ctx.stream)
         offset = 0
